@@ -255,6 +255,106 @@ const char* conv1d_kernel_name(int pass, int N, int C, int K, int W, int S, int 
 /* Human-readable text for a conv1d_status_t (static storage). */
 const char* conv1d_status_string(int status);
 
+/* ==== Sequence operators =======================================================
+ * What stands beside the layer in a network over long sequences, in the layer's
+ * own layout (samples, channels, positions): a short causal convolution of every
+ * channel by itself, a selective state space scan, and the clipping of gradients.
+ * Rules of pointers, streams, errors and threads as above, and:
+ *   - inputs and the forward outputs are contiguous along the sequence; samples
+ *     (sn) and channels (sd, sc) may be any number of elements apart, so that the
+ *     halves of a projection need no copy.  Rows may begin at any element.
+ *     Strides must not make elements of an output coincide.  Gradients, weights
+ *     and states are contiguous.
+ *   - x, w, dy and what is named "dtype" below share one type; sums are in FP32,
+ *     y, dx and the other outputs in that type are rounded once, at the end.
+ *   - lengths: device, N ints, or NULL.  Positions from lengths[n] on (brought into
+ *     [0, L]) are not part of sequence n: whatever stands there is not used, outputs
+ *     and gradients are 0 there, and the final state is the one before them.  A
+ *     sequence may be empty.
+ *   - an infinite or NaN input reaches the outputs of its own sequence (and group)
+ *     alone, and parameters' gradients.
+ * Sums over samples and positions are added in a fixed order. */
+
+/* Depthwise causal convolution, S <= 8 taps (more: CONV1D_EUNSUPPORTED):
+ *   p[n][c][t] = bias[c] + sum_{s<S} w[c][s] * xe[n][c][t + s],  xe = the S - 1 inputs before the sequence, then x
+ *   y = p, or p * sigmoid(p) with CONV1D_CAUSAL_SILU. */
+#define CONV1D_CAUSAL_SILU 1
+typedef struct {
+    const void* x;        /* [N][C][L] dtype, sn and sc elements apart */
+    const void* w;        /* [C][S] dtype */
+    const float* bias;    /* [C] or NULL */
+    const void* init;     /* [N][C][S - 1] dtype, oldest first, or NULL: zeros */
+    const int* lengths;   /* [N] or NULL */
+    long x_sn, x_sc;
+    int N, C, L, S, dtype, flags;
+} conv1d_causal_t;
+
+/* final: [N][C][S - 1] dtype, the last S - 1 elements of xe, or NULL if it is not wanted.  It may not be init. */
+int conv1d_causal_fwd(const conv1d_causal_t* p, void* y, long y_sn, long y_sc, void* final, void* stream);
+
+/* Gradients for dy (and dfinal: [N][C][S - 1] dtype or NULL) of the call that p describes:
+ *   dx [N][C][L] dtype;  dw [C][S] float or NULL;  dbias [C] float or NULL (wanted with dw only);  dinit [N][C][S - 1] dtype or NULL.
+ * workspace: 4-byte aligned, conv1d_causal_bwd_workspace_bytes(...) bytes, where dw is wanted. */
+size_t conv1d_causal_bwd_workspace_bytes(int N, int C, int L, int S);
+int conv1d_causal_bwd(const conv1d_causal_t* p, const void* dy, long dy_sn, long dy_sc, const void* dfinal, void* dx, float* dw,
+                      float* dbias, void* dinit, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One position of every sequence: x and y [N][C] (x_sn and y_sn elements apart; L must be 1, init and lengths NULL),
+ * state [N][C][S - 1] dtype, read and replaced by the inputs that the next position needs (NULL for S = 1). */
+int conv1d_causal_step(const conv1d_causal_t* p, void* state, void* y, long y_sn, void* stream);
+
+/* Selective state space scan, S <= 64 states (more: CONV1D_EUNSUPPORTED), N * D < 2^25.  For sample n, channel d of group g:
+ *   e[t] = dt[n][d][t] + dt_bias[d], through log(1 + exp(.)) with CONV1D_SCAN_SOFTPLUS
+ *   h[s] = exp(e[t] A[d][s]) h[s] + e[t] x[n][d][t] B[n][g][s][t],   h = init before the first position
+ *   y[t] = (sum_s C[n][g][s][t] h[s] + skip[d] x[n][d][t]) * (z ? z[n][d][t] sigmoid(z[n][d][t]) : 1)
+ * The D channels are G groups of D / G neighbours, which share B and C. */
+#define CONV1D_SCAN_SOFTPLUS 1
+typedef struct {
+    const void *x, *dt;              /* [N][D][L] dtype */
+    const void *B, *C;               /* [N][G][S][L] dtype; groups sg, states ss elements apart */
+    const void* z;                   /* [N][D][L] dtype, or NULL: no gate */
+    const float* A;                  /* [D][S] */
+    const float *skip, *dt_bias;     /* [D] or NULL */
+    const float* init;               /* [N][D][S] or NULL: zeros */
+    const int* lengths;              /* [N] or NULL */
+    long x_sn, x_sd, dt_sn, dt_sd, z_sn, z_sd, b_sn, b_sg, b_ss, c_sn, c_sg, c_ss;
+    int N, D, L, S, G, dtype, flags;
+} conv1d_scan_t;
+
+/* final: [N][D][S] float or NULL; it may not be init.  saved: what conv1d_scan_bwd needs, conv1d_scan_saved_bytes(...) bytes,
+ * 16-byte aligned, or NULL without a backward pass.  workspace: 256-byte aligned, for the bytes asked for (0: NULL will do). */
+size_t conv1d_scan_fwd_workspace_bytes(int N, int D, int L, int S, int G);
+size_t conv1d_scan_saved_bytes(int N, int D, int L, int S);
+int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float* final, void* saved, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* Gradients for dy (and dfinal: [N][D][S] float or NULL) of the forward call that p describes and that wrote `saved`:
+ *   dx, ddt [N][D][L] dtype;  dA [D][S] float;  dB, dC [N][G][S][L] dtype;  dz [N][D][L] dtype, where there is a gate, NULL
+ *   elsewhere;  dskip, ddt_bias [D] float, or NULL if not wanted;  dinit [N][D][S] float or NULL.
+ * workspace: 256-byte aligned. */
+size_t conv1d_scan_bwd_workspace_bytes(int N, int D, int L, int S, int G);
+int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_sd, const float* dfinal, const void* saved, void* dx,
+                    void* ddt, float* dA, void* dB, void* dC, float* dskip, void* dz, float* ddt_bias, float* dinit, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* One position of every sequence: x, dt, z and y [N][D] (sn elements apart), B and C [N][G][S] (states contiguous), L = 1,
+ * init and lengths NULL; state [N][D][S] float, updated in place. */
+int conv1d_scan_step(const conv1d_scan_t* p, float* state, void* y, long y_sn, void* stream);
+
+/* Norm over all elements of `tensors` tensors of counts[i] contiguous elements of dtypes[i] at the device address data[i]
+ * (the three arrays are read on the host before the call returns): the root of the sum of squares, summed in 64 bits, or the
+ * largest magnitude; NaN where an element is.  norm: device, one float.  workspace: 8-byte aligned. */
+#define CONV1D_NORM_2 2
+#define CONV1D_NORM_MAX 0
+size_t conv1d_grad_norm_workspace_bytes(const size_t* counts, int tensors);
+int conv1d_grad_norm(void* const* data, const size_t* counts, const int* dtypes, int tensors, int kind, float* norm, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Scales every element in place by min(1, most / (norm + 1e-6)), the factor rounded to float: 0 for an infinite norm, NaN for
+ * NaN.  norm: device, one float, as conv1d_grad_norm leaves it (or summed over ranks since).  CONV1D_EINVAL where two of the
+ * tensors share memory. */
+int conv1d_grad_clip(void* const* data, const size_t* counts, const int* dtypes, int tensors, const float* norm, float most, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

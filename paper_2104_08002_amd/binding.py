@@ -23,6 +23,10 @@ EXPORTS = (
     "conv1d_bwd_weight_workspace_bytes", "conv1d_bwd_workspace_bytes", "conv1d_bwd",
     "conv1d_bwd_ex", "conv1d_relu_mask", "conv1d_epilogue_bwd_workspace_bytes", "conv1d_epilogue_bwd",
     "conv1d_bwd_weight", "conv1d_bwd_weight_noalloc", "conv1d_set_variant", "conv1d_kernel_name", "conv1d_status_string",
+    # the sequence operators: marshalled in sequence.py and gradients.py
+    "conv1d_causal_fwd", "conv1d_causal_bwd_workspace_bytes", "conv1d_causal_bwd", "conv1d_causal_step",
+    "conv1d_scan_fwd_workspace_bytes", "conv1d_scan_saved_bytes", "conv1d_scan_fwd", "conv1d_scan_bwd_workspace_bytes",
+    "conv1d_scan_bwd", "conv1d_scan_step", "conv1d_grad_norm_workspace_bytes", "conv1d_grad_norm", "conv1d_grad_clip",
 )
 
 _lib = None
@@ -81,6 +85,24 @@ def load() -> ctypes.CDLL:
     lib.conv1d_kernel_name.argtypes = [i] + geom + [i]
     lib.conv1d_status_string.restype = ctypes.c_char_p
     lib.conv1d_status_string.argtypes = [i]
+    l, f = ctypes.c_long, ctypes.c_float
+    for name, restype, argtypes in (
+        ("conv1d_causal_fwd", i, [vp, vp, l, l, vp, vp]),
+        ("conv1d_causal_bwd_workspace_bytes", sz, [i] * 4),
+        ("conv1d_causal_bwd", i, [vp, vp, l, l] + [vp] * 6 + [sz, vp]),
+        ("conv1d_causal_step", i, [vp, vp, vp, l, vp]),
+        ("conv1d_scan_fwd_workspace_bytes", sz, [i] * 5),
+        ("conv1d_scan_saved_bytes", sz, [i] * 4),
+        ("conv1d_scan_fwd", i, [vp, vp, l, l, vp, vp, vp, sz, vp]),
+        ("conv1d_scan_bwd_workspace_bytes", sz, [i] * 5),
+        ("conv1d_scan_bwd", i, [vp, vp, l, l] + [vp] * 12 + [sz, vp]),
+        ("conv1d_scan_step", i, [vp, vp, vp, l, vp]),
+        ("conv1d_grad_norm_workspace_bytes", sz, [vp, i]),
+        ("conv1d_grad_norm", i, [vp, vp, vp, i, i, vp, vp, sz, vp]),
+        ("conv1d_grad_clip", i, [vp, vp, vp, i, vp, f, vp]),
+    ):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = restype, argtypes
     _lib = lib
     return lib
 

@@ -1,0 +1,130 @@
+// The selective scan: arguments and tile shape shared by its forward and backward kernels.  Not part of the public ABI.
+//
+//   e = dt + dt_bias[d], through softplus if asked;  a[s] = exp(e A[d][s])
+//   h[s] = a[s] h[s] + e x B[s];  y = sum_s C[s] h[s] + skip[d] x;  out = y z sigmoid(z)
+// for every sample n and channel d, S states each; B and C are shared by the D / G channels of a group.
+//
+// Lanes.  P = 1, 2, 4, 8 or 16 neighbouring lanes have one channel, kK = 4 states each, in registers (S is padded to 4 P with
+// zeros); a wave has 64 / P channels.  One step costs a lane 4 exponentials (a quarter of the rate of a product) and 16
+// products: 8 issue slots per state, which is what bounds the scan.  Rows lie along the sequence, states across lanes: a tile
+// of kTile steps goes through LDS, loaded and stored along rows (8 elements a lane), read step by step.
+// Positions behind a sequence's length have e = 0 and e x = 0, which leaves the state as it is.
+#pragma once
+
+#include "conv1d_sequence.h"
+
+namespace conv1d {
+
+constexpr int kK = 4;         // states of a lane
+constexpr int kSub = 16;      // steps between the states that the forward pass keeps for the backward pass
+constexpr int kScanWaves = 4; // most waves of a workgroup
+constexpr int kMostStates = 64;
+
+struct ScanArgs {
+    const void *x, *dt, *B, *C, *z;  // z: nullptr: no gate
+    const float *A, *skip, *dt_bias, *init;
+    const int* lengths;
+    void* out;
+    float* final;      // [N][D][S] or nullptr
+    float* saved;      // [N][chunks][D][4 P]: the state before every kSub-th step, or nullptr
+    float* starts;     // [N][nseg][D][4 P]: state before each segment (split only)
+    float* sums;       // [N][nseg][D]: sum of e over each segment
+    int N, D, L, S, G, Dg, softplus;
+    long x_sn, x_sd, dt_sn, dt_sd, z_sn, z_sd, out_sn, out_sd;
+    long b_sn, b_sg, b_ss, c_sn, c_sg, c_ss;
+    int nseg, seg_len; // the sequence in segments of seg_len steps, a multiple of 64
+    int chunks;        // ceil(L / kSub)
+    int blocks_d;      // workgroups along the channels of a group
+    long first;        // first workgroup of the launch
+    // backward
+    const void* dout;
+    long dout_sn, dout_sd;
+    const float* dfinal;
+    void *dx, *ddt, *dz, *dB, *dC;   // contiguous, in the type of x
+    float* part_bc;    // [2][blocks_d][N][G][S][L]: sums over a workgroup's channels (blocks_d > 1)
+    float* part_a;     // [N * nseg][D][4 P]
+    float* part_d;     // [2][N * nseg][D]: of skip and of dt_bias
+    float* carries;    // [N][nseg][D][4 P]: what the later segments send into each (split only)
+    float* dinit;      // [N][D][S] or nullptr
+};
+
+// steps of a tile: a wave has 64 / P rows of it, 1024 elements where the tile of B and C leaves room
+constexpr int scan_tile(int P) { return P >= 4 ? 64 : 16 * P; }
+
+// sum over the P lanes of a channel, in all of them
+#ifdef HOSTMODEL
+template <int P>
+inline float channel_sum(float v) { return v; }
+#else
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int P>
+__device__ __forceinline__ float channel_sum(float v) {
+    if constexpr (P >= 2) v = add_dpp<0xB1>(v);    // quad_perm 1,0,3,2
+    if constexpr (P >= 4) v = add_dpp<0x4E>(v);    // quad_perm 2,3,0,1
+    if constexpr (P >= 8) v = add_dpp<0x141>(v);   // row_half_mirror: the other quad, whose lanes agree
+    if constexpr (P >= 16) v = add_dpp<0x140>(v);  // row_mirror
+    return v;
+}
+#endif
+
+// where a workgroup works: sample, group, segment, its channels
+struct ScanPlace {
+    long n;
+    int g, seg, cb;
+};
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
+    long b = a.first + blockIdx.x;
+    ScanPlace p;
+    long q = b / a.blocks_d;
+    p.cb = static_cast<int>(b - q * a.blocks_d);
+    b = q / a.nseg;
+    p.seg = static_cast<int>(q - b * a.nseg);
+    p.n = b / a.G;
+    p.g = static_cast<int>(b - p.n * a.G);
+    return p;
+}
+
+// state k of lane-in-channel p of channel d: its rate times log2(e); 0 where there is no such state
+__device__ __forceinline__ float scan_rate(const ScanArgs& a, long d, int s, bool there) {
+    return there && s < a.S ? a.A[d * a.S + s] * kLog2e : 0.f;
+}
+
+template <bool BF16>
+__device__ __forceinline__ const typename RowElem<BF16>::type* scan_row(const void* base, long sn, long sd, long n, long d) {
+    return static_cast<const typename RowElem<BF16>::type*>(base) + n * sn + d * sd;
+}
+
+// B or C of kTile steps from t0 on into LDS, [step][4 P]; 0 behind `end` and for states that are not there
+template <bool BF16, int P>
+__device__ __forceinline__ void scan_stage_states(const void* from, long base, long ss, int S, long t0, long end, float* to) {
+    constexpr int SP = kK * P, T = scan_tile(P);
+    const typename RowElem<BF16>::type* row0 = static_cast<const typename RowElem<BF16>::type*>(from) + base;
+    for (int i = threadIdx.x; i < SP * (T / 8); i += blockDim.x) {
+        const int s = i & (SP - 1), c = i / SP;
+        float v[8];
+        if (s < S) {
+            row_load8<BF16>(row0 + s * ss, t0 + 8 * c, end, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[(8 * c + e) * SP + s] = v[e];
+    }
+}
+
+// host
+struct ScanPlan {
+    int P, waves, blocks_d, nseg, seg_len, chunks;
+};
+ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd);
+hipError_t scan_fwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, hipStream_t st);
+hipError_t scan_bwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, float* dA, float* dskip, float* dbias, hipStream_t st);
+
+// workgroups of a launch
+inline long scan_blocks(const ScanArgs& a) { return static_cast<long>(a.N) * a.G * a.nseg * a.blocks_d; }
+
+}  // namespace conv1d

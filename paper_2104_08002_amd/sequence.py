@@ -1,0 +1,290 @@
+"""Sequence operators beside the layer: a short causal convolution of every channel by itself, and a selective scan.
+
+Tensor-level marshalling of ``conv1d_causal_*`` and ``conv1d_scan_*`` (declared in ``include/conv1d.h``, which states the
+formulas): every arithmetic step runs in the library's kernels.  Layout as for the layer: [N, channels, positions],
+contiguous along the positions; samples and channels may be strided, so the halves of a projection need no copy.
+
+All of them run on the device of their tensors, on its current stream or on `stream`; outputs and workspaces are then
+allocated for that stream, and the caller sees to the order between it and the streams that the inputs come from.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding
+
+CAUSAL_SILU = 1
+SCAN_SOFTPLUS = 1
+MOST_TAPS, MOST_STATES = 8, 64
+
+
+class _Causal(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("x", "w", "bias", "init", "lengths")] + [(k, ctypes.c_long) for k in ("x_sn", "x_sc")] +
+                [(k, ctypes.c_int) for k in ("N", "C", "L", "S", "dtype", "flags")])
+
+
+class _Scan(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("x", "dt", "B", "C", "z", "A", "skip", "dt_bias", "init", "lengths")] +
+                [(k, ctypes.c_long) for k in ("x_sn", "x_sd", "dt_sn", "dt_sd", "z_sn", "z_sd", "b_sn", "b_sg", "b_ss", "c_sn", "c_sg", "c_ss")] +
+                [(k, ctypes.c_int) for k in ("N", "D", "L", "S", "G", "dtype", "flags")])
+
+
+class ScanGrads(NamedTuple):
+    """Gradients of conv1d_scan_fwd; None for an input that was not there (dinit: that was not asked for)."""
+
+    dx: torch.Tensor
+    ddt: torch.Tensor
+    dA: torch.Tensor
+    dB: torch.Tensor
+    dC: torch.Tensor
+    dskip: Optional[torch.Tensor]
+    dz: Optional[torch.Tensor]
+    ddt_bias: Optional[torch.Tensor]
+    dinit: Optional[torch.Tensor]
+
+
+def _on_device(fn):
+    """Runs fn with the device of its first argument current and, if asked for, on `stream`."""
+    name = fn.__code__.co_varnames[0]
+
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        t = args[0] if args else kw[name]
+        if not t.is_cuda:
+            raise ValueError("the tensors must be on the device")
+        if stream is not None:
+            if stream.device != t.device:
+                raise ValueError("the stream belongs to another device than the tensors")
+            with torch.cuda.stream(stream):
+                return fn(*args, **kw)
+        if t.device.index != torch._C._cuda_getDevice():
+            with torch.cuda.device(t.device):
+                return fn(*args, **kw)
+        return fn(*args, **kw)
+
+    return call
+
+
+def _rows(t, name, shape, dtype, device):
+    """A tensor of that shape whose last axis is contiguous."""
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device}: got {t.dtype} {list(t.shape)} on {t.device}")
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+    return t
+
+
+def _whole(t, name, shape, dtype, device):
+    _rows(t, name, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _spread(t, name):
+    """An output: no two of its elements in one place."""
+    last, strides = 1, sorted((t.stride(i), t.shape[i]) for i in range(t.dim()) if t.shape[i] > 1)
+    for stride, size in strides:
+        if stride < last:
+            raise ValueError(f"elements of {name} share memory")
+        last = stride * size
+    return t
+
+
+def _span(t):
+    return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _apart(out, ins):
+    """An output given by the caller: no memory between its first and last element may be an input's."""
+    first, last = _span(out)
+    for t in ins:
+        if t is not None and t.numel():
+            t0, t1 = _span(t)
+            if t0 < last and first < t1:
+                raise ValueError("out shares memory with an input")
+    return out
+
+
+# ---- depthwise causal convolution --------------------------------------------------------------------------------------
+def _causal(x, w, bias, silu, init, lengths, step=False):
+    if x.dim() != (2 if step else 3) or 0 in x.shape:
+        raise ValueError(f"x must have the shape {'[N, C]' if step else '[N, C, L]'}, none of it 0")
+    N, C = x.shape[:2]
+    L = 1 if step else x.shape[2]
+    if w.dim() != 2 or w.shape[0] != C or w.shape[1] < 1:
+        raise ValueError("w must have the shape [C, S]")
+    S, dev, code = w.shape[1], x.device, binding._dtype_code(x)
+    _rows(x, "x", x.shape, x.dtype, dev)
+    _whole(w, "w", (C, S), x.dtype, dev)
+    if bias is not None:
+        _whole(bias, "bias", (C,), torch.float32, dev)
+    if init is not None:
+        _whole(init, "init", (N, C, S - 1), x.dtype, dev)
+    if lengths is not None:
+        _whole(lengths, "lengths", (N,), torch.int32, dev)
+    return _Causal(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(init), _ptr(lengths), x.stride(0), 0 if step else x.stride(1), N, C, L, S, code,
+                   CAUSAL_SILU if silu else 0)
+
+
+@_on_device
+def conv1d_causal_fwd(x, w, bias=None, silu: bool = False, init=None, lengths=None, want_final: bool = False, out=None):
+    """y[N, C, L] of x[N, C, L] and w[C, S], in x's type; (y, final) with want_final.
+
+    init, final [N, C, S - 1]: the inputs before the sequence, and those that the position behind it needs.
+    lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there.
+    """
+    p = _causal(x, w, bias, silu, init, lengths)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
+    if out is not None:
+        _apart(out, (x, w, bias, init, lengths))
+    final = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=x.device) if want_final else None
+    binding._check(binding.load().conv1d_causal_fwd(ctypes.byref(p), y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), binding._current_stream()))
+    return (y, final) if want_final else y
+
+
+@_on_device
+def conv1d_causal_bwd(dy, x, w, bias=None, silu: bool = False, init=None, lengths=None, dfinal=None, want_init: bool = False, workspace=None):
+    """(dx, dw, dbias, dinit) of conv1d_causal_fwd(x, w, bias, silu, init, lengths): dx and dinit in x's type, dw [C, S] and dbias [C]
+    in float32.  dbias is None without a bias, dinit unless wanted."""
+    p, dev = _causal(x, w, bias, silu, init, lengths), x.device
+    _rows(dy, "dy", x.shape, x.dtype, dev)
+    if dfinal is not None:
+        _whole(dfinal, "dfinal", (p.N, p.C, p.S - 1), x.dtype, dev)
+    lib = binding.load()
+    if workspace is None:
+        workspace = torch.empty(max(lib.conv1d_causal_bwd_workspace_bytes(p.N, p.C, p.L, p.S), 4), dtype=torch.uint8, device=dev)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    dw = torch.empty((p.C, p.S), dtype=torch.float32, device=dev)
+    db = None if bias is None else torch.empty(p.C, dtype=torch.float32, device=dev)
+    di = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=dev) if want_init else None
+    binding._check(lib.conv1d_causal_bwd(ctypes.byref(p), dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), dx.data_ptr(), dw.data_ptr(),
+                                         _ptr(db), _ptr(di), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                         binding._current_stream()))
+    return dx, dw, db, di
+
+
+@_on_device
+def conv1d_causal_step(x, w, state, bias=None, silu: bool = False, out=None):
+    """y[N, C] for one position x[N, C] of every sequence; state [N, C, S - 1], as conv1d_causal_fwd leaves it in `final`, is
+    moved on by that position."""
+    p = _causal(x, w, bias, silu, None, None, step=True)
+    _whole(state, "state", (p.N, p.C, p.S - 1), x.dtype, x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
+    if out is not None:
+        _apart(out, (x, w, bias, state))
+    binding._check(binding.load().conv1d_causal_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    return y
+
+
+# ---- selective scan ----------------------------------------------------------------------------------------------------
+def _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths, step=False):
+    if x.dim() != (2 if step else 3) or 0 in x.shape:
+        raise ValueError(f"x must have the shape {'[N, D]' if step else '[N, D, L]'}, none of it 0")
+    N, D = x.shape[:2]
+    L = 1 if step else x.shape[2]
+    if A.dim() != 2 or A.shape[0] != D or A.shape[1] < 1:
+        raise ValueError("A must have the shape [D, S]")
+    S, dev, t, code = A.shape[1], x.device, x.dtype, binding._dtype_code(x)
+    if B.dim() != (3 if step else 4) or B.shape[1] < 1 or D % B.shape[1]:
+        raise ValueError(f"B must have the shape {'[N, G, S]' if step else '[N, G, S, L]'}, G a divisor of D")
+    G = B.shape[1]
+    states = (N, G, S) if step else (N, G, S, L)
+    _rows(x, "x", x.shape, t, dev)
+    _rows(dt, "dt", x.shape, t, dev)
+    _whole(A, "A", (D, S), torch.float32, dev)
+    _rows(B, "B", states, t, dev)
+    _rows(C, "C", states, t, dev)
+    if skip is not None:
+        _whole(skip, "skip", (D,), torch.float32, dev)
+    if z is not None:
+        _rows(z, "z", x.shape, t, dev)
+    if dt_bias is not None:
+        _whole(dt_bias, "dt_bias", (D,), torch.float32, dev)
+    if init is not None:
+        _whole(init, "init", (N, D, S), torch.float32, dev)
+    if lengths is not None:
+        _whole(lengths, "lengths", (N,), torch.int32, dev)
+    xs, ds, bs, cs = x.stride(), dt.stride(), B.stride(), C.stride()
+    zs = (0, 0) if z is None else z.stride()
+    return _Scan(x.data_ptr(), dt.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(z), A.data_ptr(), _ptr(skip), _ptr(dt_bias), _ptr(init), _ptr(lengths),
+                 xs[0], xs[1], ds[0], ds[1], zs[0], zs[1], bs[0], bs[1], bs[2], cs[0], cs[1], cs[2], N, D, L, S, G, code,
+                 SCAN_SOFTPLUS if softplus else 0)
+
+
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+@_on_device
+def conv1d_scan_fwd(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool = False, init=None, lengths=None, want_final: bool = False,
+                    save: bool = False, out=None, workspace=None):
+    """(y, final, saved): the selective scan of x[N, D, L] with steps dt[N, D, L], rates A[D, S] (float32), B and C [N, G, S, L],
+    gated by z[N, D, L]; y in x's type.
+
+    init, final [N, D, S] float32: the state before and behind the sequence (final is None unless wanted).
+    saved: what conv1d_scan_bwd needs of this call, with `save`; None without.
+    lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there and the state stays.
+    """
+    p, dev = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device
+    lib = binding.load()
+    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, dev), "out")
+    if out is not None:
+        _apart(out, (x, dt, A, B, C, skip, z, dt_bias, init, lengths))
+    final = torch.empty((p.N, p.D, p.S), dtype=torch.float32, device=dev) if want_final else None
+    saved = _scratch(lib.conv1d_scan_saved_bytes(p.N, p.D, p.L, p.S), dev) if save else None
+    if workspace is None:
+        workspace = _scratch(lib.conv1d_scan_fwd_workspace_bytes(p.N, p.D, p.L, p.S, p.G), dev)
+    binding._check(lib.conv1d_scan_fwd(ctypes.byref(p), y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), _ptr(saved), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel() * workspace.element_size(), binding._current_stream()))
+    return y, final, saved
+
+
+@_on_device
+def conv1d_scan_bwd(dy, saved, x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool = False, init=None, lengths=None, dfinal=None,
+                    want_init: bool = False, workspace=None) -> ScanGrads:
+    """Gradients of the call of conv1d_scan_fwd that had the same arguments and left `saved`: those of x, dt, B, C and z in their
+    type, of A, skip, dt_bias and init in float32."""
+    p, dev, t = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device, x.dtype
+    lib = binding.load()
+    _rows(dy, "dy", x.shape, t, dev)
+    if dfinal is not None:
+        _whole(dfinal, "dfinal", (p.N, p.D, p.S), torch.float32, dev)
+    _whole(saved, "saved", (lib.conv1d_scan_saved_bytes(p.N, p.D, p.L, p.S),), torch.uint8, dev)
+    if workspace is None:
+        workspace = _scratch(lib.conv1d_scan_bwd_workspace_bytes(p.N, p.D, p.L, p.S, p.G), dev)
+
+    def rows():
+        return torch.empty(x.shape, dtype=t, device=dev)
+
+    def floats(*shape):
+        return torch.empty(shape, dtype=torch.float32, device=dev)
+
+    g = ScanGrads(rows(), rows(), floats(p.D, p.S), torch.empty(B.shape, dtype=t, device=dev), torch.empty(C.shape, dtype=t, device=dev),
+                  None if skip is None else floats(p.D), None if z is None else rows(), None if dt_bias is None else floats(p.D),
+                  floats(p.N, p.D, p.S) if want_init else None)
+    binding._check(lib.conv1d_scan_bwd(ctypes.byref(p), dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), saved.data_ptr(), *map(_ptr, g),
+                                       _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                       binding._current_stream()))
+    return g
+
+
+@_on_device
+def conv1d_scan_step(x, dt, A, B, C, state, skip=None, z=None, dt_bias=None, softplus: bool = False, out=None):
+    """y[N, D] for one position of every sequence: x, dt, z [N, D], B and C [N, G, S]; state [N, D, S] float32, as conv1d_scan_fwd
+    leaves it in `final`, is moved on by that position."""
+    p = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, None, None, step=True)
+    _whole(state, "state", (p.N, p.D, p.S), torch.float32, x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
+    if out is not None:
+        _apart(out, (x, dt, A, B, C, skip, z, dt_bias, state))
+    binding._check(binding.load().conv1d_scan_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    return y
