@@ -303,7 +303,7 @@ int conv1d_causal_bwd(const conv1d_causal_t* p, const void* dy, long dy_sn, long
  * state [N][C][S - 1] dtype, read and replaced by the inputs that the next position needs (NULL for S = 1). */
 int conv1d_causal_step(const conv1d_causal_t* p, void* state, void* y, long y_sn, void* stream);
 
-/* Selective state space scan, S <= 64 states (more: CONV1D_EUNSUPPORTED), N * D < 2^25.  For sample n, channel d of group g:
+/* Selective state space scan, S <= 64 states, N * D < 2^25, L <= 2^30 (more: CONV1D_EUNSUPPORTED).  For sample n, channel d of group g:
  *   e[t] = dt[n][d][t] + dt_bias[d], through log(1 + exp(.)) with CONV1D_SCAN_SOFTPLUS
  *   h[s] = exp(e[t] A[d][s]) h[s] + e[t] x[n][d][t] B[n][g][s][t],   h = init before the first position
  *   y[t] = (sum_s C[n][g][s][t] h[s] + skip[d] x[n][d][t]) * (z ? z[n][d][t] sigmoid(z[n][d][t]) : 1)

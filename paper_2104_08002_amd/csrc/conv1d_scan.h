@@ -6,8 +6,8 @@
 //
 // Lanes.  P = 1, 2, 4, 8 or 16 neighbouring lanes have one channel, kK = 4 states each, in registers (S is padded to 4 P with
 // zeros); a wave has 64 / P channels.  One step costs a lane 4 exponentials (a quarter of the rate of a product) and 16
-// products: 8 issue slots per state, which is what bounds the scan.  Rows lie along the sequence, states across lanes: a tile
-// of kTile steps goes through LDS, loaded and stored along rows (8 elements a lane), read step by step.
+// products, which is what bounds the scan.  Rows lie along the sequence, states across lanes: a tile of steps goes through
+// LDS, loaded and stored along rows (8 elements a lane), read 4 steps at a time.
 // Positions behind a sequence's length have e = 0 and e x = 0, which leaves the state as it is.
 #pragma once
 
@@ -48,8 +48,13 @@ struct ScanArgs {
     float* dinit;      // [N][D][S] or nullptr
 };
 
-// steps of a tile: a wave has 64 / P rows of it, 1024 elements where the tile of B and C leaves room
-constexpr int scan_tile(int P) { return P >= 4 ? 64 : 16 * P; }
+typedef __attribute__((ext_vector_type(4))) float scan_f32x4;  // (16-byte aligned: LDS, and what the kernels keep)
+
+// steps of a tile: 64 lanes stage 8 elements each of a wave's 64 / P rows, once or twice
+constexpr int scan_tile(int P) { return P == 16 || P == 8 ? 64 : P == 4 ? 32 : 16; }
+constexpr int scan_tile_back(int P) { return P >= 4 ? 32 : 16; }
+// floats of a row in LDS: 16 rows of 4 steps lie in distinct banks
+constexpr int scan_stride(int T) { return T + 4; }
 
 // sum over the P lanes of a channel, in all of them
 #ifdef HOSTMODEL
@@ -97,10 +102,10 @@ __device__ __forceinline__ const typename RowElem<BF16>::type* scan_row(const vo
     return static_cast<const typename RowElem<BF16>::type*>(base) + n * sn + d * sd;
 }
 
-// B or C of kTile steps from t0 on into LDS, [step][4 P]; 0 behind `end` and for states that are not there
-template <bool BF16, int P>
-__device__ __forceinline__ void scan_stage_states(const void* from, long base, long ss, int S, long t0, long end, float* to) {
-    constexpr int SP = kK * P, T = scan_tile(P);
+// B or C of T steps from t0 on into LDS, [step][4 P]; 0 behind `end` and for states that are not there
+template <bool BF16, int P, int T>
+__device__ __forceinline__ void scan_stage_states(const void* from, long base, long ss, int S, int t0, int end, float* to) {
+    constexpr int SP = kK * P;
     const typename RowElem<BF16>::type* row0 = static_cast<const typename RowElem<BF16>::type*>(from) + base;
     for (int i = threadIdx.x; i < SP * (T / 8); i += blockDim.x) {
         const int s = i & (SP - 1), c = i / SP;
@@ -114,6 +119,74 @@ __device__ __forceinline__ void scan_stage_states(const void* from, long base, l
 #pragma unroll
         for (int e = 0; e < 8; ++e) to[(8 * c + e) * SP + s] = v[e];
     }
+}
+
+// the lane's part in loading and storing rows: row (q * RPP + lane / LPR) of the wave, 8 elements from 8 (lane % LPR) on
+template <int P, int T>
+struct ScanRows {
+    static constexpr int CW = kSeqWave / P, LPR = T / 8, RPP = kSeqWave / LPR, PASSES = CW > RPP ? CW / RPP : 1;
+    static constexpr int RS = scan_stride(T);
+};
+
+__device__ __forceinline__ void lds_put8(float* to, const float (&v)[8]) {
+    *reinterpret_cast<scan_f32x4*>(to) = scan_f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<scan_f32x4*>(to + 4) = scan_f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void lds_get8(const float* from, float (&v)[8]) {
+    const scan_f32x4 a = *reinterpret_cast<const scan_f32x4*>(from), b = *reinterpret_cast<const scan_f32x4*>(from + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = a[e];
+        v[4 + e] = b[e];
+    }
+}
+
+// One (sample, channel) row of segment values joined along the sequence: value[seg] holds what a segment adds, and becomes
+// what comes into it from the segments before (BACK: behind) it, `first` into the first; sums[seg]: exp(A sum) is a segment's
+// decay.  SP states times `chunks` runs of `len` segments a row; a run is joined in itself, the runs before it through LDS.
+template <bool BACK>
+__global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const float* sums, const float* first, const float* A, int N, int D,
+                                                         int S, int SP, int nseg, int chunks, int len) {
+    __shared__ float run_decay[1024], run_add[1024];
+    const int per_row = SP * chunks;
+    const long row = static_cast<long>(blockIdx.x) * (blockDim.x / per_row) + threadIdx.x / per_row;
+    const bool there = row < static_cast<long>(N) * D;
+    const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP;
+    const long n = there ? row / D : 0, d = there ? row - n * D : 0;
+    const float rate = there && s < S ? A[d * S + s] * kLog2e : 0.f;
+    const int from = min(nseg, chunk * len), to = there ? min(nseg, from + len) : from;
+    float decay = 1.f, add = 0.f;
+#pragma unroll 8
+    for (int i = from; i < to; ++i) {
+        const long at = (n * nseg + (BACK ? nseg - 1 - i : i)) * D + d;
+        const float f = exp2_hw(rate * sums[at]);
+        add = fmaf(f, add, value[at * SP + s]);
+        decay *= f;
+    }
+    run_decay[threadIdx.x] = decay;
+    run_add[threadIdx.x] = add;
+    __syncthreads();
+    float h = there && first && s < S ? first[(n * D + d) * S + s] : 0.f;
+    const int base = threadIdx.x - in_row + s;
+    for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
+#pragma unroll 8
+    for (int i = from; i < to; ++i) {
+        const long at = (n * nseg + (BACK ? nseg - 1 - i : i)) * D + d;
+        const float f = exp2_hw(rate * sums[at]), v = value[at * SP + s];
+        value[at * SP + s] = h;
+        h = fmaf(f, h, v);
+    }
+}
+
+// runs of about 8 segments, 1024 lanes of a workgroup at most
+template <bool BACK>
+inline hipError_t scan_join_launch(float* value, const float* sums, const float* first, const float* A, int N, int D, int S, int SP, int nseg,
+                                   hipStream_t st) {
+    int chunks = 1;
+    while (chunks * 8 < nseg && chunks * 2 * SP <= 1024) chunks *= 2;
+    const int per_row = SP * chunks, threads = per_row > 256 ? per_row : 256;
+    return launch_kernel(scan_join_kernel<BACK>, dim3(static_cast<unsigned>(cdiv(static_cast<long>(N) * D, threads / per_row))), dim3(threads), 0, st,
+                         value, sums, first, A, N, D, S, SP, nseg, chunks, cdiv(nseg, chunks));
 }
 
 // host

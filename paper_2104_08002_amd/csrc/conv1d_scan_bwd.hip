@@ -13,7 +13,10 @@ namespace conv1d {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int bwd_tile(int P) { return P >= 4 ? 32 : 16; }
+// What was read from LDS before is read again: kept, it would take the registers that a third and fourth wave need.
+__device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
+
+constexpr int kHalf = kSub / 2;  // steps whose states and decays are in registers at a time
 
 // One value per lane and state k, for dB and dC: the sums over the channels of the wave.  Afterwards the lanes whose place
 // within their row of 16 is p < P hold them: q[0] dB, q[1] dC of state 4 p + channel_state(row).
@@ -51,94 +54,113 @@ __device__ __forceinline__ int channel_state(int lane) {
     return (row >> 1) | ((row & 1) << 1);
 }
 
-// what a step needs; the walk back leaves its own sums in the place
-struct alignas(16) Slot {
-    float e, ex, dy, unused;
+// The lane's rows: where they begin and what they share.
+template <bool BF16, int P, int T>
+struct Rows {
+    using R = ScanRows<P, T>;
+    using E = typename RowElem<BF16>::type;
+    const E *x[R::PASSES], *dt[R::PASSES], *dout[R::PASSES], *z[R::PASSES];
+    float bias[R::PASSES];
+    bool real[R::PASSES];
+    long d[R::PASSES];
+    int c;
+
+    __device__ __forceinline__ Rows(const ScanArgs& a, const ScanPlace& at, int base, int lane) {
+        c = 8 * (lane % R::LPR);
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            real[q] = row < R::CW && base + row < a.Dg;
+            d[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
+            x[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, d[q]);
+            dt[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, d[q]);
+            dout[q] = scan_row<BF16>(a.dout, a.dout_sn, a.dout_sd, at.n, d[q]);
+            z[q] = a.z ? scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, d[q]) : nullptr;
+            bias[q] = a.dt_bias ? a.dt_bias[d[q]] : 0.f;
+        }
+    }
+    __device__ __forceinline__ static void load(const E* row, int t, bool inside, int end, float (&v)[8]) {
+        if (inside) row_load8_inside<BF16>(row, t, v);
+        else row_load8<BF16>(row, t, end, v);
+    }
+    // e, dy and (WITH_X) x of the tile at t0 into LDS
+    template <bool WITH_X>
+    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, bool inside, float* sE, float* sX, float* sY) const {
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            if (row >= R::CW) continue;
+            const int end = real[q] ? len : 0;
+            float v[8], g[8], u[8];
+            load(dt[q], t0 + c, inside, end, v);
+            load(dout[q], t0 + c, inside, end, g);
+            if (a.z) load(z[q], t0 + c, inside, end, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += bias[q];
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = softplus_of(v[i]);
+            }
+            if (!inside) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < end ? v[i] : 0.f;
+            }
+            if (a.z) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= u[i] * sigmoid_of(u[i]);
+            }
+            lds_put8(sE + row * R::RS + c, v);
+            lds_put8(sY + row * R::RS + c, g);
+            if (WITH_X) {
+                load(x[q], t0 + c, inside, end, u);
+                lds_put8(sX + row * R::RS + c, u);
+            }
+        }
+    }
 };
-
-// e, e x and dy of the wave's rows, tile at t0
-template <bool BF16, int P>
-__device__ __forceinline__ void stage_rows(const ScanArgs& a, const ScanPlace& at, int base, long t0, long len, Slot* mine) {
-    constexpr int T = bwd_tile(P), CW = kSeqWave / P, LPR = T / 8, RPP = kSeqWave / LPR, STRIDE = T + 1;
-    const int lane = threadIdx.x & (kSeqWave - 1);
-#pragma unroll
-    for (int r0 = 0; r0 < CW; r0 += RPP) {
-        const int row = r0 + lane / LPR, c = 8 * (lane % LPR);
-        if (row >= CW) continue;
-        const bool real = base + row < a.Dg;
-        const long d = static_cast<long>(at.g) * a.Dg + (real ? base + row : 0), end = real ? len : 0;
-        float x[8], e[8], dy[8], z[8];
-        row_load8<BF16>(scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, d), t0 + c, end, x);
-        row_load8<BF16>(scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, d), t0 + c, end, e);
-        row_load8<BF16>(scan_row<BF16>(a.dout, a.dout_sn, a.dout_sd, at.n, d), t0 + c, end, dy);
-        if (a.z) row_load8<BF16>(scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, d), t0 + c, end, z);
-        const float bias = a.dt_bias ? a.dt_bias[d] : 0.f;
-        Slot* to = mine + row * STRIDE + c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float v = e[i] + bias;
-            if (a.softplus) v = softplus_of(v);
-            v = t0 + c + i < end ? v : 0.f;
-            if (a.z) dy[i] *= z[i] * sigmoid_of(z[i]);
-            to[i] = Slot{v, v * x[i], dy[i], 0.f};
-        }
-    }
-}
-
-template <bool BF16, int P>
-__device__ __forceinline__ void stage_states(const void* from, long base, long ss, int S, long t0, long end, float* to) {
-    constexpr int SP = kK * P, T = bwd_tile(P);
-    const typename RowElem<BF16>::type* row0 = static_cast<const typename RowElem<BF16>::type*>(from) + base;
-    for (int i = threadIdx.x; i < SP * (T / 8); i += blockDim.x) {
-        const int s = i & (SP - 1), c = i / SP;
-        float v[8];
-        if (s < S) {
-            row_load8<BF16>(row0 + s * ss, t0 + 8 * c, end, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) to[(8 * c + e) * SP + s] = v[e];
-    }
-}
 
 // what a segment sends into the one before it, from nothing sent into itself, and the sum of its steps
 template <bool BF16, int P>
-__global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_adjoint_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = bwd_tile(P), CW = kSeqWave / P, STRIDE = T + 1;
-    __shared__ __align__(16) Slot steps[kScanWaves][CW * STRIDE];
+__global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(ScanArgs a) {
+    constexpr int SP = kK * P, T = scan_tile(P);
+    using R = ScanRows<P, T>;
+    __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sY[kScanWaves][R::CW * R::RS];  // e and dy
     __shared__ __align__(16) float sC[T * SP];
     const ScanPlace at = scan_place(a);
     if (at.seg == 0) return;
     const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
-    const long len = seq_length(a.lengths, at.n, a.L);
-    const int base = (at.cb * waves + wave) * CW;
-    const bool there = base + cl < a.Dg;
+    const int len = seq_length(a.lengths, at.n, a.L);
+    const int base = (at.cb * waves + wave) * R::CW;
+    const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
-    Slot* mine = steps[wave];
+    const Rows<BF16, P, T> rows(a, at, base, lane);
     float rate[kK], carry[kK], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < kK; ++k) {
         rate[k] = scan_rate(a, d, kK * p + k, there);
         carry[k] = 0.f;
     }
-    const long t_begin = static_cast<long>(at.seg) * a.seg_len, t_end = min(static_cast<long>(a.L), t_begin + a.seg_len);
-    for (long t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
-        stage_rows<BF16, P>(a, at, base, t0, len, mine);
-        stage_states<BF16, P>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+    const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
+        rows.template stage<false>(a, lane, t0, len, t0 + T <= len && full, sE[wave], nullptr, sY[wave]);
+        scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
-        const Slot* row = mine + cl * STRIDE;
+        const float *e_row = sE[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
+#pragma unroll 1
         for (int t = T - kSub; t >= 0; t -= kSub) {
             float part = 0.f;
 #pragma unroll
-            for (int i = kSub - 1; i >= 0; --i) {
-                const Slot s = row[t + i];
-                part += s.e;
+            for (int j = kSub - 4; j >= 0; j -= 4) {
+                __builtin_amdgcn_sched_barrier(0);
+                const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t + j);
 #pragma unroll
-                for (int k = 0; k < kK; ++k)
-                    carry[k] = exp2_hw(s.e * rate[k]) * fmaf(sC[(t + i) * SP + kK * p + k], s.dy, carry[k]);
+                for (int i = 3; i >= 0; --i) {
+                    const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    part += e[i];
+#pragma unroll
+                    for (int k = 0; k < kK; ++k) carry[k] = exp2_hw(e[i] * rate[k]) * fmaf(o[k], dy[i], carry[k]);
+                }
             }
             sum += part;
         }
@@ -146,46 +168,28 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_adjoint_kernel(Scan
     }
     if (!there) return;
     const long i = (at.n * a.nseg + at.seg) * a.D + d;
-    *reinterpret_cast<seq_f32x4*>(a.carries + i * SP + kK * p) = seq_f32x4{carry[0], carry[1], carry[2], carry[3]};
+    *reinterpret_cast<scan_f32x4*>(a.carries + i * SP + kK * p) = scan_f32x4{carry[0], carry[1], carry[2], carry[3]};
     if (p == 0) a.sums[i] = sum;
 }
 
-// carries[seg]: what segment seg sends on from nothing -> what is sent into it.  One lane per state.
-__global__ __launch_bounds__(kThreads) void scan_join_back_kernel(ScanArgs a, int SP) {
-    const long i = static_cast<long>(blockIdx.x) * kThreads + threadIdx.x;
-    const long nd = i / SP;
-    if (nd >= static_cast<long>(a.N) * a.D) return;
-    const int s = static_cast<int>(i - nd * SP);
-    const long n = nd / a.D, d = nd - n * a.D;
-    const float rate = scan_rate(a, d, s, true);
-    float c = a.dfinal && s < a.S ? a.dfinal[nd * a.S + s] : 0.f;
-#pragma unroll 8
-    for (int seg = a.nseg - 1; seg > 0; --seg) {
-        const long at = (n * a.nseg + seg) * a.D + d;
-        const float add = a.carries[at * SP + s], decay = exp2_hw(rate * a.sums[at]);
-        a.carries[at * SP + s] = c;
-        c = fmaf(decay, c, add);
-    }
-    a.carries[(n * a.nseg * a.D + d) * SP + s] = c;
-}
-
 template <bool BF16, int P>
-__global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_bwd_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = bwd_tile(P), CW = kSeqWave / P, STRIDE = T + 1;
-    constexpr int LPR = T / 8, RPP = kSeqWave / LPR, PASSES = CW > RPP ? CW / RPP : 1;
-    constexpr int RED = SP + 1;
-    __shared__ __align__(16) Slot steps[kScanWaves][CW * STRIDE];
+__global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanArgs a) {
+    constexpr int SP = kK * P, T = scan_tile_back(P), RED = SP + 1;
+    using R = ScanRows<P, T>;
+    using E = typename RowElem<BF16>::type;
+    // e, x and dy of a step; the walk back leaves sum_s e g B, de and sum_s C h in their places
+    __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS], sY[kScanWaves][R::CW * R::RS];
     __shared__ __align__(16) float sB[T * SP], sC[T * SP];
     __shared__ float red[kScanWaves][2][kSub * RED];
     const ScanPlace at = scan_place(a);
     const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
-    const long len = seq_length(a.lengths, at.n, a.L);
-    const int base = (at.cb * waves + wave) * CW;
-    const bool there = base + cl < a.Dg;
+    const int len = seq_length(a.lengths, at.n, a.L);
+    const int base = (at.cb * waves + wave) * R::CW;
+    const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
-    Slot* mine = steps[wave];
-    float rate[kK], carry[kK], dA[kK], dskip[PASSES], dbias[PASSES];
+    const Rows<BF16, P, T> rows(a, at, base, lane);
+    float rate[kK], carry[kK], dA[kK], dskip[R::PASSES], dbias[R::PASSES];
 #pragma unroll
     for (int k = 0; k < kK; ++k) {
         const int s = kK * p + k;
@@ -196,65 +200,105 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_bwd_kernel(ScanArgs
         else if (a.dfinal && there && s < a.S) carry[k] = a.dfinal[(at.n * a.D + d) * a.S + s];
     }
 #pragma unroll
-    for (int q = 0; q < PASSES; ++q) dskip[q] = dbias[q] = 0.f;
-    const long t_begin = static_cast<long>(at.seg) * a.seg_len, t_end = min(static_cast<long>(a.L), t_begin + a.seg_len);
-    for (long t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
-        stage_rows<BF16, P>(a, at, base, t0, len, mine);
-        stage_states<BF16, P>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        stage_states<BF16, P>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+    for (int q = 0; q < R::PASSES; ++q) dskip[q] = dbias[q] = 0.f;
+    const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
+        const bool inside = t0 + T <= len && full;
+        rows.template stage<true>(a, lane, t0, len, inside, sE[wave], sX[wave], sY[wave]);
+        scan_stage_states<BF16, P, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
+        scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
-        Slot* row = mine + cl * STRIDE;
+        float *e_row = sE[wave] + cl * R::RS, *x_row = sX[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
+#pragma unroll 1
         for (int t = T - kSub; t >= 0; t -= kSub) {
             if (t0 + t >= a.L) continue;
-            float h0[kK], h[kSub][kK], decay[kSub][kK];
+            float first[kK], mid[kK];  // the state before the first and the second half
+#pragma unroll
+            for (int k = 0; k < kK; ++k) first[k] = 0.f;
             if (there) {
-                const seq_f32x4 v = *reinterpret_cast<const seq_f32x4*>(a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + kK * p);
+                const scan_f32x4 v = *reinterpret_cast<const scan_f32x4*>(a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + kK * p);
 #pragma unroll
-                for (int k = 0; k < kK; ++k) h0[k] = v[k];
-            } else {
-#pragma unroll
-                for (int k = 0; k < kK; ++k) h0[k] = 0.f;
+                for (int k = 0; k < kK; ++k) first[k] = v[k];
             }
 #pragma unroll
-            for (int i = 0; i < kSub; ++i) {
-                const Slot s = row[t + i];
+            for (int k = 0; k < kK; ++k) mid[k] = first[k];
 #pragma unroll
-                for (int k = 0; k < kK; ++k) {
-                    decay[i][k] = exp2_hw(s.e * rate[k]);
-                    h[i][k] = fmaf(decay[i][k], i ? h[i - 1][k] : h0[k], s.ex * sB[(t + i) * SP + kK * p + k]);
+            for (int j = 0; j < kHalf; j += 4) {
+                __builtin_amdgcn_sched_barrier(0);
+                const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
+                    const float ex = e[i] * x[i];
+#pragma unroll
+                    for (int k = 0; k < kK; ++k) mid[k] = fmaf(exp2_hw(e[i] * rate[k]), mid[k], ex * b[k]);
                 }
             }
             float dA_sub[kK] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int half = kHalf; half >= 0; half -= kHalf) {
+                const int t1 = t + half;
+                float h[kHalf][kK], decay[kHalf][kK];
 #pragma unroll
-            for (int i = kSub - 1; i >= 0; --i) {
-                const Slot s = row[t + i];
-                float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK], q[2];
+                for (int j = 0; j < kHalf; j += 4) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t1 + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t1 + j);
 #pragma unroll
-                for (int k = 0; k < kK; ++k) {
-                    const float b = sB[(t + i) * SP + kK * p + k], c = sC[(t + i) * SP + kK * p + k];
-                    const float g = fmaf(c, s.dy, carry[k]);
-                    y = fmaf(c, h[i][k], y);
-                    vC[k] = s.dy * h[i][k];
-                    vB[k] = g * s.ex;
-                    gb = fmaf(g, b, gb);
-                    carry[k] = g * decay[i][k];
-                    const float kept = carry[k] * (i ? h[i - 1][k] : h0[k]);
-                    qa = fmaf(kept, rate[k], qa);
-                    dA_sub[k] = fmaf(kept, s.e, dA_sub[k]);
+                    for (int i = 0; i < 4; ++i) {
+                        const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t1 + j + i) * SP + kK * p);
+                        const float ex = e[i] * x[i];
+#pragma unroll
+                        for (int k = 0; k < kK; ++k) {
+                            decay[j + i][k] = exp2_hw(e[i] * rate[k]);
+                            h[j + i][k] = fmaf(decay[j + i][k], j + i ? h[j + i - (j + i ? 1 : 0)][k] : mid[k], ex * b[k]);
+                        }
+                    }
                 }
-                gb = channel_sum<P>(gb);
-                qa = channel_sum<P>(qa);
-                y = channel_sum<P>(y);
-                if (p == 0) {
-                    row[t + i].e = gb;
-                    row[t + i].ex = qa;
-                    row[t + i].dy = y;
+#pragma unroll
+                for (int j = kHalf - 4; j >= 0; j -= 4) {
+                    reload_lds();
+                    __builtin_amdgcn_sched_barrier(0);
+                    const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t1 + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t1 + j),
+                                     dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t1 + j);
+                    scan_f32x4 out_x, out_e, out_y;
+#pragma unroll
+                    for (int i = 3; i >= 0; --i) {
+                        const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t1 + j + i) * SP + kK * p);
+                        const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t1 + j + i) * SP + kK * p);
+                        const float ex = e[i] * x[i];
+                        float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK], q[2];
+#pragma unroll
+                        for (int k = 0; k < kK; ++k) {
+                            const float g = fmaf(o[k], dy[i], carry[k]);
+                            y = fmaf(o[k], h[j + i][k], y);
+                            vC[k] = dy[i] * h[j + i][k];
+                            vB[k] = g * ex;
+                            gb = fmaf(g, b[k], gb);
+                            carry[k] = g * decay[j + i][k];
+                            const float kept = carry[k] * (j + i ? h[j + i - (j + i ? 1 : 0)][k] : mid[k]);
+                            qa = fmaf(kept, rate[k], qa);
+                            dA_sub[k] = fmaf(kept, e[i], dA_sub[k]);
+                        }
+                        gb = channel_sum<P>(gb);
+                        qa = channel_sum<P>(qa);
+                        out_y[i] = channel_sum<P>(y);
+                        out_x[i] = gb * e[i];
+                        out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
+                        wave_sums<P>(vB, vC, q);
+                        if ((lane & 15) < P) {
+                            const int to = (half + j + i) * RED + kK * p + channel_state(lane);
+                            red[wave][0][to] = q[0];
+                            red[wave][1][to] = q[1];
+                        }
+                    }
+                    if (p == 0) {
+                        *reinterpret_cast<scan_f32x4*>(e_row + t1 + j) = out_x;
+                        *reinterpret_cast<scan_f32x4*>(x_row + t1 + j) = out_e;
+                        *reinterpret_cast<scan_f32x4*>(dy_row + t1 + j) = out_y;
+                    }
                 }
-                wave_sums<P>(vB, vC, q);
-                if ((lane & 15) < P) {
-                    red[wave][0][i * RED + kK * p + channel_state(lane)] = q[0];
-                    red[wave][1][i * RED + kK * p + channel_state(lane)] = q[1];
-                }
+#pragma unroll
+                for (int k = 0; k < kK; ++k) mid[k] = first[k];
             }
 #pragma unroll
             for (int k = 0; k < kK; ++k) dA[k] += dA_sub[k];
@@ -262,7 +306,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_bwd_kernel(ScanArgs
             // over the waves of the workgroup, lanes along the sequence
             for (int i = threadIdx.x; i < 2 * kSub * SP; i += blockDim.x) {
                 const int step = i & (kSub - 1), s = (i / kSub) & (SP - 1), which = i / (kSub * SP);
-                const long tt = t0 + t + step;
+                const int tt = t0 + t + step;
                 if (s >= a.S || tt >= a.L) continue;
                 float v = 0.f;
                 for (int w = 0; w < waves; ++w) v += red[w][which][step * RED + s];
@@ -274,58 +318,62 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_bwd_kernel(ScanArgs
         }
         // rows again: the gradients of x, dt and z
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) {
-            const int r = q * RPP + lane / LPR, c = 8 * (lane % LPR);
-            if (r >= CW || base + r >= a.Dg || t0 + c >= a.L) continue;
-            const long dr = static_cast<long>(at.g) * a.Dg + base + r, o = (at.n * a.D + dr) * a.L;
-            float x[8], v[8], dout[8], z[8], dx[8], ddt[8], dz[8];
-            row_load8<BF16>(scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, dr), t0 + c, len, x);
-            row_load8<BF16>(scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, dr), t0 + c, len, v);
-            row_load8<BF16>(scan_row<BF16>(a.dout, a.dout_sn, a.dout_sd, at.n, dr), t0 + c, len, dout);
-            if (a.z) row_load8<BF16>(scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, dr), t0 + c, len, z);
-            const float bias = a.dt_bias ? a.dt_bias[dr] : 0.f, skip = a.skip ? a.skip[dr] : 0.f;
-            const Slot* from = mine + r * STRIDE + c;
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int r = q * R::RPP + lane / R::LPR, c = rows.c;
+            if (!rows.real[q] || t0 + c >= a.L) continue;
+            const long o = (at.n * a.D + rows.d[q]) * a.L;
+            const float skip = a.skip ? a.skip[rows.d[q]] : 0.f;
+            float x[8], v[8], dout[8], dx[8], ddt[8];
+            rows.load(rows.x[q], t0 + c, inside, len, x);
+            rows.load(rows.dout[q], t0 + c, inside, len, dout);
+            if (a.z) {
+                float z[8], y[8];
+                rows.load(rows.z[q], t0 + c, inside, len, z);
+                lds_get8(sY[wave] + r * R::RS + c, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float sig = sigmoid_of(z[i]);
+                    y[i] = dout[i] * fmaf(skip, x[i], y[i]) * (sig * fmaf(z[i], 1.f - sig, 1.f));
+                    dout[i] *= z[i] * sig;
+                    if (!inside) y[i] = t0 + c + i < len ? y[i] : 0.f;
+                }
+                row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, a.L, y);
+            }
+            lds_get8(sE[wave] + r * R::RS + c, dx);
+            lds_get8(sX[wave] + r * R::RS + c, ddt);
+            if (a.softplus) {
+                rows.load(rows.dt[q], t0 + c, inside, len, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ddt[i] *= sigmoid_of(v[i] + rows.bias[q]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = t0 + c + i < len;
-                const float gb = from[i].e, qa = from[i].ex;
-                float dy = dout[i];
-                if (a.z) {
-                    const float sig = sigmoid_of(z[i]);
-                    dy *= z[i] * sig;
-                    dz[i] = in ? dout[i] * fmaf(skip, x[i], from[i].dy) * (sig * fmaf(z[i], 1.f - sig, 1.f)) : 0.f;
+                dx[i] = fmaf(skip, dout[i], dx[i]);
+                if (!inside) {
+                    dx[i] = t0 + c + i < len ? dx[i] : 0.f;
+                    ddt[i] = t0 + c + i < len ? ddt[i] : 0.f;
                 }
-                const float raw = v[i] + bias;
-                const float e = a.softplus ? softplus_of(raw) : raw;
-                float de = fmaf(gb, x[i], qa * (1.f / kLog2e));
-                if (a.softplus) de *= sigmoid_of(raw);
-                dx[i] = in ? fmaf(gb, e, skip * dy) : 0.f;
-                ddt[i] = in ? de : 0.f;
-                dskip[q] = in ? fmaf(dy, x[i], dskip[q]) : dskip[q];
+                dskip[q] = fmaf(dout[i], x[i], dskip[q]);
                 dbias[q] += ddt[i];
             }
-            using E = typename RowElem<BF16>::type;
             row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, a.L, dx);
             row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, a.L, ddt);
-            if (a.z) row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, a.L, dz);
         }
     }
-    const long part = at.n * a.nseg + at.seg, rows = static_cast<long>(a.N) * a.nseg;
+    const long part = at.n * a.nseg + at.seg, segs = static_cast<long>(a.N) * a.nseg;
 #pragma unroll
-    for (int q = 0; q < PASSES; ++q) {
+    for (int q = 0; q < R::PASSES; ++q) {
 #pragma unroll
-        for (int m = 1; m < LPR; m <<= 1) {
+        for (int m = 1; m < R::LPR; m <<= 1) {
             dskip[q] += lane_xor(dskip[q], m);
             dbias[q] += lane_xor(dbias[q], m);
         }
-        const int r = q * RPP + lane / LPR;
-        if (lane % LPR || r >= CW || base + r >= a.Dg) continue;
-        const long dr = static_cast<long>(at.g) * a.Dg + base + r;
-        a.part_d[part * a.D + dr] = dskip[q];
-        a.part_d[(rows + part) * a.D + dr] = dbias[q];
+        if (lane % R::LPR || !rows.real[q]) continue;
+        a.part_d[part * a.D + rows.d[q]] = dskip[q];
+        a.part_d[(segs + part) * a.D + rows.d[q]] = dbias[q];
     }
     if (!there) return;
-    *reinterpret_cast<seq_f32x4*>(a.part_a + (part * a.D + d) * SP + kK * p) = seq_f32x4{dA[0], dA[1], dA[2], dA[3]};
+    *reinterpret_cast<scan_f32x4*>(a.part_a + (part * a.D + d) * SP + kK * p) = scan_f32x4{dA[0], dA[1], dA[2], dA[3]};
     if (a.dinit && at.seg == 0) {
 #pragma unroll
         for (int k = 0; k < kK; ++k)
@@ -380,9 +428,7 @@ hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
     const long most = kSeqMostThreads / block.x, blocks = scan_blocks(a);
     for (int stage = p.nseg > 1 ? 0 : 2; stage < 3; ++stage) {
         if (stage == 1) {
-            const long threads = static_cast<long>(a.N) * a.D * kK * P;
-            a.first = 0;
-            const hipError_t e = launch_kernel(scan_join_back_kernel, dim3(static_cast<unsigned>(cdiv(threads, kThreads))), dim3(kThreads), 0, st, a, kK * P);
+            const hipError_t e = scan_join_launch<true>(a.carries, a.sums, a.dfinal, a.A, a.N, a.D, a.S, kK * P, a.nseg, st);
             if (e != hipSuccess) return e;
             continue;
         }

@@ -11,22 +11,20 @@ constexpr int kThreads = 256;
 
 // ENDS: no output but the state each segment adds and the sum of its steps.
 template <bool BF16, int P, bool ENDS>
-__global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_fwd_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = scan_tile(P), CW = kSeqWave / P;
-    constexpr int LPR = T / 8, RPP = kSeqWave / LPR;      // lanes of a row, rows of a pass
-    constexpr int PASSES = CW * LPR / kSeqWave > 0 ? CW * LPR / kSeqWave : 1;
-    constexpr int STRIDE = T + 2;                         // of a row, in pairs: 16 rows lie in distinct banks
-    struct alignas(8) Pair { float e, ex; };
-    __shared__ __align__(16) Pair steps[kScanWaves][CW * STRIDE];
+__global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanArgs a) {
+    constexpr int SP = kK * P, T = scan_tile(P);
+    using R = ScanRows<P, T>;
+    using E = typename RowElem<BF16>::type;
+    __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS];  // e (then y) and e x
     __shared__ __align__(16) float sB[T * SP], sC[ENDS ? 4 : T * SP];
     const ScanPlace at = scan_place(a);
+    if (ENDS && at.seg == a.nseg - 1) return;             // nothing comes behind the last segment
     const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
-    const long len = seq_length(a.lengths, at.n, a.L);
-    const int base = (at.cb * waves + wave) * CW;         // first channel of the wave, within its group
-    const bool there = base + cl < a.Dg;
+    const int len = seq_length(a.lengths, at.n, a.L);
+    const int base = (at.cb * waves + wave) * R::CW;      // first channel of the wave, within its group
+    const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
-    Pair* mine = steps[wave];
 
     float rate[kK], h[kK];
 #pragma unroll
@@ -38,105 +36,121 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave) void scan_fwd_kernel(ScanArgs
         if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
         else if (a.init && there && s < a.S) h[k] = a.init[(at.n * a.D + d) * a.S + s];
     }
-    const long t_begin = static_cast<long>(at.seg) * a.seg_len, t_end = min(static_cast<long>(a.L), t_begin + a.seg_len);
+    const int c = 8 * (lane % R::LPR);
+    const E *x_row[R::PASSES], *dt_row[R::PASSES];
+    float bias[R::PASSES], skip[R::PASSES];
+    bool real[R::PASSES];
+    long dr[R::PASSES];
+#pragma unroll
+    for (int q = 0; q < R::PASSES; ++q) {
+        const int row = q * R::RPP + lane / R::LPR;
+        real[q] = row < R::CW && base + row < a.Dg;
+        dr[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
+        x_row[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, dr[q]);
+        dt_row[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, dr[q]);
+        bias[q] = a.dt_bias ? a.dt_bias[dr[q]] : 0.f;
+        skip[q] = a.skip ? a.skip[dr[q]] : 0.f;
+    }
+    const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     float sum = 0.f;
-    for (long t0 = t_begin; t0 < t_end; t0 += T) {
-        // rows of the wave's own channels: e and e x
+    for (int t0 = t_begin; t0 < t_end; t0 += T) {
+        const bool inside = t0 + T <= len && full;        // of the whole wave: no masks
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) {
-            const int row = q * RPP + lane / LPR, c = 8 * (lane % LPR);
-            if (row >= CW) continue;
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            if (row >= R::CW) continue;
             float x[8], e[8];
-            const bool real = base + row < a.Dg;
-            const long dr = static_cast<long>(at.g) * a.Dg + (real ? base + row : 0);
-            const long end = real ? len : 0;
-            row_load8<BF16>(scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, dr), t0 + c, end, x);
-            row_load8<BF16>(scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, dr), t0 + c, end, e);
-            const float bias = a.dt_bias ? a.dt_bias[dr] : 0.f;
-            Pair* to = mine + row * STRIDE + c;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v = e[i] + bias;
-                if (a.softplus) v = softplus_of(v);
-                v = t0 + c + i < end ? v : 0.f;
-                to[i] = Pair{v, v * x[i]};
+            if (inside) {
+                row_load8_inside<BF16>(x_row[q], t0 + c, x);
+                row_load8_inside<BF16>(dt_row[q], t0 + c, e);
+            } else {
+                row_load8<BF16>(x_row[q], t0 + c, real[q] ? len : 0, x);
+                row_load8<BF16>(dt_row[q], t0 + c, real[q] ? len : 0, e);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] += bias[q];
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
+            }
+            if (!inside) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = real[q] && t0 + c + i < len ? e[i] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= e[i];
+            lds_put8(sE[wave] + row * R::RS + c, e);
+            lds_put8(sX[wave] + row * R::RS + c, x);
         }
-        scan_stage_states<BF16, P>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        if (!ENDS) scan_stage_states<BF16, P>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        scan_stage_states<BF16, P, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
+        if (!ENDS) scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
-        Pair* row = mine + cl * STRIDE;
+        float* e_row = sE[wave] + cl * R::RS;
+        const float* ex_row = sX[wave] + cl * R::RS;
+#pragma unroll 1
         for (int t = 0; t < T; t += kSub) {
             if (!ENDS && a.saved && there && t0 + t < a.L) {
                 float* to = a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + kK * p;
-                *reinterpret_cast<seq_f32x4*>(to) = seq_f32x4{h[0], h[1], h[2], h[3]};
+                *reinterpret_cast<scan_f32x4*>(to) = scan_f32x4{h[0], h[1], h[2], h[3]};
             }
             float part = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSub; ++i) {
-                const Pair s = row[t + i];
-                if (ENDS) part += s.e;
-                float y = 0.f;
+            for (int j = 0; j < kSub; j += 4) {
+                const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), ex = *reinterpret_cast<const scan_f32x4*>(ex_row + t + j);
+                scan_f32x4 y;
 #pragma unroll
-                for (int k = 0; k < kK; ++k) {
-                    h[k] = fmaf(exp2_hw(s.e * rate[k]), h[k], s.ex * sB[(t + i) * SP + kK * p + k]);
-                    if (!ENDS) y = fmaf(sC[(t + i) * SP + kK * p + k], h[k], y);
+                for (int i = 0; i < 4; ++i) {
+                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
+                    scan_f32x4 o;
+                    if (!ENDS) o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    float v = 0.f;
+#pragma unroll
+                    for (int k = 0; k < kK; ++k) {
+                        h[k] = fmaf(exp2_hw(e[i] * rate[k]), h[k], ex[i] * b[k]);
+                        if (!ENDS) v = k ? fmaf(o[k], h[k], v) : o[k] * h[k];
+                    }
+                    if (ENDS) part += e[i];
+                    else y[i] = channel_sum<P>(v);
                 }
-                if (!ENDS) {
-                    y = channel_sum<P>(y);
-                    if (p == 0) row[t + i].e = y;
-                }
+                if (!ENDS && p == 0) *reinterpret_cast<scan_f32x4*>(e_row + t + j) = y;
             }
             sum += part;
         }
         __syncthreads();
         if (ENDS) continue;
 #pragma unroll
-        for (int q = 0; q < PASSES; ++q) {
-            const int r = q * RPP + lane / LPR, c = 8 * (lane % LPR);
-            if (r >= CW || base + r >= a.Dg || t0 + c >= a.L) continue;
-            const long dr = static_cast<long>(at.g) * a.Dg + base + r;
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            if (!real[q] || t0 + c >= a.L) continue;
             float x[8], z[8], y[8];
-            row_load8<BF16>(scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, dr), t0 + c, len, x);
-            if (a.z) row_load8<BF16>(scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, dr), t0 + c, len, z);
-            const float skip = a.skip ? a.skip[dr] : 0.f;
-            const Pair* from = mine + r * STRIDE + c;
+            lds_get8(sE[wave] + row * R::RS + c, y);
+            if (inside) row_load8_inside<BF16>(x_row[q], t0 + c, x);
+            else row_load8<BF16>(x_row[q], t0 + c, len, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[i] = fmaf(skip, x[i], from[i].e);
-                if (a.z) y[i] *= z[i] * sigmoid_of(z[i]);
-                if (t0 + c + i >= len) y[i] = 0.f;
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(skip[q], x[i], y[i]);
+            if (a.z) {
+                const E* z_row = scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, dr[q]);
+                if (inside) row_load8_inside<BF16>(z_row, t0 + c, z);
+                else row_load8<BF16>(z_row, t0 + c, len, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] *= z[i] * sigmoid_of(z[i]);
             }
-            row_store8<BF16>(const_cast<typename RowElem<BF16>::type*>(scan_row<BF16>(a.out, a.out_sn, a.out_sd, at.n, dr)), t0 + c, a.L, y);
+            if (!inside) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
+            }
+            row_store8<BF16>(const_cast<E*>(scan_row<BF16>(a.out, a.out_sn, a.out_sd, at.n, dr[q])), t0 + c, a.L, y);
         }
     }
     if (!there) return;
     if (ENDS) {
         const long i = (at.n * a.nseg + at.seg) * a.D + d;
-        *reinterpret_cast<seq_f32x4*>(a.starts + i * SP + kK * p) = seq_f32x4{h[0], h[1], h[2], h[3]};
+        *reinterpret_cast<scan_f32x4*>(a.starts + i * SP + kK * p) = scan_f32x4{h[0], h[1], h[2], h[3]};
         if (p == 0) a.sums[i] = sum;
     } else if (a.final && at.seg == a.nseg - 1) {
 #pragma unroll
         for (int k = 0; k < kK; ++k)
             if (kK * p + k < a.S) a.final[(at.n * a.D + d) * a.S + kK * p + k] = h[k];
-    }
-}
-
-// starts[seg]: what segment seg adds to its state -> the state before it.  One lane per state.
-__global__ __launch_bounds__(kThreads) void scan_join_kernel(ScanArgs a, int SP) {
-    const long i = static_cast<long>(blockIdx.x) * kThreads + threadIdx.x;
-    const long nd = i / SP;
-    if (nd >= static_cast<long>(a.N) * a.D) return;
-    const int s = static_cast<int>(i - nd * SP);
-    const long n = nd / a.D, d = nd - n * a.D;
-    const float rate = scan_rate(a, d, s, true);
-    float h = a.init && s < a.S ? a.init[nd * a.S + s] : 0.f;
-#pragma unroll 8
-    for (int seg = 0; seg < a.nseg; ++seg) {
-        const long at = (n * a.nseg + seg) * a.D + d;
-        const float add = a.starts[at * SP + s], decay = exp2_hw(rate * a.sums[at]);
-        a.starts[at * SP + s] = h;
-        h = fmaf(decay, h, add);
     }
 }
 
@@ -198,9 +212,7 @@ hipError_t fwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
     const long most = kSeqMostThreads / block.x, blocks = scan_blocks(a);
     for (int stage = p.nseg > 1 ? 0 : 2; stage < 3; ++stage) {
         if (stage == 1) {
-            const long threads = static_cast<long>(a.N) * a.D * kK * P;
-            a.first = 0;
-            const hipError_t e = launch_kernel(scan_join_kernel, dim3(static_cast<unsigned>(cdiv(threads, kThreads))), dim3(kThreads), 0, st, a, kK * P);
+            const hipError_t e = scan_join_launch<false>(a.starts, a.sums, a.init, a.A, a.N, a.D, a.S, kK * P, a.nseg, st);
             if (e != hipSuccess) return e;
             continue;
         }
@@ -246,7 +258,7 @@ bool scan_ok(const conv1d_scan_t* p) {
 
 // rows and the lanes of their states are counted in 31 bits
 bool scan_sizes_ok(const conv1d_scan_t* p) {
-    return p->S <= kMostStates && static_cast<long>(p->N) * p->D <= 0x7fffffffL / 64;
+    return p->S <= kMostStates && static_cast<long>(p->N) * p->D <= 0x7fffffffL / 64 && p->L <= 1 << 30;
 }
 
 ScanArgs scan_args(const conv1d_scan_t* p, const ScanPlan& plan) {
@@ -300,9 +312,9 @@ ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd) {
     p.blocks_d = cdiv(need, p.waves);
     p.chunks = cdiv(L, kSub);
     const long waves = static_cast<long>(N) * G * p.blocks_d * p.waves;
-    long nseg = waves >= 700 ? 1 : cdiv(2048, waves);
+    long nseg = waves >= 1536 ? 1 : cdiv(4096, waves);
     const long tiles = cdiv(L, 64);
-    if (nseg > tiles / 4) nseg = tiles / 4;
+    if (nseg > tiles / 2) nseg = tiles / 2;
     if (nseg < 1) nseg = 1;
     p.seg_len = 64 * cdiv(tiles, nseg);
     p.nseg = cdiv(L, p.seg_len);

@@ -51,26 +51,39 @@ __device__ __forceinline__ unsigned short float_to_bf16(float v) {
     return u;
 }
 
-// elements at .. at + 7 of a row whose elements [0, end) are there; 0 elsewhere
+// elements at .. at + 7 of a row, all of them there
 template <bool BF16>
-__device__ __forceinline__ void row_load8(const void* row, long at, long end, float (&v)[8]) {
+__device__ __forceinline__ void row_load8_inside(const void* row, long at, float (&v)[8]) {
+    if constexpr (BF16) {
+        const seq_u16x8 t = *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = bf16_to_float(t[e]);
+    } else {
+        const seq_f32x4 a = *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + at);
+        const seq_f32x4 b = *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + at + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a[e];
+            v[4 + e] = b[e];
+        }
+    }
+}
+
+// elements at .. at + 7 of a row whose elements [0, end) are there; 0 elsewhere
+template <bool BF16, typename I>
+__device__ __forceinline__ void row_load8(const void* row, I at, I end, float (&v)[8]) {
     if (at >= 0 && at + 8 <= end) {
-        if constexpr (BF16) {
-            const seq_u16x8 t = *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + at);
+        row_load8_inside<BF16>(row, at, v);
+    } else if (at + 8 > 0 && at < end) {  // some of them: every load from a place that is there, without a branch
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = bf16_to_float(t[e]);
-        } else {
-            const seq_f32x4 a = *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + at);
-            const seq_f32x4 b = *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + at + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = a[e];
-                v[4 + e] = b[e];
-            }
+        for (int e = 0; e < 8; ++e) {
+            const I i = at + e, j = i < 0 ? 0 : i < end ? i : end - 1;
+            const float u = load_elem<BF16>(row, j);
+            v[e] = i == j ? u : 0.f;
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = at + e >= 0 && at + e < end ? load_elem<BF16>(row, at + e) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
     }
 }
 
@@ -109,7 +122,7 @@ __device__ __forceinline__ void store_elem(void* base, long i, float v) {
 }
 
 // positions of sequence n that count: all of them, or lengths[n] brought into [0, L]
-__device__ __forceinline__ long seq_length(const int* lengths, long n, int L) {
+__device__ __forceinline__ int seq_length(const int* lengths, long n, int L) {
     return lengths ? clampi(lengths[n], 0, L) : L;
 }
 
@@ -130,7 +143,7 @@ __device__ __forceinline__ float softplus_of(float v) {
     s = fmaf(s, q, 2.f / 5.f);
     s = fmaf(s, q, 2.f / 3.f);
     s = fmaf(s, q, 2.f);
-    return (v > 0.f ? v : v != v ? v : 0.f) + s * r;
+    return fmaf(s, r, fmaxf(v, 0.f));  // (a NaN comes through s r)
 }
 
 }  // namespace conv1d
