@@ -52,7 +52,7 @@ typedef __attribute__((ext_vector_type(4))) float scan_f32x4;  // (16-byte align
 
 // steps of a tile: 64 lanes stage 8 elements each of a wave's 64 / P rows, once or twice
 constexpr int scan_tile(int P) { return P == 16 || P == 8 ? 64 : P == 4 ? 32 : 16; }
-constexpr int scan_tile_back(int P) { return P >= 4 ? 32 : 16; }
+constexpr int scan_tile_back(int P) { return P == 4 ? 32 : 16; }
 // floats of a row in LDS: 16 rows of 4 steps lie in distinct banks
 constexpr int scan_stride(int T) { return T + 4; }
 

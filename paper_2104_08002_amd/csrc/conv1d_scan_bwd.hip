@@ -18,13 +18,24 @@ __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
 constexpr int kHalf = kSub / 2;  // steps whose states and decays are in registers at a time
 
-// One value per lane and state k, for dB and dC: the sums over the channels of the wave.  Afterwards the lanes whose place
-// within their row of 16 is p < P hold them: q[0] dB, q[1] dC of state 4 p + channel_state(row).
-#ifdef HOSTMODEL
+// Sums over the channels of a wave, of one value per lane for each of 4 states and 4 steps, halved by every exchange: over the
+// four rows of 16 lanes a pair of states leaves each lane one of them (rows_sum), over the channels within a row a pair of steps
+// (row_sums).  What is left are kSums<P> values; value j belongs to state kK p + sum_state(lane), step sum_step<P>(lane, j).
 template <int P>
-inline void wave_sums(const float (&dB)[kK], const float (&dC)[kK], float (&q)[2]) {
-    q[0] = dB[0];
-    q[1] = dC[0];
+constexpr int kSums = P <= 4 ? 1 : P == 8 ? 2 : 4;
+__device__ __forceinline__ int sum_state(int lane) {
+    const int row = lane >> 4;
+    return (row >> 1) | ((row & 1) << 1);
+}
+template <int P>
+__device__ __forceinline__ int sum_step(int lane, int j) {
+    return P <= 4 ? (lane >> 2) & 3 : P == 8 ? j + 2 * ((lane >> 3) & 1) : j;
+}
+#ifdef HOSTMODEL
+inline float rows_sum(const float (&v)[kK]) { return v[0]; }
+template <int P>
+inline void row_sums(const float (&q)[4], float (&out)[kSums<P>]) {
+    for (float& o : out) o = q[0];
 }
 #else
 __device__ __forceinline__ float swap32_add(float u, float v) {
@@ -35,24 +46,35 @@ __device__ __forceinline__ float swap16_add(float u, float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ __forceinline__ float rows_sum(const float (&v)[kK]) { return swap16_add(swap32_add(v[0], v[1]), swap32_add(v[2], v[3])); }
+// v in the banks (4 lanes each) of MASK, u in the others
+template <int MASK>
+__device__ __forceinline__ float by_bank(float u, float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(u), __float_as_int(v), 0xE4, 0xf, MASK, false));
+}
+// u of a lane's own and the other bank of a pair in the banks outside MASK, v in those of MASK; CTRL brings the other bank's
+template <int CTRL, int MASK>
+__device__ __forceinline__ float pair_sum(float u, float v) {
+    const float other = by_bank<MASK>(v, u);
+    return by_bank<MASK>(u, v) + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(other), CTRL, 0xf, 0xf, true));
+}
 template <int P>
-__device__ __forceinline__ void wave_sums(const float (&dB)[kK], const float (&dC)[kK], float (&q)[2]) {
-    q[0] = swap16_add(swap32_add(dB[0], dB[1]), swap32_add(dB[2], dB[3]));
-    q[1] = swap16_add(swap32_add(dC[0], dC[1]), swap32_add(dC[2], dC[3]));
+__device__ __forceinline__ void row_sums(const float (&q)[4], float (&out)[kSums<P>]) {
+    if constexpr (P <= 4) {
+        // row_ror:4 pairs every bank with the one before it, row_ror:8 with the one after the next: all four in two steps
+        float s = pair_sum<0x128, 0xC>(pair_sum<0x124, 0xA>(q[0], q[1]), pair_sum<0x124, 0xA>(q[2], q[3]));
+        if constexpr (P <= 2) s = add_dpp<0x4E>(s);
+        if constexpr (P <= 1) s = add_dpp<0xB1>(s);
+        out[0] = s;
+    } else if constexpr (P == 8) {
+        out[0] = pair_sum<0x128, 0xC>(q[0], q[2]);
+        out[1] = pair_sum<0x128, 0xC>(q[1], q[3]);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        if constexpr (P <= 8) q[j] = add_dpp<0x128>(q[j]);  // row_ror:8
-        if constexpr (P <= 4) q[j] = add_dpp<0x124>(q[j]);  // row_ror:4
-        if constexpr (P <= 2) q[j] = add_dpp<0x4E>(q[j]);
-        if constexpr (P <= 1) q[j] = add_dpp<0xB1>(q[j]);
+        for (int i = 0; i < 4; ++i) out[i] = q[i];
     }
 }
 #endif
-// rows of 16 lanes: 0, 1, 2, 3 hold state 0, 2, 1, 3
-__device__ __forceinline__ int channel_state(int lane) {
-    const int row = lane >> 4;
-    return (row >> 1) | ((row & 1) << 1);
-}
 
 // The lane's rows: where they begin and what they share.
 template <bool BF16, int P, int T>
@@ -174,13 +196,13 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
 
 template <bool BF16, int P>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = scan_tile_back(P), RED = SP + 1;
+    constexpr int SP = kK * P, T = scan_tile_back(P);
     using R = ScanRows<P, T>;
     using E = typename RowElem<BF16>::type;
     // e, x and dy of a step; the walk back leaves sum_s e g B, de and sum_s C h in their places
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS], sY[kScanWaves][R::CW * R::RS];
     __shared__ __align__(16) float sB[T * SP], sC[T * SP];
-    __shared__ float red[kScanWaves][2][kSub * RED];
+    __shared__ __align__(16) float red[kScanWaves][2][SP * R::RS];  // dB and dC of the wave's channels, [state][step]
     const ScanPlace at = scan_place(a);
     const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
@@ -261,22 +283,23 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t1 + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t1 + j),
                                      dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t1 + j);
                     scan_f32x4 out_x, out_e, out_y;
+                    float qB[4], qC[4];
 #pragma unroll
                     for (int i = 3; i >= 0; --i) {
                         const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t1 + j + i) * SP + kK * p);
                         const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t1 + j + i) * SP + kK * p);
                         const float ex = e[i] * x[i];
-                        float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK], q[2];
+                        float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK];
 #pragma unroll
                         for (int k = 0; k < kK; ++k) {
                             const float g = fmaf(o[k], dy[i], carry[k]);
-                            y = fmaf(o[k], h[j + i][k], y);
+                            y = k ? fmaf(o[k], h[j + i][k], y) : o[k] * h[j + i][k];
                             vC[k] = dy[i] * h[j + i][k];
                             vB[k] = g * ex;
-                            gb = fmaf(g, b[k], gb);
+                            gb = k ? fmaf(g, b[k], gb) : g * b[k];
                             carry[k] = g * decay[j + i][k];
                             const float kept = carry[k] * (j + i ? h[j + i - (j + i ? 1 : 0)][k] : mid[k]);
-                            qa = fmaf(kept, rate[k], qa);
+                            qa = k ? fmaf(kept, rate[k], qa) : kept * rate[k];
                             dA_sub[k] = fmaf(kept, e[i], dA_sub[k]);
                         }
                         gb = channel_sum<P>(gb);
@@ -284,12 +307,17 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                         out_y[i] = channel_sum<P>(y);
                         out_x[i] = gb * e[i];
                         out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
-                        wave_sums<P>(vB, vC, q);
-                        if ((lane & 15) < P) {
-                            const int to = (half + j + i) * RED + kK * p + channel_state(lane);
-                            red[wave][0][to] = q[0];
-                            red[wave][1][to] = q[1];
-                        }
+                        qB[i] = rows_sum(vB);
+                        qC[i] = rows_sum(vC);
+                    }
+                    float out_B[kSums<P>], out_C[kSums<P>];
+                    row_sums<P>(qB, out_B);
+                    row_sums<P>(qC, out_C);
+#pragma unroll
+                    for (int i = 0; i < kSums<P>; ++i) {
+                        const int to = (kK * p + sum_state(lane)) * R::RS + t1 + j + sum_step<P>(lane, i);
+                        red[wave][0][to] = out_B[i];
+                        red[wave][1][to] = out_C[i];
                     }
                     if (p == 0) {
                         *reinterpret_cast<scan_f32x4*>(e_row + t1 + j) = out_x;
@@ -302,19 +330,29 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             }
 #pragma unroll
             for (int k = 0; k < kK; ++k) dA[k] += dA_sub[k];
-            __syncthreads();
-            // over the waves of the workgroup, lanes along the sequence
-            for (int i = threadIdx.x; i < 2 * kSub * SP; i += blockDim.x) {
-                const int step = i & (kSub - 1), s = (i / kSub) & (SP - 1), which = i / (kSub * SP);
-                const int tt = t0 + t + step;
-                if (s >= a.S || tt >= a.L) continue;
-                float v = 0.f;
-                for (int w = 0; w < waves; ++w) v += red[w][which][step * RED + s];
-                const long o = ((at.n * a.G + at.g) * a.S + s) * a.L + tt;
-                if (a.blocks_d == 1) store_elem<BF16>(which ? a.dC : a.dB, o, v);
-                else a.part_bc[(static_cast<long>(which) * a.blocks_d + at.cb) * a.N * a.G * a.S * a.L + o] = v;
+        }
+        __syncthreads();
+        // dB and dC over the waves of the workgroup, 4 steps of a state each
+        for (int i = threadIdx.x; i < 2 * SP * (T / 4); i += blockDim.x) {
+            const int step = 4 * (i % (T / 4)), s = i / (T / 4) % SP, which = i / (T / 4) / SP, t = t0 + step;
+            if (s >= a.S || t >= a.L) continue;
+            scan_f32x4 v = *reinterpret_cast<const scan_f32x4*>(&red[0][which][s * R::RS + step]);
+            for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const scan_f32x4*>(&red[w][which][s * R::RS + step]);
+            const long o = ((at.n * a.G + at.g) * a.S + s) * a.L + t;
+            if (a.blocks_d > 1) {
+                float* to = a.part_bc + (static_cast<long>(which) * a.blocks_d + at.cb) * a.N * a.G * a.S * a.L + o;
+                if (t + 4 <= a.L) {
+                    *reinterpret_cast<seq_f32x4*>(to) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (t + e < a.L) to[e] = v[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t + e < a.L) store_elem<BF16>(which ? a.dC : a.dB, o + e, v[e]);
             }
-            __syncthreads();
         }
         // rows again: the gradients of x, dt and z
 #pragma unroll
@@ -359,6 +397,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, a.L, dx);
             row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, a.L, ddt);
         }
+        // (the next tile's barrier stands between these reads of `red` and its next values)
     }
     const long part = at.n * a.nseg + at.seg, segs = static_cast<long>(a.N) * a.nseg;
 #pragma unroll
