@@ -16,7 +16,7 @@
 namespace conv1d {
 
 constexpr int kK = 4;         // states of a lane
-constexpr int kSub = 16;      // steps between the states that the forward pass keeps for the backward pass
+constexpr int kSub = 8;       // steps between the states that the forward pass keeps for the backward pass
 constexpr int kScanWaves = 4; // most waves of a workgroup
 constexpr int kMostStates = 64;
 

@@ -16,7 +16,6 @@ constexpr int kThreads = 256;
 // What was read from LDS before is read again: kept, it would take the registers that a third and fourth wave need.
 __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
-constexpr int kHalf = kSub / 2;  // steps whose states and decays are in registers at a time
 
 // Sums over the channels of a wave, of one value per lane for each of 4 states and 4 steps, halved by every exchange: over the
 // four rows of 16 lanes a pair of states leaves each lane one of them (rows_sum), over the channels within a row a pair of steps
@@ -230,11 +229,12 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         scan_stage_states<BF16, P, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
         scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
+        float dA_tile[kK] = {0.f, 0.f, 0.f, 0.f};
         float *e_row = sE[wave] + cl * R::RS, *x_row = sX[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
 #pragma unroll 1
         for (int t = T - kSub; t >= 0; t -= kSub) {
             if (t0 + t >= a.L) continue;
-            float first[kK], mid[kK];  // the state before the first and the second half
+            float first[kK], h[kSub][kK], decay[kSub][kK];
 #pragma unroll
             for (int k = 0; k < kK; ++k) first[k] = 0.f;
             if (there) {
@@ -243,9 +243,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                 for (int k = 0; k < kK; ++k) first[k] = v[k];
             }
 #pragma unroll
-            for (int k = 0; k < kK; ++k) mid[k] = first[k];
-#pragma unroll
-            for (int j = 0; j < kHalf; j += 4) {
+            for (int j = 0; j < kSub; j += 4) {
                 __builtin_amdgcn_sched_barrier(0);
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j);
 #pragma unroll
@@ -253,84 +251,64 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
                     const float ex = e[i] * x[i];
 #pragma unroll
-                    for (int k = 0; k < kK; ++k) mid[k] = fmaf(exp2_hw(e[i] * rate[k]), mid[k], ex * b[k]);
+                    for (int k = 0; k < kK; ++k) {
+                        decay[j + i][k] = exp2_hw(e[i] * rate[k]);
+                        h[j + i][k] = fmaf(decay[j + i][k], j + i ? h[j + i - (j + i ? 1 : 0)][k] : first[k], ex * b[k]);
+                    }
                 }
             }
-            float dA_sub[kK] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-            for (int half = kHalf; half >= 0; half -= kHalf) {
-                const int t1 = t + half;
-                float h[kHalf][kK], decay[kHalf][kK];
 #pragma unroll
-                for (int j = 0; j < kHalf; j += 4) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t1 + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t1 + j);
+            for (int j = kSub - 4; j >= 0; j -= 4) {
+                reload_lds();
+                __builtin_amdgcn_sched_barrier(0);
+                const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j),
+                                 dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t + j);
+                scan_f32x4 out_x, out_e, out_y;
+                float qB[4], qC[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t1 + j + i) * SP + kK * p);
-                        const float ex = e[i] * x[i];
+                for (int i = 3; i >= 0; --i) {
+                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
+                    const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    const float ex = e[i] * x[i];
+                    float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK];
 #pragma unroll
-                        for (int k = 0; k < kK; ++k) {
-                            decay[j + i][k] = exp2_hw(e[i] * rate[k]);
-                            h[j + i][k] = fmaf(decay[j + i][k], j + i ? h[j + i - (j + i ? 1 : 0)][k] : mid[k], ex * b[k]);
-                        }
+                    for (int k = 0; k < kK; ++k) {
+                        const float g = fmaf(o[k], dy[i], carry[k]);
+                        y = k ? fmaf(o[k], h[j + i][k], y) : o[k] * h[j + i][k];
+                        vC[k] = dy[i] * h[j + i][k];
+                        vB[k] = g * ex;
+                        gb = k ? fmaf(g, b[k], gb) : g * b[k];
+                        carry[k] = g * decay[j + i][k];
+                        const float kept = carry[k] * (j + i ? h[j + i - (j + i ? 1 : 0)][k] : first[k]);
+                        qa = k ? fmaf(kept, rate[k], qa) : kept * rate[k];
+                        dA_tile[k] = fmaf(kept, e[i], dA_tile[k]);
                     }
+                    gb = channel_sum<P>(gb);
+                    qa = channel_sum<P>(qa);
+                    out_y[i] = channel_sum<P>(y);
+                    out_x[i] = gb * e[i];
+                    out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
+                    qB[i] = rows_sum(vB);
+                    qC[i] = rows_sum(vC);
                 }
+                float out_B[kSums<P>], out_C[kSums<P>];
+                row_sums<P>(qB, out_B);
+                row_sums<P>(qC, out_C);
 #pragma unroll
-                for (int j = kHalf - 4; j >= 0; j -= 4) {
-                    reload_lds();
-                    __builtin_amdgcn_sched_barrier(0);
-                    const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t1 + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t1 + j),
-                                     dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t1 + j);
-                    scan_f32x4 out_x, out_e, out_y;
-                    float qB[4], qC[4];
-#pragma unroll
-                    for (int i = 3; i >= 0; --i) {
-                        const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t1 + j + i) * SP + kK * p);
-                        const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t1 + j + i) * SP + kK * p);
-                        const float ex = e[i] * x[i];
-                        float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK];
-#pragma unroll
-                        for (int k = 0; k < kK; ++k) {
-                            const float g = fmaf(o[k], dy[i], carry[k]);
-                            y = k ? fmaf(o[k], h[j + i][k], y) : o[k] * h[j + i][k];
-                            vC[k] = dy[i] * h[j + i][k];
-                            vB[k] = g * ex;
-                            gb = k ? fmaf(g, b[k], gb) : g * b[k];
-                            carry[k] = g * decay[j + i][k];
-                            const float kept = carry[k] * (j + i ? h[j + i - (j + i ? 1 : 0)][k] : mid[k]);
-                            qa = k ? fmaf(kept, rate[k], qa) : kept * rate[k];
-                            dA_sub[k] = fmaf(kept, e[i], dA_sub[k]);
-                        }
-                        gb = channel_sum<P>(gb);
-                        qa = channel_sum<P>(qa);
-                        out_y[i] = channel_sum<P>(y);
-                        out_x[i] = gb * e[i];
-                        out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
-                        qB[i] = rows_sum(vB);
-                        qC[i] = rows_sum(vC);
-                    }
-                    float out_B[kSums<P>], out_C[kSums<P>];
-                    row_sums<P>(qB, out_B);
-                    row_sums<P>(qC, out_C);
-#pragma unroll
-                    for (int i = 0; i < kSums<P>; ++i) {
-                        const int to = (kK * p + sum_state(lane)) * R::RS + t1 + j + sum_step<P>(lane, i);
-                        red[wave][0][to] = out_B[i];
-                        red[wave][1][to] = out_C[i];
-                    }
-                    if (p == 0) {
-                        *reinterpret_cast<scan_f32x4*>(e_row + t1 + j) = out_x;
-                        *reinterpret_cast<scan_f32x4*>(x_row + t1 + j) = out_e;
-                        *reinterpret_cast<scan_f32x4*>(dy_row + t1 + j) = out_y;
-                    }
+                for (int i = 0; i < kSums<P>; ++i) {
+                    const int to = (kK * p + sum_state(lane)) * R::RS + t + j + sum_step<P>(lane, i);
+                    red[wave][0][to] = out_B[i];
+                    red[wave][1][to] = out_C[i];
                 }
-#pragma unroll
-                for (int k = 0; k < kK; ++k) mid[k] = first[k];
+                if (p == 0) {
+                    *reinterpret_cast<scan_f32x4*>(e_row + t + j) = out_x;
+                    *reinterpret_cast<scan_f32x4*>(x_row + t + j) = out_e;
+                    *reinterpret_cast<scan_f32x4*>(dy_row + t + j) = out_y;
+                }
             }
-#pragma unroll
-            for (int k = 0; k < kK; ++k) dA[k] += dA_sub[k];
         }
+#pragma unroll
+        for (int k = 0; k < kK; ++k) dA[k] += dA_tile[k];
         __syncthreads();
         // dB and dC over the waves of the workgroup, 4 steps of a state each
         for (int i = threadIdx.x; i < 2 * SP * (T / 4); i += blockDim.x) {

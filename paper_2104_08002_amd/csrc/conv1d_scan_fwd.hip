@@ -311,14 +311,13 @@ ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd) {
     p.waves = need < kScanWaves ? need : kScanWaves;
     p.blocks_d = cdiv(need, p.waves);
     p.chunks = cdiv(L, kSub);
-    const long waves = static_cast<long>(N) * G * p.blocks_d * p.waves;
-    long nseg = waves >= 1536 ? 1 : cdiv(4096, waves);
+    const long waves = static_cast<long>(N) * G * p.blocks_d * p.waves, room = 1024L * 8;
     const long tiles = cdiv(L, 64);
+    long nseg = room / waves;
     if (nseg > tiles / 2) nseg = tiles / 2;
     if (nseg < 1) nseg = 1;
     p.seg_len = 64 * cdiv(tiles, nseg);
     p.nseg = cdiv(L, p.seg_len);
-    (void)bwd;
     return p;
 }
 
