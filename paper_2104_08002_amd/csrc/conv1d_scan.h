@@ -32,7 +32,7 @@ struct ScanArgs {
     int N, D, L, S, G, Dg, softplus;
     long x_sn, x_sd, dt_sn, dt_sd, z_sn, z_sd, out_sn, out_sd;
     long b_sn, b_sg, b_ss, c_sn, c_sg, c_ss;
-    int nseg, seg_len; // the sequence in segments of seg_len steps, a multiple of 64
+    int nseg, seg_len; // the sequence in segments of seg_len steps, a multiple of scan_tile(P)
     int chunks;        // ceil(L / kSub)
     int blocks_d;      // workgroups along the channels of a group
     long first;        // first workgroup of the launch
@@ -42,8 +42,7 @@ struct ScanArgs {
     const float* dfinal;
     void *dx, *ddt, *dz, *dB, *dC;   // contiguous, in the type of x
     float* part_bc;    // [2][blocks_d][N][G][S][L]: sums over a workgroup's channels (blocks_d > 1)
-    float* part_a;     // [N * nseg][D][4 P]
-    float* part_d;     // [2][N * nseg][D]: of skip and of dt_bias
+    float* part_p;     // [N * nseg][D * (4 P + 2)]: what a segment adds to the gradients of A, then of skip, then of dt_bias
     float* carries;    // [N][nseg][D][4 P]: what the later segments send into each (split only)
     float* dinit;      // [N][D][S] or nullptr
 };
@@ -143,57 +142,67 @@ __device__ __forceinline__ void lds_get8(const float* from, float (&v)[8]) {
 
 // One (sample, channel) row of segment values joined along the sequence: value[seg] holds what a segment adds, and becomes
 // what comes into it from the segments before (BACK: behind) it, `first` into the first; sums[seg]: exp(A sum) is a segment's
-// decay.  SP states times `chunks` runs of `len` segments a row; a run is joined in itself, the runs before it through LDS.
+// decay.  SP states times `chunks` runs of kRun segments at a time: a run is joined in registers, the runs through LDS.
+constexpr int kRun = 8;
 template <bool BACK>
 __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const float* sums, const float* first, const float* A, int N, int D,
-                                                         int S, int SP, int nseg, int chunks, int len) {
-    __shared__ float run_decay[1024], run_add[1024];
+                                                         int S, int SP, int nseg, int chunks) {
+    __shared__ float run_decay[1024], run_add[1024], last[1024];
     const int per_row = SP * chunks;
     const long row = static_cast<long>(blockIdx.x) * (blockDim.x / per_row) + threadIdx.x / per_row;
     const bool there = row < static_cast<long>(N) * D;
-    const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP;
+    const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP, base = threadIdx.x - in_row + s;
     const long n = there ? row / D : 0, d = there ? row - n * D : 0;
     const float rate = there && s < S ? A[d * S + s] * kLog2e : 0.f;
-    const int from = min(nseg, chunk * len), to = there ? min(nseg, from + len) : from;
-    float decay = 1.f, add = 0.f;
-#pragma unroll 8
-    for (int i = from; i < to; ++i) {
-        const long at = (n * nseg + (BACK ? nseg - 1 - i : i)) * D + d;
-        const float f = exp2_hw(rate * sums[at]);
-        add = fmaf(f, add, value[at * SP + s]);
-        decay *= f;
-    }
-    run_decay[threadIdx.x] = decay;
-    run_add[threadIdx.x] = add;
-    __syncthreads();
     float h = there && first && s < S ? first[(n * D + d) * S + s] : 0.f;
-    const int base = threadIdx.x - in_row + s;
-    for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
+    for (int from = 0; from < nseg; from += kRun * chunks) {
+        float f[kRun], v[kRun], decay = 1.f, add = 0.f;
+        const int i0 = from + kRun * chunk;
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const bool real = there && i0 + i < nseg;
+            const long at = (n * nseg + (!real ? 0 : BACK ? nseg - 1 - (i0 + i) : i0 + i)) * D + d;
+            f[i] = real ? sums[at] : 0.f;
+            v[i] = real ? value[at * SP + s] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            f[i] = exp2_hw(rate * f[i]);
+            add = fmaf(f[i], add, v[i]);
+            decay *= f[i];
+        }
+        run_decay[threadIdx.x] = decay;
+        run_add[threadIdx.x] = add;
+        __syncthreads();
 #pragma unroll 8
-    for (int i = from; i < to; ++i) {
-        const long at = (n * nseg + (BACK ? nseg - 1 - i : i)) * D + d;
-        const float f = exp2_hw(rate * sums[at]), v = value[at * SP + s];
-        value[at * SP + s] = h;
-        h = fmaf(f, h, v);
+        for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            if (there && i0 + i < nseg) value[((n * nseg + (BACK ? nseg - 1 - (i0 + i) : i0 + i)) * D + d) * SP + s] = h;
+            h = fmaf(f[i], h, v[i]);
+        }
+        if (from + kRun * chunks >= nseg) break;  // (of the whole workgroup)
+        if (chunk == chunks - 1) last[base] = h;
+        __syncthreads();
+        h = last[base];
     }
 }
 
-// runs of about 8 segments, 1024 lanes of a workgroup at most
 template <bool BACK>
 inline hipError_t scan_join_launch(float* value, const float* sums, const float* first, const float* A, int N, int D, int S, int SP, int nseg,
                                    hipStream_t st) {
     int chunks = 1;
-    while (chunks * 8 < nseg && chunks * 2 * SP <= 1024) chunks *= 2;
+    while (chunks * kRun < nseg && chunks * 2 * SP <= 1024) chunks *= 2;
     const int per_row = SP * chunks, threads = per_row > 256 ? per_row : 256;
     return launch_kernel(scan_join_kernel<BACK>, dim3(static_cast<unsigned>(cdiv(static_cast<long>(N) * D, threads / per_row))), dim3(threads), 0, st,
-                         value, sums, first, A, N, D, S, SP, nseg, chunks, cdiv(nseg, chunks));
+                         value, sums, first, A, N, D, S, SP, nseg, chunks);
 }
 
 // host
 struct ScanPlan {
     int P, waves, blocks_d, nseg, seg_len, chunks;
 };
-ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd);
+ScanPlan scan_plan(int N, int D, int L, int S, int G);
 hipError_t scan_fwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, hipStream_t st);
 hipError_t scan_bwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, float* dA, float* dskip, float* dbias, hipStream_t st);
 

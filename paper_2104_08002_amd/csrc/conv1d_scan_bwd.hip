@@ -12,7 +12,6 @@
 namespace conv1d {
 namespace {
 
-constexpr int kThreads = 256;
 // What was read from LDS before is read again: kept, it would take the registers that a third and fourth wave need.
 __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
@@ -377,7 +376,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         }
         // (the next tile's barrier stands between these reads of `red` and its next values)
     }
-    const long part = at.n * a.nseg + at.seg, segs = static_cast<long>(a.N) * a.nseg;
+    float* part = a.part_p + (at.n * a.nseg + at.seg) * (static_cast<long>(a.D) * (SP + 2));
 #pragma unroll
     for (int q = 0; q < R::PASSES; ++q) {
 #pragma unroll
@@ -386,11 +385,11 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             dbias[q] += lane_xor(dbias[q], m);
         }
         if (lane % R::LPR || !rows.real[q]) continue;
-        a.part_d[part * a.D + rows.d[q]] = dskip[q];
-        a.part_d[(segs + part) * a.D + rows.d[q]] = dbias[q];
+        part[static_cast<long>(a.D) * SP + rows.d[q]] = dskip[q];
+        part[static_cast<long>(a.D) * (SP + 1) + rows.d[q]] = dbias[q];
     }
     if (!there) return;
-    *reinterpret_cast<scan_f32x4*>(a.part_a + (part * a.D + d) * SP + kK * p) = scan_f32x4{dA[0], dA[1], dA[2], dA[3]};
+    *reinterpret_cast<seq_f32x4*>(part + d * SP + kK * p) = seq_f32x4{dA[0], dA[1], dA[2], dA[3]};
     if (a.dinit && at.seg == 0) {
 #pragma unroll
         for (int k = 0; k < kK; ++k)
@@ -398,49 +397,62 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     }
 }
 
-// dB and dC from the sums of the workgroups along the channels
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void scan_sum_states_kernel(const float* part, void* dB, void* dC, long n, int blocks, long first) {
-    const long groups = (n + 7) / 8;
-    long i = first + static_cast<long>(blockIdx.x) * kThreads + threadIdx.x;
-    if (i >= 2 * groups) return;
-    const int which = i >= groups;
-    i = 8 * (i - which * groups);
-    float v[8] = {}, u[8];
-    for (int b = 0; b < blocks; ++b) {
-        row_load8<false>(part + (static_cast<long>(which) * blocks + b) * n, i, n, u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += u[e];
-    }
-    row_store8<BF16>(which ? dC : dB, i, n, v);
-}
-
-// columns of a matrix [rows][cols] summed in 64 bits: 16 columns, 64 shares of the rows a workgroup
+// What is left of sums: the first workgroups add the columns of part_p over its rows in 64 bits (the error of a gradient is that
+// of its partial sums), kCols columns and kShares shares of the rows each; the others add dB and dC over the workgroups along
+// the channels, 8 elements a lane.
 constexpr int kCols = 16, kShares = 64;
-__global__ __launch_bounds__(kCols* kShares) void scan_sum_rows_kernel(const float* part, float* out, long rows, long cols, int SP, int S) {
+struct SumArgs {
+    const float *part_p, *part_bc;
+    float *dA, *dskip, *dbias;
+    void *dB, *dC;
+    long rows, n;          // rows of part_p; elements of dB
+    int D, S, SP, blocks_d, param_blocks;
+    long first;            // first workgroup of the launch
+};
+template <bool BF16>
+__global__ __launch_bounds__(kCols* kShares) void scan_sums_kernel(SumArgs a) {
     __shared__ double sums[kShares][kCols];
+    const long block = a.first + blockIdx.x;
+    if (block >= a.param_blocks) {
+        const long groups = (a.n + 7) / 8;
+        long i = (block - a.param_blocks) * (kCols * kShares) + threadIdx.x;
+        if (i >= 2 * groups) return;
+        const int which = i >= groups;
+        i = 8 * (i - which * groups);
+        float v[8] = {}, u[8];
+        for (int b = 0; b < a.blocks_d; ++b) {
+            row_load8<false>(a.part_bc + (static_cast<long>(which) * a.blocks_d + b) * a.n, i, a.n, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += u[e];
+        }
+        row_store8<BF16>(which ? a.dC : a.dB, i, a.n, v);
+        return;
+    }
     const int c = threadIdx.x % kCols, share = threadIdx.x / kCols;
-    const long col = static_cast<long>(blockIdx.x) * kCols + c;
+    const long cols = static_cast<long>(a.D) * (a.SP + 2), col = block * kCols + c;
     double sum = 0.0;
     if (col < cols) {
 #pragma unroll 8
-        for (long r = share; r < rows; r += kShares) sum += static_cast<double>(part[r * cols + col]);
+        for (long r = share; r < a.rows; r += kShares) sum += static_cast<double>(a.part_p[r * cols + col]);
     }
     sums[share][c] = sum;
     __syncthreads();
     if (share || col >= cols) return;
+#pragma unroll 8
     for (int i = 1; i < kShares; ++i) sum += sums[i][c];
-    const long d = col / SP;
-    const int s = static_cast<int>(col - d * SP);
-    if (s < S) out[d * S + s] = static_cast<float>(sum);
-}
-
-hipError_t sum_rows(const float* part, float* out, long rows, long cols, int SP, int S, hipStream_t st) {
-    return launch_kernel(scan_sum_rows_kernel, dim3(static_cast<unsigned>(cdiv(cols, kCols))), dim3(kCols * kShares), 0, st, part, out, rows, cols, SP, S);
+    const long d = col / a.SP;
+    const int s = static_cast<int>(col - d * a.SP);
+    if (d < a.D) {
+        if (s < a.S) a.dA[d * a.S + s] = static_cast<float>(sum);
+    } else {
+        const long j = col - static_cast<long>(a.D) * a.SP;
+        float* to = j < a.D ? a.dskip : a.dbias;
+        if (to) to[j < a.D ? j : j - a.D] = static_cast<float>(sum);
+    }
 }
 
 template <bool BF16, int P>
-hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
+hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, float* dA, float* dskip, float* dbias, hipStream_t st) {
     const dim3 block(static_cast<unsigned>(p.waves * kSeqWave));
     const long most = kSeqMostThreads / block.x, blocks = scan_blocks(a);
     for (int stage = p.nseg > 1 ? 0 : 2; stage < 3; ++stage) {
@@ -456,39 +468,38 @@ hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
             if (e != hipSuccess) return e;
         }
     }
-    if (p.blocks_d > 1) {
-        const long n = static_cast<long>(a.N) * a.G * a.S * a.L, threads = 2 * ((n + 7) / 8);
-        for (long first = 0; first < threads; first += kSeqMostThreads) {
-            const long left = threads - first;
-            const hipError_t e = launch_kernel(scan_sum_states_kernel<BF16>, dim3(static_cast<unsigned>(cdiv(left < kSeqMostThreads ? left : kSeqMostThreads, kThreads))),
-                                               dim3(kThreads), 0, st, a.part_bc, a.dB, a.dC, n, p.blocks_d, first);
-            if (e != hipSuccess) return e;
-        }
+    SumArgs u{};
+    u.part_p = a.part_p; u.part_bc = a.part_bc;
+    u.dA = dA; u.dskip = dskip; u.dbias = dbias; u.dB = a.dB; u.dC = a.dC;
+    u.rows = static_cast<long>(a.N) * a.nseg;
+    u.n = static_cast<long>(a.N) * a.G * a.S * a.L;
+    u.D = a.D; u.S = a.S; u.SP = kK * P; u.blocks_d = p.blocks_d;
+    u.param_blocks = cdiv(static_cast<long>(a.D) * (u.SP + 2), kCols);
+    const long sum_blocks = u.param_blocks + (p.blocks_d > 1 ? (2 * ((u.n + 7) / 8) + kCols * kShares - 1) / (kCols * kShares) : 0);
+    constexpr long most_sums = kSeqMostThreads / (kCols * kShares);
+    for (u.first = 0; u.first < sum_blocks; u.first += most_sums) {
+        const long left = sum_blocks - u.first;
+        const hipError_t e = launch_kernel(scan_sums_kernel<BF16>, dim3(static_cast<unsigned>(left < most_sums ? left : most_sums)), dim3(kCols * kShares), 0, st, u);
+        if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
 template <bool BF16>
-hipError_t bwd_type(const ScanArgs& a, const ScanPlan& p, hipStream_t st) {
+hipError_t bwd_type(const ScanArgs& a, const ScanPlan& p, float* dA, float* dskip, float* dbias, hipStream_t st) {
     switch (p.P) {
-        case 1: return bwd_launch<BF16, 1>(a, p, st);
-        case 2: return bwd_launch<BF16, 2>(a, p, st);
-        case 4: return bwd_launch<BF16, 4>(a, p, st);
-        case 8: return bwd_launch<BF16, 8>(a, p, st);
-        default: return bwd_launch<BF16, 16>(a, p, st);
+        case 1: return bwd_launch<BF16, 1>(a, p, dA, dskip, dbias, st);
+        case 2: return bwd_launch<BF16, 2>(a, p, dA, dskip, dbias, st);
+        case 4: return bwd_launch<BF16, 4>(a, p, dA, dskip, dbias, st);
+        case 8: return bwd_launch<BF16, 8>(a, p, dA, dskip, dbias, st);
+        default: return bwd_launch<BF16, 16>(a, p, dA, dskip, dbias, st);
     }
 }
 
 }  // namespace
 
 hipError_t scan_bwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, float* dA, float* dskip, float* dbias, hipStream_t st) {
-    hipError_t e = bf16 ? bwd_type<true>(a, p, st) : bwd_type<false>(a, p, st);
-    const long rows = static_cast<long>(a.N) * a.nseg;
-    const int SP = kK * p.P;
-    if (e == hipSuccess) e = sum_rows(a.part_a, dA, rows, static_cast<long>(a.D) * SP, SP, a.S, st);
-    if (e == hipSuccess && dskip) e = sum_rows(a.part_d, dskip, rows, a.D, 1, 1, st);
-    if (e == hipSuccess && dbias) e = sum_rows(a.part_d + rows * a.D, dbias, rows, a.D, 1, 1, st);
-    return e;
+    return bf16 ? bwd_type<true>(a, p, dA, dskip, dbias, st) : bwd_type<false>(a, p, dA, dskip, dbias, st);
 }
 
 }  // namespace conv1d

@@ -283,16 +283,15 @@ size_t split_bytes(int N, int D, const ScanPlan& p) {
 
 // where the parts of a backward call's workspace begin
 struct BwdSpace {
-    size_t carries, sums, a, d, bc, total;
+    size_t carries, sums, params, bc, total;
 };
 BwdSpace bwd_space(int N, int D, int L, int S, int G, const ScanPlan& p) {
     const size_t rows = static_cast<size_t>(N) * p.nseg * D;
     BwdSpace w{};
     w.carries = 0;
     w.sums = w.carries + (p.nseg > 1 ? round256(rows * kK * p.P * sizeof(float)) : 0);
-    w.a = w.sums + (p.nseg > 1 ? round256(rows * sizeof(float)) : 0);
-    w.d = w.a + round256(rows * kK * p.P * sizeof(float));
-    w.bc = w.d + round256(2 * rows * sizeof(float));
+    w.params = w.sums + (p.nseg > 1 ? round256(rows * sizeof(float)) : 0);
+    w.bc = w.params + round256(rows * (kK * p.P + 2) * sizeof(float));
     w.total = w.bc + (p.blocks_d > 1 ? round256(2 * sizeof(float) * static_cast<size_t>(p.blocks_d) * N * G * S * L) : 0);
     return w;
 }
@@ -301,9 +300,10 @@ int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; 
 
 }  // namespace
 
-// Segments: as many as give every SIMD of the chip (4 x 256) a wave or two, but none shorter than 4 tiles; none where the
-// rows alone give most SIMDs a wave, because a cut sequence takes the exponentials twice.
-ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd) {
+// Segments: as many as give the chip's 1024 SIMDs 8 waves each (2 to 3 turns of what fits beside each other: the turns even out),
+// none shorter than a tile; one where the rows alone do.  A wave alone on its SIMD issues an instruction in 8 clocks, so that
+// few rows want short segments: N = 3, D = 49, L = 4999, S = 5 in FP32 takes 18 us backwards in segments of 16 steps, 39 in 128.
+ScanPlan scan_plan(int N, int D, int L, int S, int G) {
     ScanPlan p{};
     p.P = lanes_of(S);
     const int CW = kSeqWave / p.P, Dg = D / G;
@@ -312,11 +312,12 @@ ScanPlan scan_plan(int N, int D, int L, int S, int G, bool bwd) {
     p.blocks_d = cdiv(need, p.waves);
     p.chunks = cdiv(L, kSub);
     const long waves = static_cast<long>(N) * G * p.blocks_d * p.waves, room = 1024L * 8;
-    const long tiles = cdiv(L, 64);
+    const int unit = scan_tile(p.P);
+    const long tiles = cdiv(L, unit);
     long nseg = room / waves;
-    if (nseg > tiles / 2) nseg = tiles / 2;
+    if (nseg > tiles) nseg = tiles;
     if (nseg < 1) nseg = 1;
-    p.seg_len = 64 * cdiv(tiles, nseg);
+    p.seg_len = unit * cdiv(tiles, nseg);
     p.nseg = cdiv(L, p.seg_len);
     return p;
 }
@@ -339,7 +340,7 @@ extern "C" {
 
 size_t conv1d_scan_fwd_workspace_bytes(int N, int D, int L, int S, int G) {
     if (N < 1 || D < 1 || L < 1 || S < 1 || S > kMostStates || G < 1 || D % G) return 0;
-    return split_bytes(N, D, scan_plan(N, D, L, S, G, false));
+    return split_bytes(N, D, scan_plan(N, D, L, S, G));
 }
 
 size_t conv1d_scan_saved_bytes(int N, int D, int L, int S) {
@@ -353,7 +354,7 @@ int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float
     if (!seq_aligned(y, p->dtype == CONV1D_BF16 ? 2 : 4) || !seq_aligned(final, 4) || !seq_aligned(saved, 16) || !seq_aligned(workspace, 256))
         return CONV1D_EINVAL;
     if (!scan_sizes_ok(p)) return CONV1D_EUNSUPPORTED;
-    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G, false);
+    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G);
     const size_t need = split_bytes(p->N, p->D, plan);
     if (need && (!workspace || workspace_bytes < need)) return CONV1D_EWORKSPACE;
     ScanArgs a = scan_args(p, plan);
@@ -367,7 +368,7 @@ int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float
 
 size_t conv1d_scan_bwd_workspace_bytes(int N, int D, int L, int S, int G) {
     if (N < 1 || D < 1 || L < 1 || S < 1 || S > kMostStates || G < 1 || D % G) return 0;
-    return bwd_space(N, D, L, S, G, scan_plan(N, D, L, S, G, true)).total;
+    return bwd_space(N, D, L, S, G, scan_plan(N, D, L, S, G)).total;
 }
 
 int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_sd, const float* dfinal, const void* saved, void* dx,
@@ -384,7 +385,7 @@ int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_
         if (!seq_aligned(v, 4)) return CONV1D_EINVAL;
     if (!seq_aligned(saved, 16) || !seq_aligned(workspace, 256)) return CONV1D_EINVAL;
     if (!scan_sizes_ok(p)) return CONV1D_EUNSUPPORTED;
-    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G, true);
+    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G);
     const BwdSpace w = bwd_space(p->N, p->D, p->L, p->S, p->G, plan);
     if (!workspace || workspace_bytes < w.total) return CONV1D_EWORKSPACE;
     char* ws = static_cast<char*>(workspace);
@@ -394,8 +395,7 @@ int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_
     a.dx = dx; a.ddt = ddt; a.dz = dz; a.dB = dB; a.dC = dC; a.dinit = dinit;
     a.carries = reinterpret_cast<float*>(ws + w.carries);
     a.sums = reinterpret_cast<float*>(ws + w.sums);
-    a.part_a = reinterpret_cast<float*>(ws + w.a);
-    a.part_d = reinterpret_cast<float*>(ws + w.d);
+    a.part_p = reinterpret_cast<float*>(ws + w.params);
     a.part_bc = reinterpret_cast<float*>(ws + w.bc);
     return status_of(scan_bwd_launch(a, plan, p->dtype == CONV1D_BF16, dA, dskip, ddt_bias, static_cast<hipStream_t>(stream)));
 }
