@@ -4,9 +4,10 @@
 //   h[s] = a[s] h[s] + e x B[s];  y = sum_s C[s] h[s] + skip[d] x;  out = y z sigmoid(z)
 // for every sample n and channel d, S states each; B and C are shared by the D / G channels of a group.
 //
-// Lanes.  P = 1, 2, 4, 8 or 16 neighbouring lanes have one channel, kK = 4 states each, in registers (S is padded to 4 P with
-// zeros); a wave has 64 / P channels.  One step costs a lane 4 exponentials (a quarter of the rate of a product) and 16
-// products, which is what bounds the scan.  Rows lie along the sequence, states across lanes: a tile of steps goes through
+// Lanes.  P neighbouring lanes have one channel, K states each, in registers (S is padded to K P with zeros): 4 lanes of 1, 2 or
+// 4 states up to S = 16, 8 or 16 lanes of 4 beyond; a wave has 64 / P channels.  One step costs a lane K exponentials (half the
+// rate of a product) and 4 K products, which is what bounds the scan.  (With 4 states a lane for every S, S = 8 has 32 channels a
+// wave and room in LDS for 16 steps of them: it took as long as S = 16.)  Rows lie along the sequence, states across lanes: a tile of steps goes through
 // LDS, loaded and stored along rows (8 elements a lane), read 4 steps at a time.
 // Positions behind a sequence's length have e = 0 and e x = 0, which leaves the state as it is.
 #pragma once
@@ -15,7 +16,6 @@
 
 namespace conv1d {
 
-constexpr int kK = 4;         // states of a lane
 constexpr int kSub = 8;       // steps between the states that the forward pass keeps for the backward pass
 constexpr int kScanWaves = 4; // most waves of a workgroup
 constexpr int kMostStates = 64;
@@ -26,8 +26,8 @@ struct ScanArgs {
     const int* lengths;
     void* out;
     float* final;      // [N][D][S] or nullptr
-    float* saved;      // [N][chunks][D][4 P]: the state before every kSub-th step, or nullptr
-    float* starts;     // [N][nseg][D][4 P]: state before each segment (split only)
+    float* saved;      // [N][chunks][D][K P]: the state before every kSub-th step, or nullptr
+    float* starts;     // [N][nseg][D][K P]: state before each segment (split only)
     float* sums;       // [N][nseg][D]: sum of e over each segment
     int N, D, L, S, G, Dg, softplus;
     long x_sn, x_sd, dt_sn, dt_sd, z_sn, z_sd, out_sn, out_sd;
@@ -42,15 +42,41 @@ struct ScanArgs {
     const float* dfinal;
     void *dx, *ddt, *dz, *dB, *dC;   // contiguous, in the type of x
     float* part_bc;    // [2][blocks_d][N][G][S][L]: sums over a workgroup's channels (blocks_d > 1)
-    float* part_p;     // [N * nseg][D * (4 P + 2)]: what a segment adds to the gradients of A, then of skip, then of dt_bias
-    float* carries;    // [N][nseg][D][4 P]: what the later segments send into each (split only)
+    float* part_p;     // [N * nseg][D * (K P + 2)]: what a segment adds to the gradients of A, then of skip, then of dt_bias
+    float* carries;    // [N][nseg][D][K P]: what the later segments send into each (split only)
     float* dinit;      // [N][D][S] or nullptr
 };
 
 typedef __attribute__((ext_vector_type(4))) float scan_f32x4;  // (16-byte aligned: LDS, and what the kernels keep)
 
-// steps of a tile: 64 lanes stage 8 elements each of a wave's 64 / P rows, once or twice
-constexpr int scan_tile(int P) { return P == 16 || P == 8 ? 64 : P == 4 ? 32 : 16; }
+template <int K>
+struct States {  // of a lane, aligned
+    typedef __attribute__((ext_vector_type(K))) float vec;
+    vec v;
+    __device__ __forceinline__ float operator[](int k) const { return v[k]; }
+};
+template <>
+struct States<1> {
+    float v;
+    __device__ __forceinline__ float operator[](int) const { return v; }
+};
+template <int K>
+__device__ __forceinline__ States<K> states_at(const float* p) { return *reinterpret_cast<const States<K>*>(p); }
+template <int K>
+__device__ __forceinline__ void put_states(float* p, const float (&h)[K]) {
+    States<K> s;
+    if constexpr (K == 1) {
+        s.v = h[0];
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) s.v[k] = h[k];
+    }
+    *reinterpret_cast<States<K>*>(p) = s;
+}
+
+// steps of a tile: forwards the 64 lanes stage 8 elements each of a wave's 64 / P rows (half of them for P = 16); backwards the
+// sums over waves want LDS too
+constexpr int scan_tile(int P) { return P == 4 ? 32 : 64; }
 constexpr int scan_tile_back(int P) { return P == 4 ? 32 : 16; }
 // floats of a row in LDS: 16 rows of 4 steps lie in distinct banks
 constexpr int scan_stride(int T) { return T + 4; }
@@ -101,10 +127,9 @@ __device__ __forceinline__ const typename RowElem<BF16>::type* scan_row(const vo
     return static_cast<const typename RowElem<BF16>::type*>(base) + n * sn + d * sd;
 }
 
-// B or C of T steps from t0 on into LDS, [step][4 P]; 0 behind `end` and for states that are not there
-template <bool BF16, int P, int T>
+// B or C of T steps from t0 on into LDS, [step][SP]; 0 behind `end` and for states that are not there
+template <bool BF16, int SP, int T>
 __device__ __forceinline__ void scan_stage_states(const void* from, long base, long ss, int S, int t0, int end, float* to) {
-    constexpr int SP = kK * P;
     const typename RowElem<BF16>::type* row0 = static_cast<const typename RowElem<BF16>::type*>(from) + base;
     for (int i = threadIdx.x; i < SP * (T / 8); i += blockDim.x) {
         const int s = i & (SP - 1), c = i / SP;
@@ -200,7 +225,7 @@ inline hipError_t scan_join_launch(float* value, const float* sums, const float*
 
 // host
 struct ScanPlan {
-    int P, waves, blocks_d, nseg, seg_len, chunks;
+    int K, P, waves, blocks_d, nseg, seg_len, chunks;
 };
 ScanPlan scan_plan(int N, int D, int L, int S, int G);
 hipError_t scan_fwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, hipStream_t st);

@@ -16,23 +16,22 @@ namespace {
 __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
 
-// Sums over the channels of a wave, of one value per lane for each of 4 states and 4 steps, halved by every exchange: over the
-// four rows of 16 lanes a pair of states leaves each lane one of them (rows_sum), over the channels within a row a pair of steps
-// (row_sums).  What is left are kSums<P> values; value j belongs to state kK p + sum_state(lane), step sum_step<P>(lane, j).
-template <int P>
-constexpr int kSums = P <= 4 ? 1 : P == 8 ? 2 : 4;
-__device__ __forceinline__ int sum_state(int lane) {
-    const int row = lane >> 4;
-    return (row >> 1) | ((row & 1) << 1);
-}
-template <int P>
-__device__ __forceinline__ int sum_step(int lane, int j) {
-    return P <= 4 ? (lane >> 2) & 3 : P == 8 ? j + 2 * ((lane >> 3) & 1) : j;
+// Sums over the channels of a wave, of one value per lane for each of K states and 4 steps, value K step + state.  Every exchange
+// adds a pair of values and leaves each lane one of the two: between the halves of the wave, between its rows of 16, between
+// banks of 4 lanes (P <= 4), between halves of a row (P <= 8); a level that finds a single value adds it in all lanes.  The
+// kSums<K, P> values left are those of sum_value.
+template <int K, int P>
+constexpr int kSums = P <= 4 ? 1 : P == 8 ? K / 2 : K;
+template <int K, int P>
+__device__ __forceinline__ int sum_value(int lane, int j) {
+    const int half = lane >> 5, row = (lane >> 4) & 1, bank = (lane >> 2) & 1, side = (lane >> 3) & 1;
+    if (P <= 4) return K == 4 ? half + 2 * row + 4 * bank + 8 * side : K == 2 ? half + 2 * row + 4 * bank : half + 2 * row;
+    return P == 8 ? half + 2 * row + 4 * side + 8 * j : half + 2 * row + 4 * j;
 }
 #ifdef HOSTMODEL
-inline float rows_sum(const float (&v)[kK]) { return v[0]; }
-template <int P>
-inline void row_sums(const float (&q)[4], float (&out)[kSums<P>]) {
+inline float rows_sum(const float* v) { return v[0]; }
+template <int K, int P>
+inline void row_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
     for (float& o : out) o = q[0];
 }
 #else
@@ -44,7 +43,6 @@ __device__ __forceinline__ float swap16_add(float u, float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float rows_sum(const float (&v)[kK]) { return swap16_add(swap32_add(v[0], v[1]), swap32_add(v[2], v[3])); }
 // v in the banks (4 lanes each) of MASK, u in the others
 template <int MASK>
 __device__ __forceinline__ float by_bank(float u, float v) {
@@ -56,20 +54,22 @@ __device__ __forceinline__ float pair_sum(float u, float v) {
     const float other = by_bank<MASK>(v, u);
     return by_bank<MASK>(u, v) + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(other), CTRL, 0xf, 0xf, true));
 }
-template <int P>
-__device__ __forceinline__ void row_sums(const float (&q)[4], float (&out)[kSums<P>]) {
+// four values over the rows of the wave
+__device__ __forceinline__ float rows_sum(const float* v) { return swap16_add(swap32_add(v[0], v[1]), swap32_add(v[2], v[3])); }
+// K of those over the channels within a row
+template <int K, int P>
+__device__ __forceinline__ void row_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
+    // row_ror:4 pairs every bank with the one before it, row_ror:8 with the one after the next: all four in two steps
     if constexpr (P <= 4) {
-        // row_ror:4 pairs every bank with the one before it, row_ror:8 with the one after the next: all four in two steps
-        float s = pair_sum<0x128, 0xC>(pair_sum<0x124, 0xA>(q[0], q[1]), pair_sum<0x124, 0xA>(q[2], q[3]));
-        if constexpr (P <= 2) s = add_dpp<0x4E>(s);
-        if constexpr (P <= 1) s = add_dpp<0xB1>(s);
-        out[0] = s;
+        if constexpr (K == 4) out[0] = pair_sum<0x128, 0xC>(pair_sum<0x124, 0xA>(q[0], q[1]), pair_sum<0x124, 0xA>(q[2], q[3]));
+        if constexpr (K == 2) out[0] = add_dpp<0x128>(pair_sum<0x124, 0xA>(q[0], q[1]));
+        if constexpr (K == 1) out[0] = add_dpp<0x128>(add_dpp<0x124>(q[0]));
     } else if constexpr (P == 8) {
-        out[0] = pair_sum<0x128, 0xC>(q[0], q[2]);
-        out[1] = pair_sum<0x128, 0xC>(q[1], q[3]);
+#pragma unroll
+        for (int i = 0; i < K / 2; ++i) out[i] = pair_sum<0x128, 0xC>(q[2 * i], q[2 * i + 1]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = q[i];
+        for (int i = 0; i < K; ++i) out[i] = q[i];
     }
 }
 #endif
@@ -140,9 +140,9 @@ struct Rows {
 };
 
 // what a segment sends into the one before it, from nothing sent into itself, and the sum of its steps
-template <bool BF16, int P>
+template <bool BF16, int K, int P>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = scan_tile(P);
+    constexpr int SP = K * P, T = scan_tile(P);
     using R = ScanRows<P, T>;
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sY[kScanWaves][R::CW * R::RS];  // e and dy
     __shared__ __align__(16) float sC[T * SP];
@@ -155,16 +155,16 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
     const Rows<BF16, P, T> rows(a, at, base, lane);
-    float rate[kK], carry[kK], sum = 0.f;
+    float rate[K], carry[K], sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < kK; ++k) {
-        rate[k] = scan_rate(a, d, kK * p + k, there);
+    for (int k = 0; k < K; ++k) {
+        rate[k] = scan_rate(a, d, K * p + k, there);
         carry[k] = 0.f;
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
         rows.template stage<false>(a, lane, t0, len, t0 + T <= len && full, sE[wave], nullptr, sY[wave]);
-        scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
         const float *e_row = sE[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
 #pragma unroll 1
@@ -176,10 +176,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t + j);
 #pragma unroll
                 for (int i = 3; i >= 0; --i) {
-                    const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    const States<K> o = states_at<K>(sC + (t + j + i) * SP + K * p);
                     part += e[i];
 #pragma unroll
-                    for (int k = 0; k < kK; ++k) carry[k] = exp2_hw(e[i] * rate[k]) * fmaf(o[k], dy[i], carry[k]);
+                    for (int k = 0; k < K; ++k) carry[k] = exp2_hw(e[i] * rate[k]) * fmaf(o[k], dy[i], carry[k]);
                 }
             }
             sum += part;
@@ -188,13 +188,13 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     }
     if (!there) return;
     const long i = (at.n * a.nseg + at.seg) * a.D + d;
-    *reinterpret_cast<scan_f32x4*>(a.carries + i * SP + kK * p) = scan_f32x4{carry[0], carry[1], carry[2], carry[3]};
+    put_states<K>(a.carries + i * SP + K * p, carry);
     if (p == 0) a.sums[i] = sum;
 }
 
-template <bool BF16, int P>
+template <bool BF16, int K, int P>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = scan_tile_back(P);
+    constexpr int SP = K * P, T = scan_tile_back(P);
     using R = ScanRows<P, T>;
     using E = typename RowElem<BF16>::type;
     // e, x and dy of a step; the walk back leaves sum_s e g B, de and sum_s C h in their places
@@ -209,10 +209,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
     const Rows<BF16, P, T> rows(a, at, base, lane);
-    float rate[kK], carry[kK], dA[kK], dskip[R::PASSES], dbias[R::PASSES];
+    float rate[K], carry[K], dA[K], dskip[R::PASSES], dbias[R::PASSES];
 #pragma unroll
-    for (int k = 0; k < kK; ++k) {
-        const int s = kK * p + k;
+    for (int k = 0; k < K; ++k) {
+        const int s = K * p + k;
         rate[k] = scan_rate(a, d, s, there);
         dA[k] = 0.f;
         carry[k] = 0.f;
@@ -225,21 +225,21 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
         const bool inside = t0 + T <= len && full;
         rows.template stage<true>(a, lane, t0, len, inside, sE[wave], sX[wave], sY[wave]);
-        scan_stage_states<BF16, P, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
+        scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
-        float dA_tile[kK] = {0.f, 0.f, 0.f, 0.f};
+        float dA_tile[K] = {};
         float *e_row = sE[wave] + cl * R::RS, *x_row = sX[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
 #pragma unroll 1
         for (int t = T - kSub; t >= 0; t -= kSub) {
             if (t0 + t >= a.L) continue;
-            float first[kK], h[kSub][kK], decay[kSub][kK];
+            float first[K], h[kSub][K], decay[kSub][K];
 #pragma unroll
-            for (int k = 0; k < kK; ++k) first[k] = 0.f;
+            for (int k = 0; k < K; ++k) first[k] = 0.f;
             if (there) {
-                const scan_f32x4 v = *reinterpret_cast<const scan_f32x4*>(a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + kK * p);
+                const States<K> v = states_at<K>(a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + K * p);
 #pragma unroll
-                for (int k = 0; k < kK; ++k) first[k] = v[k];
+                for (int k = 0; k < K; ++k) first[k] = v[k];
             }
 #pragma unroll
             for (int j = 0; j < kSub; j += 4) {
@@ -247,10 +247,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
+                    const States<K> b = states_at<K>(sB + (t + j + i) * SP + K * p);
                     const float ex = e[i] * x[i];
 #pragma unroll
-                    for (int k = 0; k < kK; ++k) {
+                    for (int k = 0; k < K; ++k) {
                         decay[j + i][k] = exp2_hw(e[i] * rate[k]);
                         h[j + i][k] = fmaf(decay[j + i][k], j + i ? h[j + i - (j + i ? 1 : 0)][k] : first[k], ex * b[k]);
                     }
@@ -263,19 +263,19 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j),
                                  dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t + j);
                 scan_f32x4 out_x, out_e, out_y;
-                float qB[4], qC[4];
+                float vB[4 * K], vC[4 * K], qB[K], qC[K];
 #pragma unroll
                 for (int i = 3; i >= 0; --i) {
-                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
-                    const scan_f32x4 o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    const States<K> b = states_at<K>(sB + (t + j + i) * SP + K * p);
+                    const States<K> o = states_at<K>(sC + (t + j + i) * SP + K * p);
                     const float ex = e[i] * x[i];
-                    float gb = 0.f, qa = 0.f, y = 0.f, vB[kK], vC[kK];
+                    float gb = 0.f, qa = 0.f, y = 0.f;
 #pragma unroll
-                    for (int k = 0; k < kK; ++k) {
+                    for (int k = 0; k < K; ++k) {
                         const float g = fmaf(o[k], dy[i], carry[k]);
                         y = k ? fmaf(o[k], h[j + i][k], y) : o[k] * h[j + i][k];
-                        vC[k] = dy[i] * h[j + i][k];
-                        vB[k] = g * ex;
+                        vC[K * i + k] = dy[i] * h[j + i][k];
+                        vB[K * i + k] = g * ex;
                         gb = k ? fmaf(g, b[k], gb) : g * b[k];
                         carry[k] = g * decay[j + i][k];
                         const float kept = carry[k] * (j + i ? h[j + i - (j + i ? 1 : 0)][k] : first[k]);
@@ -287,15 +287,17 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     out_y[i] = channel_sum<P>(y);
                     out_x[i] = gb * e[i];
                     out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
-                    qB[i] = rows_sum(vB);
-                    qC[i] = rows_sum(vC);
+                    if (K * i % 4 == 0) {  // four values are there
+                        qB[K * i / 4] = rows_sum(vB + K * i);
+                        qC[K * i / 4] = rows_sum(vC + K * i);
+                    }
                 }
-                float out_B[kSums<P>], out_C[kSums<P>];
-                row_sums<P>(qB, out_B);
-                row_sums<P>(qC, out_C);
+                float out_B[kSums<K, P>], out_C[kSums<K, P>];
+                row_sums<K, P>(qB, out_B);
+                row_sums<K, P>(qC, out_C);
 #pragma unroll
-                for (int i = 0; i < kSums<P>; ++i) {
-                    const int to = (kK * p + sum_state(lane)) * R::RS + t + j + sum_step<P>(lane, i);
+                for (int i = 0; i < kSums<K, P>; ++i) {
+                    const int value = sum_value<K, P>(lane, i), to = (K * p + value % K) * R::RS + t + j + value / K;
                     red[wave][0][to] = out_B[i];
                     red[wave][1][to] = out_C[i];
                 }
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             }
         }
 #pragma unroll
-        for (int k = 0; k < kK; ++k) dA[k] += dA_tile[k];
+        for (int k = 0; k < K; ++k) dA[k] += dA_tile[k];
         __syncthreads();
         // dB and dC over the waves of the workgroup, 4 steps of a state each
         for (int i = threadIdx.x; i < 2 * SP * (T / 4); i += blockDim.x) {
@@ -389,11 +391,12 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         part[static_cast<long>(a.D) * (SP + 1) + rows.d[q]] = dbias[q];
     }
     if (!there) return;
-    *reinterpret_cast<seq_f32x4*>(part + d * SP + kK * p) = seq_f32x4{dA[0], dA[1], dA[2], dA[3]};
+#pragma unroll
+    for (int k = 0; k < K; ++k) part[d * SP + K * p + k] = dA[k];
     if (a.dinit && at.seg == 0) {
 #pragma unroll
-        for (int k = 0; k < kK; ++k)
-            if (kK * p + k < a.S) a.dinit[(at.n * a.D + d) * a.S + kK * p + k] = carry[k];
+        for (int k = 0; k < K; ++k)
+            if (K * p + k < a.S) a.dinit[(at.n * a.D + d) * a.S + K * p + k] = carry[k];
     }
 }
 
@@ -451,20 +454,20 @@ __global__ __launch_bounds__(kCols* kShares) void scan_sums_kernel(SumArgs a) {
     }
 }
 
-template <bool BF16, int P>
+template <bool BF16, int K, int P>
 hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, float* dA, float* dskip, float* dbias, hipStream_t st) {
     const dim3 block(static_cast<unsigned>(p.waves * kSeqWave));
     const long most = kSeqMostThreads / block.x, blocks = scan_blocks(a);
     for (int stage = p.nseg > 1 ? 0 : 2; stage < 3; ++stage) {
         if (stage == 1) {
-            const hipError_t e = scan_join_launch<true>(a.carries, a.sums, a.dfinal, a.A, a.N, a.D, a.S, kK * P, a.nseg, st);
+            const hipError_t e = scan_join_launch<true>(a.carries, a.sums, a.dfinal, a.A, a.N, a.D, a.S, K * P, a.nseg, st);
             if (e != hipSuccess) return e;
             continue;
         }
         for (a.first = 0; a.first < blocks; a.first += most) {
             const long left = blocks - a.first;
             const dim3 grid(static_cast<unsigned>(left < most ? left : most));
-            const hipError_t e = launch_kernel(stage == 0 ? scan_adjoint_kernel<BF16, P> : scan_bwd_kernel<BF16, P>, grid, block, 0, st, a);
+            const hipError_t e = launch_kernel(stage == 0 ? scan_adjoint_kernel<BF16, K, P> : scan_bwd_kernel<BF16, K, P>, grid, block, 0, st, a);
             if (e != hipSuccess) return e;
         }
     }
@@ -473,7 +476,7 @@ hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, float* dA, float* dskip, fl
     u.dA = dA; u.dskip = dskip; u.dbias = dbias; u.dB = a.dB; u.dC = a.dC;
     u.rows = static_cast<long>(a.N) * a.nseg;
     u.n = static_cast<long>(a.N) * a.G * a.S * a.L;
-    u.D = a.D; u.S = a.S; u.SP = kK * P; u.blocks_d = p.blocks_d;
+    u.D = a.D; u.S = a.S; u.SP = K * P; u.blocks_d = p.blocks_d;
     u.param_blocks = cdiv(static_cast<long>(a.D) * (u.SP + 2), kCols);
     const long sum_blocks = u.param_blocks + (p.blocks_d > 1 ? (2 * ((u.n + 7) / 8) + kCols * kShares - 1) / (kCols * kShares) : 0);
     constexpr long most_sums = kSeqMostThreads / (kCols * kShares);
@@ -487,12 +490,12 @@ hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, float* dA, float* dskip, fl
 
 template <bool BF16>
 hipError_t bwd_type(const ScanArgs& a, const ScanPlan& p, float* dA, float* dskip, float* dbias, hipStream_t st) {
-    switch (p.P) {
-        case 1: return bwd_launch<BF16, 1>(a, p, dA, dskip, dbias, st);
-        case 2: return bwd_launch<BF16, 2>(a, p, dA, dskip, dbias, st);
-        case 4: return bwd_launch<BF16, 4>(a, p, dA, dskip, dbias, st);
-        case 8: return bwd_launch<BF16, 8>(a, p, dA, dskip, dbias, st);
-        default: return bwd_launch<BF16, 16>(a, p, dA, dskip, dbias, st);
+    switch (p.K * p.P) {
+        case 4: return bwd_launch<BF16, 1, 4>(a, p, dA, dskip, dbias, st);
+        case 8: return bwd_launch<BF16, 2, 4>(a, p, dA, dskip, dbias, st);
+        case 16: return bwd_launch<BF16, 4, 4>(a, p, dA, dskip, dbias, st);
+        case 32: return bwd_launch<BF16, 4, 8>(a, p, dA, dskip, dbias, st);
+        default: return bwd_launch<BF16, 4, 16>(a, p, dA, dskip, dbias, st);
     }
 }
 

@@ -10,9 +10,9 @@ namespace {
 constexpr int kThreads = 256;
 
 // ENDS: no output but the state each segment adds and the sum of its steps.
-template <bool BF16, int P, bool ENDS>
+template <bool BF16, int K, int P, bool ENDS>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanArgs a) {
-    constexpr int SP = kK * P, T = scan_tile(P);
+    constexpr int SP = K * P, T = scan_tile(P);
     using R = ScanRows<P, T>;
     using E = typename RowElem<BF16>::type;
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS];  // e (then y) and e x
@@ -26,10 +26,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
 
-    float rate[kK], h[kK];
+    float rate[K], h[K];
 #pragma unroll
-    for (int k = 0; k < kK; ++k) {
-        const int s = kK * p + k;
+    for (int k = 0; k < K; ++k) {
+        const int s = K * p + k;
         rate[k] = scan_rate(a, d, s, there);
         h[k] = 0.f;
         if (ENDS) continue;
@@ -82,16 +82,16 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
             lds_put8(sE[wave] + row * R::RS + c, e);
             lds_put8(sX[wave] + row * R::RS + c, x);
         }
-        scan_stage_states<BF16, P, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        if (!ENDS) scan_stage_states<BF16, P, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
+        if (!ENDS) scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
         float* e_row = sE[wave] + cl * R::RS;
         const float* ex_row = sX[wave] + cl * R::RS;
 #pragma unroll 1
         for (int t = 0; t < T; t += kSub) {
             if (!ENDS && a.saved && there && t0 + t < a.L) {
-                float* to = a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + kK * p;
-                *reinterpret_cast<scan_f32x4*>(to) = scan_f32x4{h[0], h[1], h[2], h[3]};
+                float* to = a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + K * p;
+                put_states<K>(to, h);
             }
             float part = 0.f;
 #pragma unroll
@@ -100,12 +100,12 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
                 scan_f32x4 y;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const scan_f32x4 b = *reinterpret_cast<const scan_f32x4*>(sB + (t + j + i) * SP + kK * p);
-                    scan_f32x4 o;
-                    if (!ENDS) o = *reinterpret_cast<const scan_f32x4*>(sC + (t + j + i) * SP + kK * p);
+                    const States<K> b = states_at<K>(sB + (t + j + i) * SP + K * p);
+                    States<K> o;
+                    if (!ENDS) o = states_at<K>(sC + (t + j + i) * SP + K * p);
                     float v = 0.f;
 #pragma unroll
-                    for (int k = 0; k < kK; ++k) {
+                    for (int k = 0; k < K; ++k) {
                         h[k] = fmaf(exp2_hw(e[i] * rate[k]), h[k], ex[i] * b[k]);
                         if (!ENDS) v = k ? fmaf(o[k], h[k], v) : o[k] * h[k];
                     }
@@ -145,14 +145,16 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     if (!there) return;
     if (ENDS) {
         const long i = (at.n * a.nseg + at.seg) * a.D + d;
-        *reinterpret_cast<scan_f32x4*>(a.starts + i * SP + kK * p) = scan_f32x4{h[0], h[1], h[2], h[3]};
+        put_states<K>(a.starts + i * SP + K * p, h);
         if (p == 0) a.sums[i] = sum;
     } else if (a.final && at.seg == a.nseg - 1) {
 #pragma unroll
-        for (int k = 0; k < kK; ++k)
-            if (kK * p + k < a.S) a.final[(at.n * a.D + d) * a.S + kK * p + k] = h[k];
+        for (int k = 0; k < K; ++k)
+            if (K * p + k < a.S) a.final[(at.n * a.D + d) * a.S + K * p + k] = h[k];
     }
 }
+
+constexpr int kK = 4;  // states of a lane in the step
 
 struct ScanStepArgs {
     const void *x, *dt, *B, *C, *z;
@@ -206,20 +208,20 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(ScanStepArgs a) {
     store_elem<BF16>(a.out, n * a.out_sn + d, y);
 }
 
-template <bool BF16, int P>
+template <bool BF16, int K, int P>
 hipError_t fwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
     const dim3 block(static_cast<unsigned>(p.waves * kSeqWave));
     const long most = kSeqMostThreads / block.x, blocks = scan_blocks(a);
     for (int stage = p.nseg > 1 ? 0 : 2; stage < 3; ++stage) {
         if (stage == 1) {
-            const hipError_t e = scan_join_launch<false>(a.starts, a.sums, a.init, a.A, a.N, a.D, a.S, kK * P, a.nseg, st);
+            const hipError_t e = scan_join_launch<false>(a.starts, a.sums, a.init, a.A, a.N, a.D, a.S, K * P, a.nseg, st);
             if (e != hipSuccess) return e;
             continue;
         }
         for (a.first = 0; a.first < blocks; a.first += most) {
             const long left = blocks - a.first;
             const dim3 grid(static_cast<unsigned>(left < most ? left : most));
-            const hipError_t e = launch_kernel(stage == 0 ? scan_fwd_kernel<BF16, P, true> : scan_fwd_kernel<BF16, P, false>, grid, block, 0, st, a);
+            const hipError_t e = launch_kernel(stage == 0 ? scan_fwd_kernel<BF16, K, P, true> : scan_fwd_kernel<BF16, K, P, false>, grid, block, 0, st, a);
             if (e != hipSuccess) return e;
         }
     }
@@ -237,10 +239,18 @@ hipError_t step_launch(ScanStepArgs a, hipStream_t st) {
     return hipSuccess;
 }
 
+// lanes of a channel in the step, of 4 states each
 int lanes_of(int S) {
     int P = 1;
     while (kK * P < S) P *= 2;
     return P;
+}
+
+// states of a channel in the scan, with the padding
+int padded_states(int S) {
+    int SP = 4;
+    while (SP < S) SP *= 2;
+    return SP;
 }
 
 bool scan_ok(const conv1d_scan_t* p) {
@@ -278,7 +288,7 @@ size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 // the states and the sums of a split sequence
 size_t split_bytes(int N, int D, const ScanPlan& p) {
     const size_t rows = static_cast<size_t>(N) * p.nseg * D;
-    return p.nseg > 1 ? round256(rows * kK * p.P * sizeof(float)) + round256(rows * sizeof(float)) : 0;
+    return p.nseg > 1 ? round256(rows * p.K * p.P * sizeof(float)) + round256(rows * sizeof(float)) : 0;
 }
 
 // where the parts of a backward call's workspace begin
@@ -289,9 +299,9 @@ BwdSpace bwd_space(int N, int D, int L, int S, int G, const ScanPlan& p) {
     const size_t rows = static_cast<size_t>(N) * p.nseg * D;
     BwdSpace w{};
     w.carries = 0;
-    w.sums = w.carries + (p.nseg > 1 ? round256(rows * kK * p.P * sizeof(float)) : 0);
+    w.sums = w.carries + (p.nseg > 1 ? round256(rows * p.K * p.P * sizeof(float)) : 0);
     w.params = w.sums + (p.nseg > 1 ? round256(rows * sizeof(float)) : 0);
-    w.bc = w.params + round256(rows * (kK * p.P + 2) * sizeof(float));
+    w.bc = w.params + round256(rows * (p.K * p.P + 2) * sizeof(float));
     w.total = w.bc + (p.blocks_d > 1 ? round256(2 * sizeof(float) * static_cast<size_t>(p.blocks_d) * N * G * S * L) : 0);
     return w;
 }
@@ -305,7 +315,9 @@ int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; 
 // few rows want short segments: N = 3, D = 49, L = 4999, S = 5 in FP32 takes 18 us backwards in segments of 16 steps, 39 in 128.
 ScanPlan scan_plan(int N, int D, int L, int S, int G) {
     ScanPlan p{};
-    p.P = lanes_of(S);
+    const int SP = padded_states(S);
+    p.K = SP < 16 ? SP / 4 : 4;
+    p.P = SP / p.K;
     const int CW = kSeqWave / p.P, Dg = D / G;
     const int need = cdiv(Dg, CW);
     p.waves = need < kScanWaves ? need : kScanWaves;
@@ -323,12 +335,12 @@ ScanPlan scan_plan(int N, int D, int L, int S, int G) {
 }
 
 hipError_t scan_fwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, hipStream_t st) {
-    switch (p.P) {
-        case 1: return bf16 ? fwd_launch<true, 1>(a, p, st) : fwd_launch<false, 1>(a, p, st);
-        case 2: return bf16 ? fwd_launch<true, 2>(a, p, st) : fwd_launch<false, 2>(a, p, st);
-        case 4: return bf16 ? fwd_launch<true, 4>(a, p, st) : fwd_launch<false, 4>(a, p, st);
-        case 8: return bf16 ? fwd_launch<true, 8>(a, p, st) : fwd_launch<false, 8>(a, p, st);
-        default: return bf16 ? fwd_launch<true, 16>(a, p, st) : fwd_launch<false, 16>(a, p, st);
+    switch (p.K * p.P) {
+        case 4: return bf16 ? fwd_launch<true, 1, 4>(a, p, st) : fwd_launch<false, 1, 4>(a, p, st);
+        case 8: return bf16 ? fwd_launch<true, 2, 4>(a, p, st) : fwd_launch<false, 2, 4>(a, p, st);
+        case 16: return bf16 ? fwd_launch<true, 4, 4>(a, p, st) : fwd_launch<false, 4, 4>(a, p, st);
+        case 32: return bf16 ? fwd_launch<true, 4, 8>(a, p, st) : fwd_launch<false, 4, 8>(a, p, st);
+        default: return bf16 ? fwd_launch<true, 4, 16>(a, p, st) : fwd_launch<false, 4, 16>(a, p, st);
     }
 }
 
@@ -345,7 +357,7 @@ size_t conv1d_scan_fwd_workspace_bytes(int N, int D, int L, int S, int G) {
 
 size_t conv1d_scan_saved_bytes(int N, int D, int L, int S) {
     if (N < 1 || D < 1 || L < 1 || S < 1 || S > kMostStates) return 0;
-    return sizeof(float) * N * static_cast<size_t>(cdiv(L, kSub)) * D * kK * lanes_of(S);
+    return sizeof(float) * N * static_cast<size_t>(cdiv(L, kSub)) * D * padded_states(S);
 }
 
 int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float* final, void* saved, void* workspace,
@@ -361,7 +373,7 @@ int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float
     a.out = y; a.out_sn = y_sn; a.out_sd = y_sd; a.final = final; a.saved = static_cast<float*>(saved);
     if (need) {
         a.starts = static_cast<float*>(workspace);
-        a.sums = a.starts + round256(static_cast<size_t>(p->N) * plan.nseg * p->D * kK * plan.P * sizeof(float)) / sizeof(float);
+        a.sums = a.starts + round256(static_cast<size_t>(p->N) * plan.nseg * p->D * plan.K * plan.P * sizeof(float)) / sizeof(float);
     }
     return status_of(scan_fwd_launch(a, plan, p->dtype == CONV1D_BF16, static_cast<hipStream_t>(stream)));
 }
