@@ -152,6 +152,12 @@ struct ScanRows {
     static constexpr int RS = scan_stride(T);
 };
 
+template <bool BF16, bool INSIDE>
+__device__ __forceinline__ void scan_load8(const void* row, int t, int end, float (&v)[8]) {
+    if constexpr (INSIDE) row_load8_inside<BF16>(row, t, v);
+    else row_load8<BF16>(row, t, end, v);
+}
+
 __device__ __forceinline__ void lds_put8(float* to, const float (&v)[8]) {
     *reinterpret_cast<scan_f32x4*>(to) = scan_f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<scan_f32x4*>(to + 4) = scan_f32x4{v[4], v[5], v[6], v[7]};

@@ -99,42 +99,86 @@ struct Rows {
             bias[q] = a.dt_bias ? a.dt_bias[d[q]] : 0.f;
         }
     }
-    __device__ __forceinline__ static void load(const E* row, int t, bool inside, int end, float (&v)[8]) {
-        if (inside) row_load8_inside<BF16>(row, t, v);
-        else row_load8<BF16>(row, t, end, v);
-    }
-    // e, dy and (WITH_X) x of the tile at t0 into LDS
-    template <bool WITH_X>
-    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, bool inside, float* sE, float* sX, float* sY) const {
+    // e, dy and (WITH_X) x of the tile at t0 into LDS.  INSIDE: it lies within the sequence, the wave's channels are all there.
+    template <bool INSIDE, bool WITH_X>
+    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, float* sE, float* sX, float* sY) const {
 #pragma unroll
         for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
+            const int row = q * R::RPP + lane / R::LPR, end = real[q] ? len : 0;
             if (row >= R::CW) continue;
-            const int end = real[q] ? len : 0;
             float v[8], g[8], u[8];
-            load(dt[q], t0 + c, inside, end, v);
-            load(dout[q], t0 + c, inside, end, g);
-            if (a.z) load(z[q], t0 + c, inside, end, u);
+            scan_load8<BF16, INSIDE>(dt[q], t0 + c, end, v);
+            scan_load8<BF16, INSIDE>(dout[q], t0 + c, end, g);
+            if (a.z) {
+                scan_load8<BF16, INSIDE>(z[q], t0 + c, end, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= u[i] * sigmoid_of(u[i]);
+            }
+            if (WITH_X) {
+                scan_load8<BF16, INSIDE>(x[q], t0 + c, end, u);
+                lds_put8(sX + row * R::RS + c, u);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += bias[q];
             if (a.softplus) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = softplus_of(v[i]);
             }
-            if (!inside) {
+            if (!INSIDE) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < end ? v[i] : 0.f;
             }
-            if (a.z) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] *= u[i] * sigmoid_of(u[i]);
-            }
             lds_put8(sE + row * R::RS + c, v);
             lds_put8(sY + row * R::RS + c, g);
-            if (WITH_X) {
-                load(x[q], t0 + c, inside, end, u);
-                lds_put8(sX + row * R::RS + c, u);
+        }
+    }
+    // the gradients of x, dt and z from what the walk back left in LDS
+    template <bool INSIDE>
+    __device__ __forceinline__ void finish(const ScanArgs& a, const ScanPlace& at, int lane, int t0, int len, const float* sE, const float* sX,
+                                           const float* sY, float (&dskip)[R::PASSES], float (&dbias)[R::PASSES]) const {
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            if (!real[q] || t0 + c >= a.L) continue;
+            const long o = (at.n * a.D + d[q]) * a.L;
+            const float skip = a.skip ? a.skip[d[q]] : 0.f;
+            float u[8], v[8], g[8];
+            scan_load8<BF16, INSIDE>(x[q], t0 + c, len, u);
+            scan_load8<BF16, INSIDE>(dout[q], t0 + c, len, g);
+            if (a.z) {
+                float w[8], y[8];
+                scan_load8<BF16, INSIDE>(z[q], t0 + c, len, w);
+                lds_get8(sY + row * R::RS + c, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float sig = sigmoid_of(w[i]), zs = w[i] * sig;
+                    y[i] = g[i] * fmaf(skip, u[i], y[i]) * fmaf(zs, 1.f - sig, sig);
+                    g[i] *= zs;
+                    if (!INSIDE) y[i] = t0 + c + i < len ? y[i] : 0.f;
+                }
+                row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, a.L, y);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dskip[q] = fmaf(g[i], u[i], dskip[q]);
+            lds_get8(sE + row * R::RS + c, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                g[i] = fmaf(skip, g[i], u[i]);
+                if (!INSIDE) g[i] = t0 + c + i < len ? g[i] : 0.f;
+            }
+            row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, a.L, g);
+            lds_get8(sX + row * R::RS + c, u);
+            if (a.softplus) {
+                scan_load8<BF16, INSIDE>(dt[q], t0 + c, len, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] *= sigmoid_of(v[i] + bias[q]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!INSIDE) u[i] = t0 + c + i < len ? u[i] : 0.f;
+                dbias[q] += u[i];
+            }
+            row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, a.L, u);
         }
     }
 };
@@ -148,7 +192,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     __shared__ __align__(16) float sC[T * SP];
     const ScanPlace at = scan_place(a);
     if (at.seg == 0) return;
-    const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & (kSeqWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
     const int len = seq_length(a.lengths, at.n, a.L);
     const int base = (at.cb * waves + wave) * R::CW;
@@ -163,7 +207,8 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
-        rows.template stage<false>(a, lane, t0, len, t0 + T <= len && full, sE[wave], nullptr, sY[wave]);
+        if (t0 + T <= len && full) rows.template stage<true, false>(a, lane, t0, len, sE[wave], nullptr, sY[wave]);
+        else rows.template stage<false, false>(a, lane, t0, len, sE[wave], nullptr, sY[wave]);
         scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
         const float *e_row = sE[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
@@ -202,7 +247,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     __shared__ __align__(16) float sB[T * SP], sC[T * SP];
     __shared__ __align__(16) float red[kScanWaves][2][SP * R::RS];  // dB and dC of the wave's channels, [state][step]
     const ScanPlace at = scan_place(a);
-    const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & (kSeqWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
     const int len = seq_length(a.lengths, at.n, a.L);
     const int base = (at.cb * waves + wave) * R::CW;
@@ -224,7 +269,8 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
         const bool inside = t0 + T <= len && full;
-        rows.template stage<true>(a, lane, t0, len, inside, sE[wave], sX[wave], sY[wave]);
+        if (inside) rows.template stage<true, true>(a, lane, t0, len, sE[wave], sX[wave], sY[wave]);
+        else rows.template stage<false, true>(a, lane, t0, len, sE[wave], sX[wave], sY[wave]);
         scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
         scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
@@ -284,7 +330,11 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     }
                     gb = channel_sum<P>(gb);
                     qa = channel_sum<P>(qa);
-                    out_y[i] = channel_sum<P>(y);
+                    y = channel_sum<P>(y);
+                    keep_here(gb);
+                    keep_here(qa);
+                    keep_here(y);
+                    out_y[i] = y;
                     out_x[i] = gb * e[i];
                     out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
                     if (K * i % 4 == 0) {  // four values are there
@@ -333,49 +383,8 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     if (t + e < a.L) store_elem<BF16>(which ? a.dC : a.dB, o + e, v[e]);
             }
         }
-        // rows again: the gradients of x, dt and z
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int r = q * R::RPP + lane / R::LPR, c = rows.c;
-            if (!rows.real[q] || t0 + c >= a.L) continue;
-            const long o = (at.n * a.D + rows.d[q]) * a.L;
-            const float skip = a.skip ? a.skip[rows.d[q]] : 0.f;
-            float x[8], v[8], dout[8], dx[8], ddt[8];
-            rows.load(rows.x[q], t0 + c, inside, len, x);
-            rows.load(rows.dout[q], t0 + c, inside, len, dout);
-            if (a.z) {
-                float z[8], y[8];
-                rows.load(rows.z[q], t0 + c, inside, len, z);
-                lds_get8(sY[wave] + r * R::RS + c, y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float sig = sigmoid_of(z[i]);
-                    y[i] = dout[i] * fmaf(skip, x[i], y[i]) * (sig * fmaf(z[i], 1.f - sig, 1.f));
-                    dout[i] *= z[i] * sig;
-                    if (!inside) y[i] = t0 + c + i < len ? y[i] : 0.f;
-                }
-                row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, a.L, y);
-            }
-            lds_get8(sE[wave] + r * R::RS + c, dx);
-            lds_get8(sX[wave] + r * R::RS + c, ddt);
-            if (a.softplus) {
-                rows.load(rows.dt[q], t0 + c, inside, len, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ddt[i] *= sigmoid_of(v[i] + rows.bias[q]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                dx[i] = fmaf(skip, dout[i], dx[i]);
-                if (!inside) {
-                    dx[i] = t0 + c + i < len ? dx[i] : 0.f;
-                    ddt[i] = t0 + c + i < len ? ddt[i] : 0.f;
-                }
-                dskip[q] = fmaf(dout[i], x[i], dskip[q]);
-                dbias[q] += ddt[i];
-            }
-            row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, a.L, dx);
-            row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, a.L, ddt);
-        }
+        if (inside) rows.template finish<true>(a, at, lane, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
+        else rows.template finish<false>(a, at, lane, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
         // (the next tile's barrier stands between these reads of `red` and its next values)
     }
     float* part = a.part_p + (at.n * a.nseg + at.seg) * (static_cast<long>(a.D) * (SP + 2));

@@ -9,6 +9,81 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// The lane's rows of a tile.  INSIDE: the tile lies within the sequence, the wave's channels are all there: no masks.
+template <bool BF16, int P, int T>
+struct FwdRows {
+    using R = ScanRows<P, T>;
+    using E = typename RowElem<BF16>::type;
+    const E *x[R::PASSES], *dt[R::PASSES];
+    float bias[R::PASSES], skip[R::PASSES];
+    bool real[R::PASSES];
+    long d[R::PASSES];
+    int c;
+
+    __device__ __forceinline__ FwdRows(const ScanArgs& a, const ScanPlace& at, int base, int lane) {
+        c = 8 * (lane % R::LPR);
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            real[q] = row < R::CW && base + row < a.Dg;
+            d[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
+            x[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, d[q]);
+            dt[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, d[q]);
+            bias[q] = a.dt_bias ? a.dt_bias[d[q]] : 0.f;
+            skip[q] = a.skip ? a.skip[d[q]] : 0.f;
+        }
+    }
+    // e and e x into LDS
+    template <bool INSIDE>
+    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, float* sE, float* sX) const {
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR, end = real[q] ? len : 0;
+            if (row >= R::CW) continue;
+            float v[8], e[8];
+            scan_load8<BF16, INSIDE>(x[q], t0 + c, end, v);
+            scan_load8<BF16, INSIDE>(dt[q], t0 + c, end, e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] += bias[q];
+            if (a.softplus) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!INSIDE) e[i] = t0 + c + i < end ? e[i] : 0.f;
+                v[i] *= e[i];
+            }
+            lds_put8(sE + row * R::RS + c, e);
+            lds_put8(sX + row * R::RS + c, v);
+        }
+    }
+    // the output from the sums in LDS
+    template <bool INSIDE>
+    __device__ __forceinline__ void finish(const ScanArgs& a, const ScanPlace& at, int lane, int t0, int len, const float* sY) const {
+#pragma unroll
+        for (int q = 0; q < R::PASSES; ++q) {
+            const int row = q * R::RPP + lane / R::LPR;
+            if (!real[q] || t0 + c >= a.L) continue;
+            float v[8], z[8], y[8];
+            lds_get8(sY + row * R::RS + c, y);
+            scan_load8<BF16, INSIDE>(x[q], t0 + c, len, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(skip[q], v[i], y[i]);
+            if (a.z) {
+                scan_load8<BF16, INSIDE>(scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, d[q]), t0 + c, len, z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] *= z[i] * sigmoid_of(z[i]);
+            }
+            if (!INSIDE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
+            }
+            row_store8<BF16>(const_cast<E*>(scan_row<BF16>(a.out, a.out_sn, a.out_sd, at.n, d[q])), t0 + c, a.L, y);
+        }
+    }
+};
+
 // ENDS: no output but the state each segment adds and the sum of its steps.
 template <bool BF16, int K, int P, bool ENDS>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanArgs a) {
@@ -19,7 +94,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     __shared__ __align__(16) float sB[T * SP], sC[ENDS ? 4 : T * SP];
     const ScanPlace at = scan_place(a);
     if (ENDS && at.seg == a.nseg - 1) return;             // nothing comes behind the last segment
-    const int lane = threadIdx.x & (kSeqWave - 1), wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int lane = threadIdx.x & (kSeqWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int p = lane & (P - 1), cl = lane / P;
     const int len = seq_length(a.lengths, at.n, a.L);
     const int base = (at.cb * waves + wave) * R::CW;      // first channel of the wave, within its group
@@ -36,52 +111,13 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
         if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
         else if (a.init && there && s < a.S) h[k] = a.init[(at.n * a.D + d) * a.S + s];
     }
-    const int c = 8 * (lane % R::LPR);
-    const E *x_row[R::PASSES], *dt_row[R::PASSES];
-    float bias[R::PASSES], skip[R::PASSES];
-    bool real[R::PASSES];
-    long dr[R::PASSES];
-#pragma unroll
-    for (int q = 0; q < R::PASSES; ++q) {
-        const int row = q * R::RPP + lane / R::LPR;
-        real[q] = row < R::CW && base + row < a.Dg;
-        dr[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
-        x_row[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, dr[q]);
-        dt_row[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, dr[q]);
-        bias[q] = a.dt_bias ? a.dt_bias[dr[q]] : 0.f;
-        skip[q] = a.skip ? a.skip[dr[q]] : 0.f;
-    }
+    const FwdRows<BF16, P, T> rows(a, at, base, lane);
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     float sum = 0.f;
     for (int t0 = t_begin; t0 < t_end; t0 += T) {
         const bool inside = t0 + T <= len && full;        // of the whole wave: no masks
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            if (row >= R::CW) continue;
-            float x[8], e[8];
-            if (inside) {
-                row_load8_inside<BF16>(x_row[q], t0 + c, x);
-                row_load8_inside<BF16>(dt_row[q], t0 + c, e);
-            } else {
-                row_load8<BF16>(x_row[q], t0 + c, real[q] ? len : 0, x);
-                row_load8<BF16>(dt_row[q], t0 + c, real[q] ? len : 0, e);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] += bias[q];
-            if (a.softplus) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
-            }
-            if (!inside) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = real[q] && t0 + c + i < len ? e[i] : 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] *= e[i];
-            lds_put8(sE[wave] + row * R::RS + c, e);
-            lds_put8(sX[wave] + row * R::RS + c, x);
-        }
+        if (inside) rows.template stage<true>(a, lane, t0, len, sE[wave], sX[wave]);
+        else rows.template stage<false>(a, lane, t0, len, sE[wave], sX[wave]);
         scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
         if (!ENDS) scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
         __syncthreads();
@@ -97,7 +133,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
 #pragma unroll
             for (int j = 0; j < kSub; j += 4) {
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), ex = *reinterpret_cast<const scan_f32x4*>(ex_row + t + j);
-                scan_f32x4 y;
+                float y[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const States<K> b = states_at<K>(sB + (t + j + i) * SP + K * p);
@@ -109,38 +145,21 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
                         h[k] = fmaf(exp2_hw(e[i] * rate[k]), h[k], ex[i] * b[k]);
                         if (!ENDS) v = k ? fmaf(o[k], h[k], v) : o[k] * h[k];
                     }
-                    if (ENDS) part += e[i];
-                    else y[i] = channel_sum<P>(v);
+                    if (ENDS) {
+                        part += e[i];
+                    } else {
+                        y[i] = channel_sum<P>(v);
+                        keep_here(y[i]);
+                    }
                 }
-                if (!ENDS && p == 0) *reinterpret_cast<scan_f32x4*>(e_row + t + j) = y;
+                if (!ENDS && p == 0) *reinterpret_cast<scan_f32x4*>(e_row + t + j) = scan_f32x4{y[0], y[1], y[2], y[3]};
             }
             sum += part;
         }
         __syncthreads();
         if (ENDS) continue;
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            if (!real[q] || t0 + c >= a.L) continue;
-            float x[8], z[8], y[8];
-            lds_get8(sE[wave] + row * R::RS + c, y);
-            if (inside) row_load8_inside<BF16>(x_row[q], t0 + c, x);
-            else row_load8<BF16>(x_row[q], t0 + c, len, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = fmaf(skip[q], x[i], y[i]);
-            if (a.z) {
-                const E* z_row = scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, dr[q]);
-                if (inside) row_load8_inside<BF16>(z_row, t0 + c, z);
-                else row_load8<BF16>(z_row, t0 + c, len, z);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] *= z[i] * sigmoid_of(z[i]);
-            }
-            if (!inside) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
-            }
-            row_store8<BF16>(const_cast<E*>(scan_row<BF16>(a.out, a.out_sn, a.out_sd, at.n, dr[q])), t0 + c, a.L, y);
-        }
+        if (inside) rows.template finish<true>(a, at, lane, t0, len, sE[wave]);
+        else rows.template finish<false>(a, at, lane, t0, len, sE[wave]);
     }
     if (!there) return;
     if (ENDS) {

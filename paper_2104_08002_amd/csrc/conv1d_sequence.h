@@ -19,19 +19,23 @@ inline float lane_xor(float v, int) { return v; }
 inline double lane_xor(double v, int) { return v; }
 inline float exp2_hw(float v) { return std::exp2(v); }
 inline float rcp_hw(float v) { return 1.f / v; }
-inline void wave_sync() {}
+inline void keep_here(float&) {}
 #else
 __device__ __forceinline__ float lane_xor(float v, int mask) { return __shfl_xor(v, mask, kSeqWave); }
 __device__ __forceinline__ double lane_xor(double v, int mask) { return __shfl_xor(v, mask, kSeqWave); }
 // 2^v and 1 / v to one unit in the last place
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float rcp_hw(float v) { return __builtin_amdgcn_rcpf(v); }
+// The value is found here and not behind a later branch, away from the lane exchange that is one instruction with its addition.
+__device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
 #endif
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
 // A row is contiguous along the sequence and begins at any element: vectors are loaded at the alignment of an element,
 // which the memory path takes at full rate but for the lines that a vector straddles.
 typedef __attribute__((ext_vector_type(8), aligned(2))) unsigned short seq_u16x8;
+typedef __attribute__((ext_vector_type(8), aligned(2))) __bf16 seq_bf16x8;
+typedef __attribute__((ext_vector_type(8))) float seq_f32x8;
 typedef __attribute__((ext_vector_type(4), aligned(4))) float seq_f32x4;
 
 template <bool BF16>
@@ -91,12 +95,10 @@ __device__ __forceinline__ void row_load8(const void* row, I at, I end, float (&
 template <bool BF16>
 __device__ __forceinline__ void row_store8(void* row, long at, long end, const float (&v)[8]) {
     if constexpr (BF16) {
-        seq_u16x8 t;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = float_to_bf16(v[e]);
-        unsigned short* o = static_cast<unsigned short*>(row) + at;
+        const seq_bf16x8 t = __builtin_convertvector((seq_f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}), seq_bf16x8);
+        __bf16* o = static_cast<__bf16*>(row) + at;
         if (at + 8 <= end) {
-            *reinterpret_cast<seq_u16x8*>(o) = t;
+            *reinterpret_cast<seq_bf16x8*>(o) = t;
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -140,7 +142,7 @@ __device__ __forceinline__ float softplus_of(float v) {
     f = fmaf(f, q, 0.40024909377098083f);
     f = fmaf(f, q, 0.6666631698608398f);
     f = fmaf(f, q, 2.f);
-    return fmaf(f, r, fmaxf(v, 0.f));  // (a NaN comes through f r)
+    return fmaf(f, r, __builtin_amdgcn_fmed3f(v, 0.f, INFINITY));  // (max(v, 0); a NaN comes through f r)
 }
 
 }  // namespace conv1d
