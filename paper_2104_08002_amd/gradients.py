@@ -34,19 +34,18 @@ class _Tensors:
             grads = [grads]
         self.grads = grads = [g for g in grads if g is not None]
         n = len(grads)
-        if n:
-            device = grads[0].device
-            for g in grads:
-                if g.dtype not in _CODES:
-                    raise TypeError(f"unsupported dtype {g.dtype}")
-                if g.device != device or not g.is_cuda:
-                    raise ValueError("the gradients must be on one device")
-                if not _dense(g):
-                    raise ValueError("a gradient has gaps between its elements, or elements in one place")
-        self.device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
-        self.data = (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads])
-        self.counts = (ctypes.c_size_t * n)(*[g.numel() for g in grads])
-        self.dtypes = (ctypes.c_int * n)(*[_CODES[g.dtype] for g in grads])
+        devices = {g.device for g in grads} or {torch.device("cuda", torch.cuda.current_device())}
+        self.device = devices.pop()
+        if devices or self.device.type != "cuda":
+            raise ValueError("the gradients must be on one device")
+        codes = [_CODES.get(g.dtype) for g in grads]
+        if None in codes:
+            raise TypeError(f"unsupported dtype {grads[codes.index(None)].dtype}")
+        if not all(map(torch.Tensor.is_contiguous, grads)) and not all(map(_dense, grads)):
+            raise ValueError("a gradient has gaps between its elements, or elements in one place")
+        self.data = (ctypes.c_void_p * n)(*map(torch.Tensor.data_ptr, grads))
+        self.counts = (ctypes.c_size_t * n)(*map(torch.Tensor.numel, grads))
+        self.dtypes = (ctypes.c_int * n)(*codes)
         self.args = (self.data, self.counts, self.dtypes, n)
 
     def norm(self, norm_type, workspace):
@@ -69,8 +68,10 @@ def _run(grads, stream, fn):
             raise ValueError("the stream belongs to another device than the gradients")
         with torch.cuda.stream(stream):
             return fn(t)
-    with torch.cuda.device(t.device):
-        return fn(t)
+    if t.device.index != torch._C._cuda_getDevice():
+        with torch.cuda.device(t.device):
+            return fn(t)
+    return fn(t)
 
 
 def conv1d_grad_norm(grads, norm_type: float = 2.0, workspace=None, stream=None):

@@ -47,6 +47,9 @@ class ScanGrads(NamedTuple):
     dinit: Optional[torch.Tensor]
 
 
+_device_now = torch._C._cuda_getDevice
+
+
 def _on_device(fn):
     """Runs fn with the device of its first argument current and, if asked for, on `stream`."""
     name = fn.__code__.co_varnames[0]
@@ -54,15 +57,16 @@ def _on_device(fn):
     @functools.wraps(fn)
     def call(*args, stream=None, **kw):
         t = args[0] if args else kw[name]
-        if not t.is_cuda:
+        device = t.device
+        if device.type != "cuda":
             raise ValueError("the tensors must be on the device")
         if stream is not None:
-            if stream.device != t.device:
+            if stream.device != device:
                 raise ValueError("the stream belongs to another device than the tensors")
             with torch.cuda.stream(stream):
                 return fn(*args, **kw)
-        if t.device.index != torch._C._cuda_getDevice():
-            with torch.cuda.device(t.device):
+        if device.index != _device_now():
+            with torch.cuda.device(device):
                 return fn(*args, **kw)
         return fn(*args, **kw)
 
@@ -73,16 +77,28 @@ def _rows(t, name, shape, dtype, device):
     """A tensor of that shape whose last axis is contiguous."""
     if t.shape != shape or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device}: got {t.dtype} {list(t.shape)} on {t.device}")
-    if shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous along its last axis")
     return t
 
 
 def _whole(t, name, shape, dtype, device):
-    _rows(t, name, shape, dtype, device)
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        _rows(t, name, shape, dtype, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
+
+
+def _like(x):
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
+def _output(out, x, ins):
+    """The caller's `out`, checked, or a new tensor as x."""
+    if out is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
+    return _apart(_spread(_rows(out, "out", x.shape, x.dtype, x.device), "out"), ins)
 
 
 def _ptr(t):
@@ -118,17 +134,16 @@ def _apart(out, ins):
 def _causal(x, w, bias, silu, init, lengths, step=False):
     if x.dim() != (2 if step else 3) or 0 in x.shape:
         raise ValueError(f"x must have the shape {'[N, C]' if step else '[N, C, L]'}, none of it 0")
-    N, C = x.shape[:2]
-    L = 1 if step else x.shape[2]
+    N, C, L = (*x.shape, 1) if step else x.shape
     if w.dim() != 2 or w.shape[0] != C or w.shape[1] < 1:
         raise ValueError("w must have the shape [C, S]")
-    S, dev, code = w.shape[1], x.device, binding._dtype_code(x)
-    _rows(x, "x", x.shape, x.dtype, dev)
-    _whole(w, "w", (C, S), x.dtype, dev)
+    S, dev, t, code = w.shape[1], x.device, x.dtype, binding._dtype_code(x)
+    _rows(x, "x", x.shape, t, dev)
+    _whole(w, "w", (C, S), t, dev)
     if bias is not None:
         _whole(bias, "bias", (C,), torch.float32, dev)
     if init is not None:
-        _whole(init, "init", (N, C, S - 1), x.dtype, dev)
+        _whole(init, "init", (N, C, S - 1), t, dev)
     if lengths is not None:
         _whole(lengths, "lengths", (N,), torch.int32, dev)
     return _Causal(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(init), _ptr(lengths), x.stride(0), 0 if step else x.stride(1), N, C, L, S, code,
@@ -143,9 +158,7 @@ def conv1d_causal_fwd(x, w, bias=None, silu: bool = False, init=None, lengths=No
     lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there.
     """
     p = _causal(x, w, bias, silu, init, lengths)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
-    if out is not None:
-        _apart(out, (x, w, bias, init, lengths))
+    y = _output(out, x, (x, w, bias, init, lengths))
     final = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=x.device) if want_final else None
     binding._check(binding.load().conv1d_causal_fwd(ctypes.byref(p), y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), binding._current_stream()))
     return (y, final) if want_final else y
@@ -162,7 +175,7 @@ def conv1d_causal_bwd(dy, x, w, bias=None, silu: bool = False, init=None, length
     lib = binding.load()
     if workspace is None:
         workspace = torch.empty(max(lib.conv1d_causal_bwd_workspace_bytes(p.N, p.C, p.L, p.S), 4), dtype=torch.uint8, device=dev)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=dev)
+    dx = _like(x)
     dw = torch.empty((p.C, p.S), dtype=torch.float32, device=dev)
     db = None if bias is None else torch.empty(p.C, dtype=torch.float32, device=dev)
     di = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=dev) if want_init else None
@@ -178,9 +191,7 @@ def conv1d_causal_step(x, w, state, bias=None, silu: bool = False, out=None):
     moved on by that position."""
     p = _causal(x, w, bias, silu, None, None, step=True)
     _whole(state, "state", (p.N, p.C, p.S - 1), x.dtype, x.device)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
-    if out is not None:
-        _apart(out, (x, w, bias, state))
+    y = _output(out, x, (x, w, bias, state))
     binding._check(binding.load().conv1d_causal_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
     return y
 
@@ -189,8 +200,8 @@ def conv1d_causal_step(x, w, state, bias=None, silu: bool = False, out=None):
 def _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths, step=False):
     if x.dim() != (2 if step else 3) or 0 in x.shape:
         raise ValueError(f"x must have the shape {'[N, D]' if step else '[N, D, L]'}, none of it 0")
-    N, D = x.shape[:2]
-    L = 1 if step else x.shape[2]
+    shape = x.shape
+    N, D, L = (*shape, 1) if step else shape
     if A.dim() != 2 or A.shape[0] != D or A.shape[1] < 1:
         raise ValueError("A must have the shape [D, S]")
     S, dev, t, code = A.shape[1], x.device, x.dtype, binding._dtype_code(x)
@@ -198,15 +209,15 @@ def _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths, step=False)
         raise ValueError(f"B must have the shape {'[N, G, S]' if step else '[N, G, S, L]'}, G a divisor of D")
     G = B.shape[1]
     states = (N, G, S) if step else (N, G, S, L)
-    _rows(x, "x", x.shape, t, dev)
-    _rows(dt, "dt", x.shape, t, dev)
+    _rows(x, "x", shape, t, dev)
+    _rows(dt, "dt", shape, t, dev)
     _whole(A, "A", (D, S), torch.float32, dev)
     _rows(B, "B", states, t, dev)
     _rows(C, "C", states, t, dev)
     if skip is not None:
         _whole(skip, "skip", (D,), torch.float32, dev)
     if z is not None:
-        _rows(z, "z", x.shape, t, dev)
+        _rows(z, "z", shape, t, dev)
     if dt_bias is not None:
         _whole(dt_bias, "dt_bias", (D,), torch.float32, dev)
     if init is not None:
@@ -236,9 +247,7 @@ def conv1d_scan_fwd(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: b
     """
     p, dev = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device
     lib = binding.load()
-    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, dev), "out")
-    if out is not None:
-        _apart(out, (x, dt, A, B, C, skip, z, dt_bias, init, lengths))
+    y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, init, lengths))
     final = torch.empty((p.N, p.D, p.S), dtype=torch.float32, device=dev) if want_final else None
     saved = _scratch(lib.conv1d_scan_saved_bytes(p.N, p.D, p.L, p.S), dev) if save else None
     if workspace is None:
@@ -262,15 +271,8 @@ def conv1d_scan_bwd(dy, saved, x, dt, A, B, C, skip=None, z=None, dt_bias=None, 
     if workspace is None:
         workspace = _scratch(lib.conv1d_scan_bwd_workspace_bytes(p.N, p.D, p.L, p.S, p.G), dev)
 
-    def rows():
-        return torch.empty(x.shape, dtype=t, device=dev)
-
-    def floats(*shape):
-        return torch.empty(shape, dtype=torch.float32, device=dev)
-
-    g = ScanGrads(rows(), rows(), floats(p.D, p.S), torch.empty(B.shape, dtype=t, device=dev), torch.empty(C.shape, dtype=t, device=dev),
-                  None if skip is None else floats(p.D), None if z is None else rows(), None if dt_bias is None else floats(p.D),
-                  floats(p.N, p.D, p.S) if want_init else None)
+    g = ScanGrads(_like(x), _like(x), _like(A), _like(B), _like(C), None if skip is None else _like(skip), None if z is None else _like(x),
+                  None if dt_bias is None else _like(dt_bias), torch.empty((p.N, p.D, p.S), dtype=torch.float32, device=dev) if want_init else None)
     binding._check(lib.conv1d_scan_bwd(ctypes.byref(p), dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), saved.data_ptr(), *map(_ptr, g),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                        binding._current_stream()))
@@ -283,8 +285,6 @@ def conv1d_scan_step(x, dt, A, B, C, state, skip=None, z=None, dt_bias=None, sof
     leaves it in `final`, is moved on by that position."""
     p = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, None, None, step=True)
     _whole(state, "state", (p.N, p.D, p.S), torch.float32, x.device)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _spread(_rows(out, "out", x.shape, x.dtype, x.device), "out")
-    if out is not None:
-        _apart(out, (x, dt, A, B, C, skip, z, dt_bias, state))
+    y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, state))
     binding._check(binding.load().conv1d_scan_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
     return y
