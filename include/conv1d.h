@@ -275,7 +275,7 @@ const char* conv1d_status_string(int status);
  *     alone, and parameters' gradients.
  * Sums over samples and positions are added in a fixed order. */
 
-/* Depthwise causal convolution, S <= 8 taps (more: CONV1D_EUNSUPPORTED):
+/* Depthwise causal convolution, S <= 8 taps, L <= 2^30 (more: CONV1D_EUNSUPPORTED):
  *   p[n][c][t] = bias[c] + sum_{s<S} w[c][s] * xe[n][c][t + s],  xe = the S - 1 inputs before the sequence, then x
  *   y = p, or p * sigmoid(p) with CONV1D_CAUSAL_SILU. */
 #define CONV1D_CAUSAL_SILU 1

@@ -34,7 +34,7 @@ struct CausalArgs {
     long first, units;     // first unit of the launch, and all of them: N * C * pieces
 };
 
-// A piece of a row belongs to 2^lg lanes, which take R steps of kV outputs each through it.
+// A piece of a row belongs to 2^lg lanes, which take one step (backwards: R) of kV outputs each through it.
 struct Piece {
     long n, c, unit;
     int piece, sub;        // which of the row, lane within it
@@ -53,14 +53,17 @@ __device__ __forceinline__ Piece piece_of(const CausalArgs& a) {
     return p;
 }
 
-// xe[at] .. xe[at + 7 + S - 1] for outputs at .. at + 7: the row's elements at - (S - 1) .. at + 7
-template <bool BF16, int S>
-__device__ __forceinline__ void load_window(const CausalArgs& a, const Piece& p, const void* row, long at, long len, float (&v)[kV + S - 1]) {
+// xe[at] .. xe[at + 7 + S - 1] for outputs at .. at + 7: the row's elements at - (S - 1) .. at + 7.  INSIDE: they are all there.
+template <bool BF16, int S, bool INSIDE>
+__device__ __forceinline__ void load_window(const CausalArgs& a, const Piece& p, const void* row, int at, int len, float (&v)[kV + S - 1]) {
     float cur[kV], before[kV];
-    row_load8<BF16>(row, at, len, cur);
-    if (S > 1) {
-        row_load8<BF16>(row, at - kV, len, before);
-        if (at == 0 && a.init) {
+    if constexpr (INSIDE) {
+        row_load8_inside<BF16>(row, at, cur);
+        if (S > 1) row_load8_inside<BF16>(row, at - kV, before);
+    } else {
+        row_load8<BF16>(row, at, len, cur);
+        if (S > 1) row_load8<BF16>(row, at - kV, len, before);
+        if (S > 1 && at == 0 && a.init) {
 #pragma unroll
             for (int s = 0; s < S - 1; ++s) before[kV - (S - 1) + s] = load_elem<BF16>(a.init, (p.n * a.C + p.c) * (S - 1) + s);
         }
@@ -71,11 +74,36 @@ __device__ __forceinline__ void load_window(const CausalArgs& a, const Piece& p,
     for (int e = 0; e < kV; ++e) v[S - 1 + e] = cur[e];
 }
 
-template <bool BF16, int S, int R>
+template <bool BF16, int S, bool INSIDE>
+__device__ __forceinline__ void forward_step(const CausalArgs& a, const Piece& p, const typename RowElem<BF16>::type* x,
+                                             typename RowElem<BF16>::type* y, int t, int len, const float (&w)[S], float bias) {
+    float v[kV + S - 1], o[kV];
+    load_window<BF16, S, INSIDE>(a, p, x, t, len, v);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+        o[e] = bias;
+#pragma unroll
+        for (int s = 0; s < S; ++s) o[e] = fmaf(w[s], v[e + s], o[e]);
+    }
+    if (a.silu) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) o[e] *= sigmoid_of(o[e]);
+    }
+    if constexpr (!INSIDE) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) o[e] = t + e < len ? o[e] : 0.f;
+        if (p.there && t < a.L) row_store8<BF16>(y, t, a.L, o);
+    } else {
+        row_store8<BF16>(y, t, t + kV, o);
+    }
+}
+
+// One step a lane: waves enough hide the loads, more steps in flight only take registers (N = 8, C = 128, L = 20000, S = 4 in
+// bfloat16: 16 us, 5.1 TB/s, what a large copy reaches).
+template <bool BF16, int S>
 __global__ __launch_bounds__(kThreads) void causal_fwd_kernel(CausalArgs a) {
     const Piece p = piece_of(a);
-    if (!p.there) return;
-    const long len = seq_length(a.lengths, p.n, a.L);
+    const int len = p.there ? seq_length(a.lengths, p.n, a.L) : 0;
     using T = typename RowElem<BF16>::type;
     const T* x = static_cast<const T*>(a.x) + p.n * a.x_sn + p.c * a.x_sc;
     T* y = static_cast<T*>(a.y) + p.n * a.y_sn + p.c * a.y_sc;
@@ -83,29 +111,14 @@ __global__ __launch_bounds__(kThreads) void causal_fwd_kernel(CausalArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) w[s] = load_elem<BF16>(a.w, p.c * S + s);
     const float bias = a.bias ? a.bias[p.c] : 0.f;
-    const long step = static_cast<long>(kV) << a.lg, t0 = p.piece * step * R + p.sub * kV;
-    float v[R][kV + S - 1];
-#pragma unroll
-    for (int r = 0; r < R; ++r) load_window<BF16, S>(a, p, x, t0 + r * step, len, v[r]);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const long t = t0 + r * step;
-        float o[kV];
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-            float s0 = bias;
-#pragma unroll
-            for (int s = 0; s < S; ++s) s0 = fmaf(w[s], v[r][e + s], s0);
-            if (a.silu) s0 *= sigmoid_of(s0);
-            o[e] = t + e < len ? s0 : 0.f;
-        }
-        if (t < a.L) row_store8<BF16>(y, t, a.L, o);
-    }
-    if (S > 1 && a.final && p.piece == 0 && p.sub == 0) {
+    const int t = ((p.piece << a.lg) + p.sub) * kV;
+    if (wave_all(t > 0 && t + kV <= len)) forward_step<BF16, S, true>(a, p, x, y, t, len, w, bias);
+    else forward_step<BF16, S, false>(a, p, x, y, t, len, w, bias);
+    if (S > 1 && a.final && p.there && t == 0) {
         const long at = (p.n * a.C + p.c) * (S - 1);
 #pragma unroll
         for (int s = 0; s < S - 1; ++s) {
-            const long j = len + s;  // xe[j]
+            const int j = len + s;  // xe[j]
             float e = 0.f;
             if (j >= S - 1) e = load_elem<BF16>(x, j - (S - 1));
             else if (a.init) e = load_elem<BF16>(a.init, at + j);
@@ -114,11 +127,87 @@ __global__ __launch_bounds__(kThreads) void causal_fwd_kernel(CausalArgs a) {
     }
 }
 
-// The gradients of x at t .. t + 7 need dp up to t + 7 + S - 1: a lane computes the S - 1 of its neighbour again.
+// act'(p) for p from the S inputs at v
+template <int S>
+__device__ __forceinline__ float slope_of(const float* v, const float (&w)[S], float bias) {
+    float q = bias;
+#pragma unroll
+    for (int s = 0; s < S; ++s) q = fmaf(w[s], v[s], q);
+    const float sig = sigmoid_of(q);
+    return fmaf(q * sig, 1.f - sig, sig);
+}
+
+// One step of a lane backwards: positions t .. t + 7.  behind: dp of the S - 1 positions behind the wave's step; those of its first
+// positions come back in it.
+template <bool BF16, int S, bool INSIDE>
+__device__ __forceinline__ void backward_step(const CausalArgs& a, const Piece& p, const typename RowElem<BF16>::type* x,
+                                              const typename RowElem<BF16>::type* dy, typename RowElem<BF16>::type* dx, int t, int len,
+                                              const float (&w)[S], float bias, float (&behind)[S > 1 ? S - 1 : 1], float (&sum)[S + 1]) {
+    float v[kV + S - 1], dp[kV + (S > 1 ? S - 1 : 1)], g[kV], o[kV];
+    load_window<BF16, S, INSIDE>(a, p, x, t, len, v);
+    if constexpr (INSIDE) row_load8_inside<BF16>(dy, t, g);
+    else row_load8<BF16>(dy, t, len, g);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) dp[e] = g[e];
+    if (a.silu) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) dp[e] *= slope_of<S>(v + e, w, bias);
+    }
+    if constexpr (!INSIDE) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) dp[e] = t + e < len ? dp[e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) {
+        const float next = lane_next(dp[i]);
+        dp[kV + i] = p.sub != (1 << a.lg) - 1 ? next : behind[i];
+        behind[i] = a.lg == 6 ? lane_first(dp[i]) : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+        o[e] = w[0] * dp[e + S - 1];
+#pragma unroll
+        for (int s = 1; s < S; ++s) o[e] = fmaf(w[s], dp[e + S - 1 - s], o[e]);
+    }
+    if constexpr (!INSIDE) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) o[e] = t + e < len ? o[e] : 0.f;
+    }
+    const long state = (p.n * a.C + p.c) * (S - 1);
+    if (S > 1 && a.dfinal && t + kV + (S - 1) > len && t < len) {
+#pragma unroll
+        for (int e = 0; e < kV; ++e) {
+            const int f = t + e + (S - 1) - len;  // x[j] is element j + S - 1 - len of the final state
+            if (f >= 0 && f < S - 1) o[e] += load_elem<BF16>(a.dfinal, state + f);
+        }
+    }
+    if constexpr (INSIDE) row_store8<BF16>(dx, t, t + kV, o);
+    else if (p.there && t < a.L) row_store8<BF16>(dx, t, a.L, o);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) sum[s] = fmaf(dp[e], v[e + s], sum[s]);
+        sum[S] += dp[e];
+    }
+    if (!INSIDE && S > 1 && t == 0 && a.dinit && p.there) {
+#pragma unroll
+        for (int j = 0; j < S - 1; ++j) {
+            float d = 0.f;
+#pragma unroll
+            for (int s = 0; s <= j; ++s) d = fmaf(w[s], dp[j - s], d);
+            if (a.dfinal && j >= len) d += load_elem<BF16>(a.dfinal, state + j - len);
+            store_elem<BF16>(a.dinit, state + j, d);
+        }
+    }
+}
+
+// The gradients of x at t .. t + 7 need dp up to t + 7 + S - 1: the next lane has them.  A piece is taken from its end, so that
+// the last lane of a wave finds them in the step before (in the first one, all lanes compute those behind the piece).
 template <bool BF16, int S, int R>
 __global__ __launch_bounds__(kThreads) void causal_bwd_kernel(CausalArgs a) {
+    constexpr int H = S > 1 ? S - 1 : 1;
     const Piece p = piece_of(a);
-    const long len = p.there ? seq_length(a.lengths, p.n, a.L) : 0;
+    const int len = p.there ? seq_length(a.lengths, p.n, a.L) : 0;
     using T = typename RowElem<BF16>::type;
     const T* x = static_cast<const T*>(a.x) + p.n * a.x_sn + p.c * a.x_sc;
     const T* dy = static_cast<const T*>(a.dy) + p.n * a.dy_sn + p.c * a.dy_sc;
@@ -127,66 +216,23 @@ __global__ __launch_bounds__(kThreads) void causal_bwd_kernel(CausalArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) w[s] = load_elem<BF16>(a.w, p.c * S + s);
     const float bias = a.bias ? a.bias[p.c] : 0.f;
-    const long state = (p.n * a.C + p.c) * (S - 1);
-    const long step = static_cast<long>(kV) << a.lg, t0 = p.piece * step * R + p.sub * kV;
+    const int step = kV << a.lg, begin = p.piece * step * R, end = begin + step * R;
+    float behind[H] = {};  // dp of the S - 1 positions behind the wave's step
+    if (S > 1 && a.lg == 6 && end < len) {
+        float u[2 * H];
+#pragma unroll
+        for (int i = 0; i < 2 * (S - 1); ++i) u[i] = end - (S - 1) + i < len ? load_elem<BF16>(x, end - (S - 1) + i) : 0.f;
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (end + i < len) behind[i] = load_elem<BF16>(dy, end + i) * (a.silu ? slope_of<S>(u + i, w, bias) : 1.f);
+    }
     float sum[S + 1];
 #pragma unroll
     for (int s = 0; s <= S; ++s) sum[s] = 0.f;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const long t = t0 + r * step;
-        if (!p.there || t >= a.L) continue;
-        float v[kV + S - 1], later[kV], g[kV], g2[kV];
-        load_window<BF16, S>(a, p, x, t, len, v);
-        row_load8<BF16>(dy, t, len, g);
-        if (S > 1) {
-            row_load8<BF16>(x, t + kV, len, later);
-            row_load8<BF16>(dy, t + kV, len, g2);
-        }
-        float dp[kV + S - 1];
-#pragma unroll
-        for (int e = 0; e < kV + S - 1; ++e) {
-            const float gy = e < kV ? g[e] : g2[e - kV];
-            float slope = 1.f;
-            if (a.silu) {
-                float q = bias;
-#pragma unroll
-                for (int s = 0; s < S; ++s) q = fmaf(w[s], e + s < kV + S - 1 ? v[e + s] : later[e + s - (kV + S - 1)], q);
-                const float sig = sigmoid_of(q);
-                slope = sig * fmaf(q, 1.f - sig, 1.f);
-            }
-            // (a position behind the end may hold anything: its product is not taken)
-            dp[e] = t + e < len ? gy * slope : 0.f;
-        }
-        float o[kV];
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-            float d = 0.f;
-#pragma unroll
-            for (int s = 0; s < S; ++s) d = fmaf(w[s], dp[e + S - 1 - s], d);
-            if (S > 1 && a.dfinal) {
-                const long f = t + e + (S - 1) - len;  // x[j] is element j + S - 1 - len of the final state
-                if (f >= 0 && f < S - 1 && t + e < len) d += load_elem<BF16>(a.dfinal, state + f);
-            }
-            o[e] = t + e < len ? d : 0.f;
-        }
-        row_store8<BF16>(dx, t, a.L, o);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) sum[s] = fmaf(dp[e], v[e + s], sum[s]);
-            sum[S] += dp[e];
-        }
-        if (S > 1 && t == 0 && a.dinit) {
-#pragma unroll
-            for (int j = 0; j < S - 1; ++j) {
-                float d = 0.f;
-#pragma unroll
-                for (int s = 0; s <= j; ++s) d = fmaf(w[s], dp[j - s], d);
-                if (a.dfinal && j >= len) d += load_elem<BF16>(a.dfinal, state + j - len);
-                store_elem<BF16>(a.dinit, state + j, d);
-            }
-        }
+#pragma unroll 1
+    for (int t = begin + (R - 1) * step + p.sub * kV; t >= begin; t -= step) {
+        if (wave_all(t > 0 && t + kV <= len)) backward_step<BF16, S, true>(a, p, x, dy, dx, t, len, w, bias, behind, sum);
+        else backward_step<BF16, S, false>(a, p, x, dy, dx, t, len, w, bias, behind, sum);
     }
     if (!a.partial) return;
     for (int m = 1; m < (1 << a.lg); m <<= 1) {
@@ -257,16 +303,20 @@ Cut cut_of(int L, int R) {
     return c;
 }
 
-// Steps of a lane: several loads in flight where that leaves enough waves for the chip.
-int steps_of(long rows, int L) {
-    const Cut c = cut_of(L, 4);
-    return c.pieces > 1 && rows * c.pieces >= 4096 ? 4 : 1;
+// Steps of a lane backwards: the more, the less is computed twice behind a piece and added up behind the launch, as long as 4096
+// waves are left for the chip (N = 8, C = 128, L = 20000, S = 4 in bfloat16: 45, 28 and 27 us with 1, 4 and 8; N = 12, C = 49,
+// L = 4999, S = 3 in FP32: 9.0, 10.2 and 14 us).
+int back_steps(long rows, int L) {
+    for (int R : {8, 4}) {
+        const Cut c = cut_of(L, R);
+        if (c.lg == 6 && rows * c.pieces >= 4096) return R;
+    }
+    return 1;
 }
 
 template <bool BF16, int S>
 hipError_t launch_taps(bool bwd, CausalArgs& a, int R, hipStream_t st) {
-    auto kern = bwd ? (R == 4 ? causal_bwd_kernel<BF16, S, 4> : causal_bwd_kernel<BF16, S, 1>)
-                    : (R == 4 ? causal_fwd_kernel<BF16, S, 4> : causal_fwd_kernel<BF16, S, 1>);
+    auto kern = !bwd ? causal_fwd_kernel<BF16, S> : R == 8 ? causal_bwd_kernel<BF16, S, 8> : R == 4 ? causal_bwd_kernel<BF16, S, 4> : causal_bwd_kernel<BF16, S, 1>;
     const long most = kSeqMostThreads >> a.lg;
     for (a.first = 0; a.first < a.units; a.first += most) {
         const long left = a.units - a.first, units = left < most ? left : most;
@@ -325,7 +375,7 @@ bool layout_ok(const conv1d_causal_t* p) {
 
 // rows are counted in 31 bits (units of a launch too: a piece has a row's share of at least kV elements)
 bool sizes_ok(const conv1d_causal_t* p) {
-    return p->S <= kMostTaps && static_cast<long>(p->N) * p->C <= 0x7fffffffL && static_cast<long>(p->C) * (p->S + 1) <= 0x7fffffffL;
+    return p->S <= kMostTaps && p->L <= 1 << 30 && static_cast<long>(p->N) * p->C <= 0x7fffffffL && static_cast<long>(p->C) * (p->S + 1) <= 0x7fffffffL;
 }
 
 CausalArgs args_of(const conv1d_causal_t* p, int R) {
@@ -354,16 +404,15 @@ int conv1d_causal_fwd(const conv1d_causal_t* p, void* y, long y_sn, long y_sc, v
     const size_t size = p->dtype == CONV1D_BF16 ? 2 : 4;
     if (!seq_aligned(y, size) || !seq_aligned(final, size)) return CONV1D_EINVAL;
     if (!sizes_ok(p)) return CONV1D_EUNSUPPORTED;
-    const int R = steps_of(static_cast<long>(p->N) * p->C, p->L);
-    CausalArgs a = args_of(p, R);
+    CausalArgs a = args_of(p, 1);
     a.y = y; a.y_sn = y_sn; a.y_sc = y_sc; a.final = final;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return status_of(p->dtype == CONV1D_BF16 ? launch_type<true>(false, a, p->S, R, st) : launch_type<false>(false, a, p->S, R, st));
+    return status_of(p->dtype == CONV1D_BF16 ? launch_type<true>(false, a, p->S, 1, st) : launch_type<false>(false, a, p->S, 1, st));
 }
 
 size_t conv1d_causal_bwd_workspace_bytes(int N, int C, int L, int S) {
     if (N < 1 || C < 1 || L < 1 || S < 1 || S > kMostTaps) return 0;
-    const Cut cut = cut_of(L, steps_of(static_cast<long>(N) * C, L));
+    const Cut cut = cut_of(L, back_steps(static_cast<long>(N) * C, L));
     return sizeof(float) * static_cast<size_t>(C) * (S + 1) * N * cut.pieces;
 }
 
@@ -376,7 +425,7 @@ int conv1d_causal_bwd(const conv1d_causal_t* p, const void* dy, long dy_sn, long
         return CONV1D_EINVAL;
     if (!sizes_ok(p)) return CONV1D_EUNSUPPORTED;
     if (dw && (!workspace || workspace_bytes < conv1d_causal_bwd_workspace_bytes(p->N, p->C, p->L, p->S))) return CONV1D_EWORKSPACE;
-    const int R = steps_of(static_cast<long>(p->N) * p->C, p->L);
+    const int R = back_steps(static_cast<long>(p->N) * p->C, p->L);
     CausalArgs a = args_of(p, R);
     a.dy = dy; a.dy_sn = dy_sn; a.dy_sc = dy_sc; a.dfinal = dfinal; a.dx = dx; a.dinit = dinit;
     a.partial = dw ? static_cast<float*>(workspace) : nullptr;

@@ -20,6 +20,9 @@ inline double lane_xor(double v, int) { return v; }
 inline float exp2_hw(float v) { return std::exp2(v); }
 inline float rcp_hw(float v) { return 1.f / v; }
 inline void keep_here(float&) {}
+inline float lane_next(float v) { return v; }
+inline bool wave_all(bool v) { return v; }
+inline float lane_first(float v) { return v; }
 #else
 __device__ __forceinline__ float lane_xor(float v, int mask) { return __shfl_xor(v, mask, kSeqWave); }
 __device__ __forceinline__ double lane_xor(double v, int mask) { return __shfl_xor(v, mask, kSeqWave); }
@@ -28,6 +31,12 @@ __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float rcp_hw(float v) { return __builtin_amdgcn_rcpf(v); }
 // The value is found here and not behind a later branch, away from the lane exchange that is one instruction with its addition.
 __device__ __forceinline__ void keep_here(float& v) { asm volatile("" : "+v"(v)); }
+// v of the next lane (0 in the last), of the first lane
+__device__ __forceinline__ float lane_next(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x130, 0xf, 0xf, true));  // wave_shl:1
+}
+__device__ __forceinline__ bool wave_all(bool v) { return __all(v); }
+__device__ __forceinline__ float lane_first(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 #endif
 
 // ---- rows -----------------------------------------------------------------------------------------------------------
