@@ -58,25 +58,43 @@ __device__ __forceinline__ double block_value(double v, double* lds) {
     return v;
 }
 
+constexpr int kAtOnce = 4;  // steps whose loads a lane has in flight
+
 template <bool BF16, bool MAX>
-__device__ __forceinline__ double piece_value(const Job& j) {
-    double acc = 0.0;
-    float most = 0.f;
-#pragma unroll 4
-    for (long i = j.from + 8 * threadIdx.x; i < j.to; i += 8 * kThreads) {
-        float v[8];
-        row_load8<BF16>(j.data, i, j.to, v);
+__device__ __forceinline__ void take(const float (&v)[8], double (&sum)[2], float& most) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (MAX) {
-                const float m = fabsf(v[e]);
-                most = m > most || m != m ? m : most;
-            } else {
-                acc = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), acc);
-            }
+    for (int e = 0; e < 8; ++e) {
+        if (MAX) {
+            const float m = fabsf(v[e]);
+            most = m > most || m != m ? m : most;
+        } else {
+            sum[e & 1] = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum[e & 1]);
         }
     }
-    return MAX ? static_cast<double>(most) : acc;
+}
+
+template <bool BF16, bool MAX>
+__device__ __forceinline__ double piece_value(const Job& j) {
+    double sum[2] = {0.0, 0.0};
+    float most = 0.f;
+    const long at = j.from + 8 * threadIdx.x;
+    if (j.to - j.from == kPiece) {
+#pragma unroll 1
+        for (long i = at; i < j.to; i += 8 * kThreads * kAtOnce) {
+            float v[kAtOnce][8];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) row_load8_inside<BF16>(j.data, i + 8 * kThreads * k, v[k]);
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) take<BF16, MAX>(v[k], sum, most);
+        }
+    } else {
+        for (long i = at; i < j.to; i += 8 * kThreads) {
+            float v[8];
+            row_load8<BF16>(j.data, i, j.to, v);
+            take<BF16, MAX>(v, sum, most);
+        }
+    }
+    return MAX ? static_cast<double>(most) : sum[0] + sum[1];
 }
 
 template <bool MAX>
@@ -99,13 +117,28 @@ __global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* part,
 
 template <bool BF16>
 __device__ __forceinline__ void scale_piece(const Job& j, float factor) {
-#pragma unroll 4
-    for (long i = j.from + 8 * threadIdx.x; i < j.to; i += 8 * kThreads) {
-        float v[8];
-        row_load8<BF16>(j.data, i, j.to, v);
+    const long at = j.from + 8 * threadIdx.x;
+    if (j.to - j.from == kPiece) {
+#pragma unroll 1
+        for (long i = at; i < j.to; i += 8 * kThreads * kAtOnce) {
+            float v[kAtOnce][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= factor;
-        row_store8<BF16>(j.data, i, j.to, v);
+            for (int k = 0; k < kAtOnce; ++k) row_load8_inside<BF16>(j.data, i + 8 * kThreads * k, v[k]);
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] *= factor;
+                row_store8<BF16>(j.data, i + 8 * kThreads * k, j.to, v[k]);
+            }
+        }
+    } else {
+        for (long i = at; i < j.to; i += 8 * kThreads) {
+            float v[8];
+            row_load8<BF16>(j.data, i, j.to, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= factor;
+            row_store8<BF16>(j.data, i, j.to, v);
+        }
     }
 }
 

@@ -5,7 +5,7 @@ bfloat16 tensors in one call, squares summed in 64 bits, in a fixed order.
 """
 from __future__ import annotations
 
-import ctypes
+import array
 import math
 
 import torch
@@ -34,19 +34,19 @@ class _Tensors:
             grads = [grads]
         self.grads = grads = [g for g in grads if g is not None]
         n = len(grads)
-        devices = {g.device for g in grads} or {torch.device("cuda", torch.cuda.current_device())}
-        self.device = devices.pop()
-        if devices or self.device.type != "cuda":
+        index = set(map(torch.Tensor.get_device, grads)) or {torch.cuda.current_device()}
+        if len(index) > 1 or min(index) < 0 or (n and grads[0].device.type != "cuda"):
             raise ValueError("the gradients must be on one device")
-        codes = [_CODES.get(g.dtype) for g in grads]
-        if None in codes:
-            raise TypeError(f"unsupported dtype {grads[codes.index(None)].dtype}")
+        self.device = torch.device("cuda", index.pop())
+        types = [g.dtype for g in grads]
+        if any(t not in _CODES for t in set(types)):
+            raise TypeError(f"unsupported dtype among {set(types)}")
         if not all(map(torch.Tensor.is_contiguous, grads)) and not all(map(_dense, grads)):
             raise ValueError("a gradient has gaps between its elements, or elements in one place")
-        self.data = (ctypes.c_void_p * n)(*map(torch.Tensor.data_ptr, grads))
-        self.counts = (ctypes.c_size_t * n)(*map(torch.Tensor.numel, grads))
-        self.dtypes = (ctypes.c_int * n)(*codes)
-        self.args = (self.data, self.counts, self.dtypes, n)
+        # (arrays of this kind are filled in half the time of ctypes' own)
+        self.keep = (array.array("Q", list(map(torch.Tensor.data_ptr, grads))), array.array("Q", list(map(torch.Tensor.numel, grads))),
+                     array.array("i", [_CODES[t] for t in types]))
+        self.args = (*(a.buffer_info()[0] for a in self.keep), n)
 
     def norm(self, norm_type, workspace):
         kind = _NORMS.get(float(norm_type))
@@ -54,7 +54,7 @@ class _Tensors:
             raise ValueError("norm_type is 2 or inf")
         lib = binding.load()
         if workspace is None:
-            workspace = torch.empty(max(lib.conv1d_grad_norm_workspace_bytes(self.counts, self.args[3]), 8), dtype=torch.uint8, device=self.device)
+            workspace = torch.empty(max(lib.conv1d_grad_norm_workspace_bytes(*self.args[1::2]), 8), dtype=torch.uint8, device=self.device)
         norm = torch.empty((), dtype=torch.float32, device=self.device)
         binding._check(lib.conv1d_grad_norm(*self.args, kind, norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                             binding._current_stream()))
