@@ -1,15 +1,19 @@
-"""The layer as a ``torch.autograd.Function`` and an ``nn.Module`` on top of the C-ABI binding.
+"""The layer, the causal convolution and the selective scan as ``torch.autograd.Function``s on top of the C-ABI binding.
 
 Glue only: every arithmetic step of the three passes and of the bias and ReLU around them runs in the library's kernels;
 torch supplies device memory, the stream and the autograd graph.  This is the interface the
 paper's single-layer measurements use (Section 4.3: ``net.forward(x)`` and ``out.sum().backward()``).
+
+A step captured into a graph takes its gradients by ``torch.autograd.grad`` while no eager graph of the same leaves is
+alive: the nodes that accumulate into ``.grad`` belong to the stream they were made on.
 """
 from __future__ import annotations
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
-from . import binding
+from . import binding, sequence
 
 
 def _has_tangent(t) -> bool:
@@ -75,3 +79,92 @@ class Conv1d(torch.nn.Module):
     def forward(self, x):
         return conv1d(x, self.weight, self.bias, self.dilation, self.padding, self.relu,
                       bf16_out=False)
+
+
+def _along(t):
+    """t with its last axis contiguous."""
+    return t if t is None or t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
+
+
+class CausalFunction(torch.autograd.Function):
+    """(y, final) of sequence.conv1d_causal_fwd; its gradients are not differentiable again."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias, init, lengths, silu: bool, want_final: bool):
+        x, w = _along(x), w.contiguous()
+        init = None if init is None else init.contiguous()
+        b = None if bias is None else bias.contiguous().float()
+        y = sequence.conv1d_causal_fwd(x, w, bias=b, silu=silu, init=init, lengths=lengths, want_final=want_final)
+        ctx.save_for_backward(x, w, b, init, lengths)
+        ctx.silu, ctx.bias_type = silu, None if bias is None else bias.dtype
+        ctx.set_materialize_grads(False)
+        return y if want_final else (y, None)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy, gfinal):
+        x, w, b, init, lengths = ctx.saved_tensors
+        gy = torch.zeros_like(x, memory_format=torch.contiguous_format) if gy is None else _along(gy.resolve_neg().to(x.dtype))
+        gfinal = None if gfinal is None else gfinal.resolve_neg().to(x.dtype).contiguous()
+        dx, dw, db, di = sequence.conv1d_causal_bwd(gy, x, w, bias=b, silu=ctx.silu, init=init, lengths=lengths, dfinal=gfinal,
+                                                    want_init=init is not None)
+        return dx, dw.to(w.dtype), None if db is None else db.to(ctx.bias_type), di, None, None, None
+
+
+def conv1d_causal(x, w, bias=None, silu: bool = False, init=None, lengths=None, want_final: bool = False):
+    """y[N, C, L] of the depthwise causal convolution of x[N, C, L] with w[C, S]; (y, final) with want_final."""
+    y, final = CausalFunction.apply(x, w, bias, init, lengths, silu, want_final)
+    return (y, final) if want_final else y
+
+
+class CausalConv1d(torch.nn.Module):
+    """Depthwise causal convolution of `kernel_size` taps, one filter per channel, with a bias and (silu) x * sigmoid(x) behind it."""
+
+    def __init__(self, channels: int, kernel_size: int, bias: bool = True, silu: bool = False, dtype=torch.float32, device="cuda"):
+        super().__init__()
+        self.silu = silu
+        w = torch.empty(channels, kernel_size, dtype=torch.float32, device=device)
+        torch.nn.init.normal_(w, std=kernel_size ** -0.5)
+        self.weight = torch.nn.Parameter(w.to(dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, dtype=torch.float32, device=device)) if bias else None
+
+    def forward(self, x, init=None, lengths=None, want_final: bool = False):
+        return conv1d_causal(x, self.weight, self.bias, self.silu, init, lengths, want_final)
+
+    def step(self, x, state):
+        """One position x[N, C] of every sequence; `state` is moved on."""
+        with torch.no_grad():
+            return sequence.conv1d_causal_step(x, self.weight, state, bias=self.bias, silu=self.silu)
+
+
+class ScanFunction(torch.autograd.Function):
+    """(y, final) of sequence.conv1d_scan_fwd; its gradients are not differentiable again."""
+
+    @staticmethod
+    def forward(ctx, x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus: bool, want_final: bool):
+        x, dt, B, C, z = (_along(t) for t in (x, dt, B, C, z))
+        ctx.types = [None if t is None else t.dtype for t in (A, skip, dt_bias, init)]
+        A, skip, dt_bias, init = (None if t is None else t.contiguous().float() for t in (A, skip, dt_bias, init))
+        y, final, saved = sequence.conv1d_scan_fwd(x, dt, A, B, C, skip=skip, z=z, dt_bias=dt_bias, softplus=softplus, init=init,
+                                                   lengths=lengths, want_final=want_final, save=any(ctx.needs_input_grad))
+        ctx.save_for_backward(x, dt, A, B, C, skip, z, dt_bias, init, lengths, saved)
+        ctx.softplus = softplus
+        ctx.set_materialize_grads(False)
+        return y, final
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy, gfinal):
+        x, dt, A, B, C, skip, z, dt_bias, init, lengths, saved = ctx.saved_tensors
+        gy = torch.zeros_like(x, memory_format=torch.contiguous_format) if gy is None else _along(gy.resolve_neg().to(x.dtype))
+        gfinal = None if gfinal is None else gfinal.resolve_neg().float().contiguous()
+        g = sequence.conv1d_scan_bwd(gy, saved, x, dt, A, B, C, skip=skip, z=z, dt_bias=dt_bias, softplus=ctx.softplus, init=init,
+                                     lengths=lengths, dfinal=gfinal, want_init=init is not None)
+        dA, dskip, ddt_bias, dinit = (None if v is None else v.to(t) for v, t in zip((g.dA, g.dskip, g.ddt_bias, g.dinit), ctx.types))
+        return g.dx, g.ddt, dA, g.dB, g.dC, dskip, g.dz, ddt_bias, dinit, None, None, None
+
+
+def conv1d_scan(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool = False, init=None, lengths=None, want_final: bool = False):
+    """y[N, D, L] of the selective scan (sequence.conv1d_scan_fwd); (y, final) with want_final."""
+    y, final = ScanFunction.apply(x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus, want_final)
+    return (y, final) if want_final else y
