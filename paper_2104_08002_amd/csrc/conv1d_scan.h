@@ -35,7 +35,7 @@ struct ScanArgs {
     int nseg, seg_len; // the sequence in segments of seg_len steps, a multiple of scan_tile(P)
     int chunks;        // ceil(L / kSub)
     int blocks_d;      // workgroups along the channels of a group
-    long first;        // first workgroup of the launch
+    int first;         // first workgroup of the launch
     // backward
     const void* dout;
     long dout_sn, dout_sd;
@@ -106,14 +106,14 @@ struct ScanPlace {
     int g, seg, cb;
 };
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
-    long b = a.first + blockIdx.x;
+    unsigned b = static_cast<unsigned>(a.first) + blockIdx.x, q = b / a.blocks_d;
     ScanPlace p;
-    long q = b / a.blocks_d;
     p.cb = static_cast<int>(b - q * a.blocks_d);
     b = q / a.nseg;
     p.seg = static_cast<int>(q - b * a.nseg);
-    p.n = b / a.G;
-    p.g = static_cast<int>(b - p.n * a.G);
+    q = b / a.G;
+    p.g = static_cast<int>(b - q * a.G);
+    p.n = q;
     return p;
 }
 
@@ -127,29 +127,49 @@ __device__ __forceinline__ const typename RowElem<BF16>::type* scan_row(const vo
     return static_cast<const typename RowElem<BF16>::type*>(base) + n * sn + d * sd;
 }
 
-// B or C of T steps from t0 on into LDS, [step][SP]; 0 behind `end` and for states that are not there
-template <bool BF16, int SP, int T>
-__device__ __forceinline__ void scan_stage_states(const void* from, long base, long ss, int S, int t0, int end, float* to) {
-    const typename RowElem<BF16>::type* row0 = static_cast<const typename RowElem<BF16>::type*>(from) + base;
-    for (int i = threadIdx.x; i < SP * (T / 8); i += blockDim.x) {
-        const int s = i & (SP - 1), c = i / SP;
-        float v[8];
+// B and C (BOTH; else `first` alone) of T steps from t0 on into LDS, [step][SP]; 0 behind `end` and for states that are not
+// there.  8 steps of a state a lane; the lane's first loads (begin) go out before the rows', their values are used behind them.
+template <bool BF16, int SP, int T, bool BOTH>
+struct ScanStates {
+    static constexpr int kItems = SP * (T / 8), kAll = BOTH ? 2 * kItems : kItems;
+    using E = typename RowElem<BF16>::type;
+    const E *first, *second;
+    long first_ss, second_ss;
+    int S;
+    float v[8];
+
+    __device__ __forceinline__ void load(int i, int t0, int end) {
+        const int s = i & (SP - 1), c = i / SP % (T / 8);
+        const bool which = BOTH && i >= kItems;
         if (s < S) {
-            row_load8<BF16>(row0 + s * ss, t0 + 8 * c, end, v);
+            row_load8<BF16>((which ? second : first) + s * (which ? second_ss : first_ss), t0 + 8 * c, end, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) to[(8 * c + e) * SP + s] = v[e];
     }
-}
+    __device__ __forceinline__ void put(int i, float* to_first, float* to_second) const {
+        float* to = (BOTH && i >= kItems ? to_second : to_first) + (i / SP % (T / 8)) * (8 * SP) + (i & (SP - 1));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[e * SP] = v[e];
+    }
+    __device__ __forceinline__ void begin(int t0, int end) {
+        if (static_cast<int>(threadIdx.x) < kAll) load(threadIdx.x, t0, end);
+    }
+    __device__ __forceinline__ void finish(int t0, int end, float* to_first, float* to_second) {
+        if (static_cast<int>(threadIdx.x) < kAll) put(threadIdx.x, to_first, to_second);
+        for (int i = threadIdx.x + blockDim.x; i < kAll; i += blockDim.x) {
+            load(i, t0, end);
+            put(i, to_first, to_second);
+        }
+    }
+};
 
-// the lane's part in loading and storing rows: row (q * RPP + lane / LPR) of the wave, 8 elements from 8 (lane % LPR) on
+// the lane's part in loading and storing rows: row lane / LPR of the wave, 8 elements from 8 (lane % LPR) on
 template <int P, int T>
 struct ScanRows {
-    static constexpr int CW = kSeqWave / P, LPR = T / 8, RPP = kSeqWave / LPR, PASSES = CW > RPP ? CW / RPP : 1;
-    static constexpr int RS = scan_stride(T);
+    static constexpr int CW = kSeqWave / P, LPR = T / 8, RS = scan_stride(T);
+    static_assert(CW * LPR <= kSeqWave, "a wave stages a tile at once");
 };
 
 template <bool BF16, bool INSIDE>

@@ -74,112 +74,102 @@ __device__ __forceinline__ void row_sums(const float (&q)[K], float (&out)[kSums
 }
 #endif
 
-// The lane's rows: where they begin and what they share.
+// The lane's row: where it begins and what its elements share.
 template <bool BF16, int P, int T>
-struct Rows {
+struct BackRow {
     using R = ScanRows<P, T>;
     using E = typename RowElem<BF16>::type;
-    const E *x[R::PASSES], *dt[R::PASSES], *dout[R::PASSES], *z[R::PASSES];
-    float bias[R::PASSES];
-    bool real[R::PASSES];
-    long d[R::PASSES];
-    int c;
+    const E *x, *dt, *dout, *z;
+    float bias;
+    bool real;
+    long d;
+    int c, at;  // first step of the lane within the tile, its place in LDS
 
-    __device__ __forceinline__ Rows(const ScanArgs& a, const ScanPlace& at, int base, int lane) {
+    __device__ __forceinline__ BackRow(const ScanArgs& a, const ScanPlace& p, int base, int lane) {
+        const int row = lane / R::LPR;
         c = 8 * (lane % R::LPR);
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            real[q] = row < R::CW && base + row < a.Dg;
-            d[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
-            x[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, d[q]);
-            dt[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, d[q]);
-            dout[q] = scan_row<BF16>(a.dout, a.dout_sn, a.dout_sd, at.n, d[q]);
-            z[q] = a.z ? scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, d[q]) : nullptr;
-            bias[q] = a.dt_bias ? a.dt_bias[d[q]] : 0.f;
-        }
+        at = row * R::RS + c;
+        real = row < R::CW && base + row < a.Dg;
+        d = static_cast<long>(p.g) * a.Dg + (real ? base + row : 0);
+        x = scan_row<BF16>(a.x, a.x_sn, a.x_sd, p.n, d);
+        dt = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, p.n, d);
+        dout = scan_row<BF16>(a.dout, a.dout_sn, a.dout_sd, p.n, d);
+        z = a.z ? scan_row<BF16>(a.z, a.z_sn, a.z_sd, p.n, d) : nullptr;
+        bias = a.dt_bias ? a.dt_bias[d] : 0.f;
     }
     // e, dy and (WITH_X) x of the tile at t0 into LDS.  INSIDE: it lies within the sequence, the wave's channels are all there.
     template <bool INSIDE, bool WITH_X>
-    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, float* sE, float* sX, float* sY) const {
+    __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, float* sE, float* sX, float* sY) const {
+        const int end = real ? len : 0;
+        if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
+        float v[8], g[8], u[8], w[8];
+        scan_load8<BF16, INSIDE>(dt, t0 + c, end, v);
+        scan_load8<BF16, INSIDE>(dout, t0 + c, end, g);
+        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, end, w);
+        if (WITH_X) scan_load8<BF16, INSIDE>(x, t0 + c, end, u);
 #pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR, end = real[q] ? len : 0;
-            if (row >= R::CW) continue;
-            float v[8], g[8], u[8];
-            scan_load8<BF16, INSIDE>(dt[q], t0 + c, end, v);
-            scan_load8<BF16, INSIDE>(dout[q], t0 + c, end, g);
-            if (a.z) {
-                scan_load8<BF16, INSIDE>(z[q], t0 + c, end, u);
+        for (int i = 0; i < 8; ++i) v[i] += bias;
+        if (a.softplus) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] *= u[i] * sigmoid_of(u[i]);
-            }
-            if (WITH_X) {
-                scan_load8<BF16, INSIDE>(x[q], t0 + c, end, u);
-                lds_put8(sX + row * R::RS + c, u);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += bias[q];
-            if (a.softplus) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = softplus_of(v[i]);
-            }
-            if (!INSIDE) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < end ? v[i] : 0.f;
-            }
-            lds_put8(sE + row * R::RS + c, v);
-            lds_put8(sY + row * R::RS + c, g);
+            for (int i = 0; i < 8; ++i) v[i] = softplus_of(v[i]);
         }
+        if (!INSIDE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < end ? v[i] : 0.f;
+        }
+        lds_put8(sE + at, v);
+        if (z) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] *= w[i] * sigmoid_of(w[i]);
+        }
+        lds_put8(sY + at, g);
+        if (WITH_X) lds_put8(sX + at, u);
     }
     // the gradients of x, dt and z from what the walk back left in LDS
     template <bool INSIDE>
-    __device__ __forceinline__ void finish(const ScanArgs& a, const ScanPlace& at, int lane, int t0, int len, const float* sE, const float* sX,
-                                           const float* sY, float (&dskip)[R::PASSES], float (&dbias)[R::PASSES]) const {
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            if (!real[q] || t0 + c >= a.L) continue;
-            const long o = (at.n * a.D + d[q]) * a.L;
-            const float skip = a.skip ? a.skip[d[q]] : 0.f;
-            float u[8], v[8], g[8];
-            scan_load8<BF16, INSIDE>(x[q], t0 + c, len, u);
-            scan_load8<BF16, INSIDE>(dout[q], t0 + c, len, g);
-            if (a.z) {
-                float w[8], y[8];
-                scan_load8<BF16, INSIDE>(z[q], t0 + c, len, w);
-                lds_get8(sY + row * R::RS + c, y);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float sig = sigmoid_of(w[i]), zs = w[i] * sig;
-                    y[i] = g[i] * fmaf(skip, u[i], y[i]) * fmaf(zs, 1.f - sig, sig);
-                    g[i] *= zs;
-                    if (!INSIDE) y[i] = t0 + c + i < len ? y[i] : 0.f;
-                }
-                row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, a.L, y);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dskip[q] = fmaf(g[i], u[i], dskip[q]);
-            lds_get8(sE + row * R::RS + c, u);
+    __device__ __forceinline__ void finish(const ScanArgs& a, const ScanPlace& p, int t0, int len, const float* sE, const float* sX,
+                                           const float* sY, float& dskip, float& dbias) const {
+        if (!real || t0 + c >= a.L) return;
+        const long o = (p.n * a.D + d) * a.L;
+        const int end = INSIDE ? t0 + c + 8 : a.L;
+        const float skip = a.skip ? a.skip[d] : 0.f;
+        float u[8], v[8], g[8], w[8];
+        scan_load8<BF16, INSIDE>(x, t0 + c, len, u);
+        scan_load8<BF16, INSIDE>(dout, t0 + c, len, g);
+        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, w);
+        if (a.softplus) scan_load8<BF16, INSIDE>(dt, t0 + c, len, v);
+        if (z) {
+            float y[8];
+            lds_get8(sY + at, y);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                g[i] = fmaf(skip, g[i], u[i]);
-                if (!INSIDE) g[i] = t0 + c + i < len ? g[i] : 0.f;
+                const float sig = sigmoid_of(w[i]), zs = w[i] * sig;
+                y[i] = g[i] * fmaf(skip, u[i], y[i]) * fmaf(zs, 1.f - sig, sig);
+                g[i] *= zs;
+                if (!INSIDE) y[i] = t0 + c + i < len ? y[i] : 0.f;
             }
-            row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, a.L, g);
-            lds_get8(sX + row * R::RS + c, u);
-            if (a.softplus) {
-                scan_load8<BF16, INSIDE>(dt[q], t0 + c, len, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] *= sigmoid_of(v[i] + bias[q]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!INSIDE) u[i] = t0 + c + i < len ? u[i] : 0.f;
-                dbias[q] += u[i];
-            }
-            row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, a.L, u);
+            row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, end, y);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dskip = fmaf(g[i], u[i], dskip);
+        lds_get8(sE + at, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] = fmaf(skip, g[i], u[i]);
+            if (!INSIDE) g[i] = t0 + c + i < len ? g[i] : 0.f;
+        }
+        row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, end, g);
+        lds_get8(sX + at, u);
+        if (a.softplus) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] *= sigmoid_of(v[i] + bias);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!INSIDE) u[i] = t0 + c + i < len ? u[i] : 0.f;
+            dbias += u[i];
+        }
+        row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, end, u);
     }
 };
 
@@ -198,7 +188,9 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     const int base = (at.cb * waves + wave) * R::CW;
     const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
-    const Rows<BF16, P, T> rows(a, at, base, lane);
+    const BackRow<BF16, P, T> line(a, at, base, lane);
+    using E = typename RowElem<BF16>::type;
+    ScanStates<BF16, SP, T, false> states{static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, nullptr, a.c_ss, 0, a.S, {}};
     float rate[K], carry[K], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -207,9 +199,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
-        if (t0 + T <= len && full) rows.template stage<true, false>(a, lane, t0, len, sE[wave], nullptr, sY[wave]);
-        else rows.template stage<false, false>(a, lane, t0, len, sE[wave], nullptr, sY[wave]);
-        scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        states.begin(t0, len);
+        if (t0 + T <= len && full) line.template stage<true, false>(a, t0, len, sE[wave], nullptr, sY[wave]);
+        else line.template stage<false, false>(a, t0, len, sE[wave], nullptr, sY[wave]);
+        states.finish(t0, len, sC, nullptr);
         __syncthreads();
         const float *e_row = sE[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
 #pragma unroll 1
@@ -241,7 +234,6 @@ template <bool BF16, int K, int P>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanArgs a) {
     constexpr int SP = K * P, T = scan_tile_back(P);
     using R = ScanRows<P, T>;
-    using E = typename RowElem<BF16>::type;
     // e, x and dy of a step; the walk back leaves sum_s e g B, de and sum_s C h in their places
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS], sY[kScanWaves][R::CW * R::RS];
     __shared__ __align__(16) float sB[T * SP], sC[T * SP];
@@ -253,8 +245,11 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     const int base = (at.cb * waves + wave) * R::CW;
     const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
-    const Rows<BF16, P, T> rows(a, at, base, lane);
-    float rate[K], carry[K], dA[K], dskip[R::PASSES], dbias[R::PASSES];
+    const BackRow<BF16, P, T> line(a, at, base, lane);
+    using E = typename RowElem<BF16>::type;
+    ScanStates<BF16, SP, T, true> states{static_cast<const E*>(a.B) + at.n * a.b_sn + at.g * a.b_sg,
+                                         static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, {}};
+    float rate[K], carry[K], dA[K], dskip = 0.f, dbias = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int s = K * p + k;
@@ -264,15 +259,13 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         if (a.nseg > 1) carry[k] = there ? a.carries[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
         else if (a.dfinal && there && s < a.S) carry[k] = a.dfinal[(at.n * a.D + d) * a.S + s];
     }
-#pragma unroll
-    for (int q = 0; q < R::PASSES; ++q) dskip[q] = dbias[q] = 0.f;
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
         const bool inside = t0 + T <= len && full;
-        if (inside) rows.template stage<true, true>(a, lane, t0, len, sE[wave], sX[wave], sY[wave]);
-        else rows.template stage<false, true>(a, lane, t0, len, sE[wave], sX[wave], sY[wave]);
-        scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        states.begin(t0, len);
+        if (inside) line.template stage<true, true>(a, t0, len, sE[wave], sX[wave], sY[wave]);
+        else line.template stage<false, true>(a, t0, len, sE[wave], sX[wave], sY[wave]);
+        states.finish(t0, len, sB, sC);
         __syncthreads();
         float dA_tile[K] = {};
         float *e_row = sE[wave] + cl * R::RS, *x_row = sX[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
@@ -383,21 +376,19 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     if (t + e < a.L) store_elem<BF16>(which ? a.dC : a.dB, o + e, v[e]);
             }
         }
-        if (inside) rows.template finish<true>(a, at, lane, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
-        else rows.template finish<false>(a, at, lane, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
+        if (inside) line.template finish<true>(a, at, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
+        else line.template finish<false>(a, at, t0, len, sE[wave], sX[wave], sY[wave], dskip, dbias);
         // (the next tile's barrier stands between these reads of `red` and its next values)
     }
     float* part = a.part_p + (at.n * a.nseg + at.seg) * (static_cast<long>(a.D) * (SP + 2));
 #pragma unroll
-    for (int q = 0; q < R::PASSES; ++q) {
-#pragma unroll
-        for (int m = 1; m < R::LPR; m <<= 1) {
-            dskip[q] += lane_xor(dskip[q], m);
-            dbias[q] += lane_xor(dbias[q], m);
-        }
-        if (lane % R::LPR || !rows.real[q]) continue;
-        part[static_cast<long>(a.D) * SP + rows.d[q]] = dskip[q];
-        part[static_cast<long>(a.D) * (SP + 1) + rows.d[q]] = dbias[q];
+    for (int m = 1; m < R::LPR; m <<= 1) {
+        dskip += lane_xor(dskip, m);
+        dbias += lane_xor(dbias, m);
+    }
+    if (lane % R::LPR == 0 && line.real) {
+        part[static_cast<long>(a.D) * SP + line.d] = dskip;
+        part[static_cast<long>(a.D) * (SP + 1) + line.d] = dbias;
     }
     if (!there) return;
 #pragma unroll
@@ -473,8 +464,9 @@ hipError_t bwd_launch(ScanArgs a, const ScanPlan& p, float* dA, float* dskip, fl
             if (e != hipSuccess) return e;
             continue;
         }
-        for (a.first = 0; a.first < blocks; a.first += most) {
-            const long left = blocks - a.first;
+        for (long first = 0; first < blocks; first += most) {
+            a.first = static_cast<int>(first);
+            const long left = blocks - first;
             const dim3 grid(static_cast<unsigned>(left < most ? left : most));
             const hipError_t e = launch_kernel(stage == 0 ? scan_adjoint_kernel<BF16, K, P> : scan_bwd_kernel<BF16, K, P>, grid, block, 0, st, a);
             if (e != hipSuccess) return e;

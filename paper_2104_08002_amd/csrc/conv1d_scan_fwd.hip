@@ -9,77 +9,73 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The lane's rows of a tile.  INSIDE: the tile lies within the sequence, the wave's channels are all there: no masks.
-template <bool BF16, int P, int T>
-struct FwdRows {
+// The lane's row of a tile.  INSIDE: the tile lies within the sequence, the wave's channels are all there: no masks.
+template <bool BF16, int P, int T, bool ENDS>
+struct FwdRow {
     using R = ScanRows<P, T>;
     using E = typename RowElem<BF16>::type;
-    const E *x[R::PASSES], *dt[R::PASSES];
-    float bias[R::PASSES], skip[R::PASSES];
-    bool real[R::PASSES];
-    long d[R::PASSES];
-    int c;
+    const E *x, *dt, *z;
+    E* out;
+    float bias, skip;
+    bool real;
+    int c, at;          // first step of the lane within the tile, its place in LDS
+    float u[8], w[8];   // x and z of the tile
 
-    __device__ __forceinline__ FwdRows(const ScanArgs& a, const ScanPlace& at, int base, int lane) {
+    __device__ __forceinline__ FwdRow(const ScanArgs& a, const ScanPlace& p, int base, int lane) {
+        const int row = lane / R::LPR;
         c = 8 * (lane % R::LPR);
-#pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            real[q] = row < R::CW && base + row < a.Dg;
-            d[q] = static_cast<long>(at.g) * a.Dg + (real[q] ? base + row : 0);
-            x[q] = scan_row<BF16>(a.x, a.x_sn, a.x_sd, at.n, d[q]);
-            dt[q] = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, at.n, d[q]);
-            bias[q] = a.dt_bias ? a.dt_bias[d[q]] : 0.f;
-            skip[q] = a.skip ? a.skip[d[q]] : 0.f;
-        }
+        at = row * R::RS + c;
+        real = row < R::CW && base + row < a.Dg;
+        const long d = static_cast<long>(p.g) * a.Dg + (real ? base + row : 0);
+        x = scan_row<BF16>(a.x, a.x_sn, a.x_sd, p.n, d);
+        dt = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, p.n, d);
+        bias = a.dt_bias ? a.dt_bias[d] : 0.f;
+        if (ENDS) return;
+        z = a.z ? scan_row<BF16>(a.z, a.z_sn, a.z_sd, p.n, d) : nullptr;
+        out = static_cast<E*>(a.out) + p.n * a.out_sn + d * a.out_sd;
+        skip = a.skip ? a.skip[d] : 0.f;
     }
     // e and e x into LDS
     template <bool INSIDE>
-    __device__ __forceinline__ void stage(const ScanArgs& a, int lane, int t0, int len, float* sE, float* sX) const {
+    __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, float* sE, float* sX) {
+        const int end = real ? len : 0;
+        if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
+        float e[8], ex[8];
+        scan_load8<BF16, INSIDE>(x, t0 + c, end, u);
+        scan_load8<BF16, INSIDE>(dt, t0 + c, end, e);
+        if (!ENDS && z) scan_load8<BF16, INSIDE>(z, t0 + c, end, w);
 #pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR, end = real[q] ? len : 0;
-            if (row >= R::CW) continue;
-            float v[8], e[8];
-            scan_load8<BF16, INSIDE>(x[q], t0 + c, end, v);
-            scan_load8<BF16, INSIDE>(dt[q], t0 + c, end, e);
+        for (int i = 0; i < 8; ++i) e[i] += bias;
+        if (a.softplus) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] += bias[q];
-            if (a.softplus) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!INSIDE) e[i] = t0 + c + i < end ? e[i] : 0.f;
-                v[i] *= e[i];
-            }
-            lds_put8(sE + row * R::RS + c, e);
-            lds_put8(sX + row * R::RS + c, v);
+            for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!INSIDE) e[i] = t0 + c + i < end ? e[i] : 0.f;
+            ex[i] = u[i] * e[i];
+        }
+        lds_put8(sE + at, e);
+        lds_put8(sX + at, ex);
     }
     // the output from the sums in LDS
     template <bool INSIDE>
-    __device__ __forceinline__ void finish(const ScanArgs& a, const ScanPlace& at, int lane, int t0, int len, const float* sY) const {
+    __device__ __forceinline__ void finish(const ScanArgs& a, int t0, int len, const float* sY) const {
+        if (!real || t0 + c >= a.L) return;
+        float y[8];
+        lds_get8(sY + at, y);
 #pragma unroll
-        for (int q = 0; q < R::PASSES; ++q) {
-            const int row = q * R::RPP + lane / R::LPR;
-            if (!real[q] || t0 + c >= a.L) continue;
-            float v[8], z[8], y[8];
-            lds_get8(sY + row * R::RS + c, y);
-            scan_load8<BF16, INSIDE>(x[q], t0 + c, len, v);
+        for (int i = 0; i < 8; ++i) y[i] = fmaf(skip, u[i], y[i]);
+        if (z) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = fmaf(skip[q], v[i], y[i]);
-            if (a.z) {
-                scan_load8<BF16, INSIDE>(scan_row<BF16>(a.z, a.z_sn, a.z_sd, at.n, d[q]), t0 + c, len, z);
+            for (int i = 0; i < 8; ++i) y[i] *= w[i] * sigmoid_of(w[i]);
+        }
+        if (!INSIDE) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] *= z[i] * sigmoid_of(z[i]);
-            }
-            if (!INSIDE) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
-            }
-            row_store8<BF16>(const_cast<E*>(scan_row<BF16>(a.out, a.out_sn, a.out_sd, at.n, d[q])), t0 + c, a.L, y);
+            for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
+            row_store8<BF16>(out, t0 + c, a.L, y);
+        } else {
+            row_store8<BF16>(out, t0 + c, t0 + c + 8, y);
         }
     }
 };
@@ -89,7 +85,6 @@ template <bool BF16, int K, int P, bool ENDS>
 __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanArgs a) {
     constexpr int SP = K * P, T = scan_tile(P);
     using R = ScanRows<P, T>;
-    using E = typename RowElem<BF16>::type;
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS];  // e (then y) and e x
     __shared__ __align__(16) float sB[T * SP], sC[ENDS ? 4 : T * SP];
     const ScanPlace at = scan_place(a);
@@ -111,15 +106,18 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
         if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
         else if (a.init && there && s < a.S) h[k] = a.init[(at.n * a.D + d) * a.S + s];
     }
-    const FwdRows<BF16, P, T> rows(a, at, base, lane);
+    FwdRow<BF16, P, T, ENDS> row(a, at, base, lane);
+    using E = typename RowElem<BF16>::type;
+    ScanStates<BF16, SP, T, !ENDS> states{static_cast<const E*>(a.B) + at.n * a.b_sn + at.g * a.b_sg,
+                                          static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, {}};
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     float sum = 0.f;
     for (int t0 = t_begin; t0 < t_end; t0 += T) {
         const bool inside = t0 + T <= len && full;        // of the whole wave: no masks
-        if (inside) rows.template stage<true>(a, lane, t0, len, sE[wave], sX[wave]);
-        else rows.template stage<false>(a, lane, t0, len, sE[wave], sX[wave]);
-        scan_stage_states<BF16, SP, T>(a.B, at.n * a.b_sn + at.g * a.b_sg, a.b_ss, a.S, t0, len, sB);
-        if (!ENDS) scan_stage_states<BF16, SP, T>(a.C, at.n * a.c_sn + at.g * a.c_sg, a.c_ss, a.S, t0, len, sC);
+        states.begin(t0, len);
+        if (inside) row.template stage<true>(a, t0, len, sE[wave], sX[wave]);
+        else row.template stage<false>(a, t0, len, sE[wave], sX[wave]);
+        states.finish(t0, len, sB, sC);
         __syncthreads();
         float* e_row = sE[wave] + cl * R::RS;
         const float* ex_row = sX[wave] + cl * R::RS;
@@ -158,8 +156,8 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
         }
         __syncthreads();
         if (ENDS) continue;
-        if (inside) rows.template finish<true>(a, at, lane, t0, len, sE[wave]);
-        else rows.template finish<false>(a, at, lane, t0, len, sE[wave]);
+        if (inside) row.template finish<true>(a, t0, len, sE[wave]);
+        else row.template finish<false>(a, t0, len, sE[wave]);
     }
     if (!there) return;
     if (ENDS) {
@@ -237,8 +235,9 @@ hipError_t fwd_launch(ScanArgs a, const ScanPlan& p, hipStream_t st) {
             if (e != hipSuccess) return e;
             continue;
         }
-        for (a.first = 0; a.first < blocks; a.first += most) {
-            const long left = blocks - a.first;
+        for (long first = 0; first < blocks; first += most) {
+            a.first = static_cast<int>(first);
+            const long left = blocks - first;
             const dim3 grid(static_cast<unsigned>(left < most ? left : most));
             const hipError_t e = launch_kernel(stage == 0 ? scan_fwd_kernel<BF16, K, P, true> : scan_fwd_kernel<BF16, K, P, false>, grid, block, 0, st, a);
             if (e != hipSuccess) return e;

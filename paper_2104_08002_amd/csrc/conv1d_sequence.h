@@ -151,7 +151,8 @@ __device__ __forceinline__ float softplus_of(float v) {
     f = fmaf(f, q, 0.40024909377098083f);
     f = fmaf(f, q, 0.6666631698608398f);
     f = fmaf(f, q, 2.f);
-    return fmaf(f, r, __builtin_amdgcn_fmed3f(v, 0.f, INFINITY));  // (max(v, 0); a NaN comes through f r)
+    const int m = static_cast<int>(__float_as_uint(v));  // max(v, 0) as a number of its bits; a NaN comes through f r
+    return fmaf(f, r, __uint_as_float(static_cast<unsigned>(m < 0 ? 0 : m)));
 }
 
 }  // namespace conv1d
