@@ -247,10 +247,10 @@ __global__ __launch_bounds__(kThreads) void causal_bwd_kernel(CausalArgs a) {
 }
 
 // one wave per sum, in 64 bits: the error of a gradient is that of its partial sums
-__global__ __launch_bounds__(kSeqWave) void causal_sums_kernel(const float* partial, float* dw, float* dbias, int S, long per) {
-    const long c = blockIdx.x / (S + 1);
-    const int s = static_cast<int>(blockIdx.x - c * (S + 1));
-    const float* from = partial + blockIdx.x * per;
+__global__ __launch_bounds__(kSeqWave) void causal_sums_kernel(const float* partial, float* dw, float* dbias, int S, long per, long first) {
+    const long i0 = first + blockIdx.x, c = i0 / (S + 1);
+    const int s = static_cast<int>(i0 - c * (S + 1));
+    const float* from = partial + i0 * per;
     double sum = 0.0;
 #pragma unroll 4
     for (long i = threadIdx.x; i < per; i += kSeqWave) sum += static_cast<double>(from[i]);
@@ -375,7 +375,7 @@ bool layout_ok(const conv1d_causal_t* p) {
 
 // rows are counted in 31 bits (units of a launch too: a piece has a row's share of at least kV elements)
 bool sizes_ok(const conv1d_causal_t* p) {
-    return p->S <= kMostTaps && p->L <= 1 << 30 && static_cast<long>(p->N) * p->C <= 0x7fffffffL && static_cast<long>(p->C) * (p->S + 1) <= 0x7fffffffL;
+    return p->S <= kMostTaps && p->L <= 1 << 30 && static_cast<long>(p->N) * p->C <= 0x7fffffffL;
 }
 
 CausalArgs args_of(const conv1d_causal_t* p, int R) {
@@ -432,8 +432,13 @@ int conv1d_causal_bwd(const conv1d_causal_t* p, const void* dy, long dy_sn, long
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = p->dtype == CONV1D_BF16 ? launch_type<true>(true, a, p->S, R, st) : launch_type<false>(true, a, p->S, R, st);
     if (e != hipSuccess || !dw) return status_of(e);
-    return status_of(launch_kernel(causal_sums_kernel, dim3(static_cast<unsigned>(p->C * (p->S + 1))), dim3(kSeqWave), 0, st, a.partial, dw,
-                                   dbias, p->S, static_cast<long>(p->N) * a.pieces));
+    const long sums = static_cast<long>(p->C) * (p->S + 1), most = kSeqMostThreads / kSeqWave;
+    for (long first = 0; first < sums; first += most) {
+        const hipError_t e2 = launch_kernel(causal_sums_kernel, dim3(static_cast<unsigned>(sums - first < most ? sums - first : most)), dim3(kSeqWave), 0, st,
+                                            a.partial, dw, dbias, p->S, static_cast<long>(p->N) * a.pieces, first);
+        if (e2 != hipSuccess) return status_of(e2);
+    }
+    return CONV1D_OK;
 }
 
 int conv1d_causal_step(const conv1d_causal_t* p, void* state, void* y, long y_sn, void* stream) {

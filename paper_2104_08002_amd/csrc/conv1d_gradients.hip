@@ -44,7 +44,7 @@ __device__ __forceinline__ Job job_of(const Table& t, int block) {
 // larger of the two; NaN if one is
 __device__ __forceinline__ double larger(double a, double b) { return b > a || b != b ? b : a; }
 
-template <bool MAX>
+template <bool MAX, int THREADS>
 __device__ __forceinline__ double block_value(double v, double* lds) {
 #pragma unroll
     for (int m = 1; m < kSeqWave; m <<= 1) {
@@ -54,7 +54,7 @@ __device__ __forceinline__ double block_value(double v, double* lds) {
     if ((threadIdx.x & (kSeqWave - 1)) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
-    for (int w = 1; w < kThreads / kSeqWave; ++w) v = MAX ? larger(v, lds[w]) : v + lds[w];
+    for (int w = 1; w < THREADS / kSeqWave; ++w) v = MAX ? larger(v, lds[w]) : v + lds[w];
     return v;
 }
 
@@ -101,17 +101,18 @@ template <bool MAX>
 __global__ __launch_bounds__(kThreads) void grad_part_kernel(Table t, double* part) {
     __shared__ double lds[kThreads / kSeqWave];
     const Job j = job_of(t, static_cast<int>(blockIdx.x));
-    const double v = block_value<MAX>(j.bf16 ? piece_value<true, MAX>(j) : piece_value<false, MAX>(j), lds);
+    const double v = block_value<MAX, kThreads>(j.bf16 ? piece_value<true, MAX>(j) : piece_value<false, MAX>(j), lds);
     if (threadIdx.x == 0) part[blockIdx.x] = v;
 }
 
+constexpr int kJoinThreads = 1024;
 template <bool MAX>
-__global__ __launch_bounds__(kThreads) void grad_join_kernel(const double* part, long n, float* norm) {
-    __shared__ double lds[kThreads / kSeqWave];
+__global__ __launch_bounds__(kJoinThreads) void grad_join_kernel(const double* part, long n, float* norm) {
+    __shared__ double lds[kJoinThreads / kSeqWave];
     double v = 0.0;
 #pragma unroll 8
-    for (long i = threadIdx.x; i < n; i += kThreads) v = MAX ? larger(v, part[i]) : v + part[i];
-    v = block_value<MAX>(v, lds);
+    for (long i = threadIdx.x; i < n; i += kJoinThreads) v = MAX ? larger(v, part[i]) : v + part[i];
+    v = block_value<MAX, kJoinThreads>(v, lds);
     if (threadIdx.x == 0) *norm = static_cast<float>(MAX ? v : sqrt(v));
 }
 
@@ -236,7 +237,7 @@ int conv1d_grad_norm(void* const* data, const size_t* counts, const int* dtypes,
         return launch_kernel(max ? grad_part_kernel<true> : grad_part_kernel<false>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, t, part + before);
     });
     if (e == hipSuccess)
-        e = launch_kernel(max ? grad_join_kernel<true> : grad_join_kernel<false>, dim3(1), dim3(kThreads), 0, st, part,
+        e = launch_kernel(max ? grad_join_kernel<true> : grad_join_kernel<false>, dim3(1), dim3(kJoinThreads), 0, st, part,
                           static_cast<long>(need / sizeof(double)), norm);
     return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP;
 }

@@ -117,9 +117,14 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a) {
     return p;
 }
 
-// state k of lane-in-channel p of channel d: its rate times log2(e); 0 where there is no such state
-__device__ __forceinline__ float scan_rate(const ScanArgs& a, long d, int s, bool there) {
-    return there && s < a.S ? a.A[d * a.S + s] * kLog2e : 0.f;
+// A rate times log2(e), kept finite: a step of 0 (a position behind the end has one) leaves the state whatever the rate is.
+__device__ __forceinline__ float rate_of(float A) {
+    const float r = A * kLog2e, most = 3.4028234e38f;
+    return r > most ? most : r < -most ? -most : r;
+}
+// that of state s of channel d; 0 where there is no such state
+__device__ __forceinline__ float scan_rate(const float* A, int S, long d, int s, bool there) {
+    return there && s < S ? rate_of(A[d * S + s]) : 0.f;
 }
 
 template <bool BF16>
@@ -204,7 +209,7 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
     const bool there = row < static_cast<long>(N) * D;
     const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP, base = threadIdx.x - in_row + s;
     const long n = there ? row / D : 0, d = there ? row - n * D : 0;
-    const float rate = there && s < S ? A[d * S + s] * kLog2e : 0.f;
+    const float rate = scan_rate(A, S, d, s, there);
     float h = there && first && s < S ? first[(n * D + d) * S + s] : 0.f;
     for (int from = 0; from < nseg; from += kRun * chunks) {
         float f[kRun], v[kRun], decay = 1.f, add = 0.f;

@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     float rate[K], carry[K], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        rate[k] = scan_rate(a, d, K * p + k, there);
+        rate[k] = scan_rate(a.A, a.S, d, K * p + k, there);
         carry[k] = 0.f;
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int s = K * p + k;
-        rate[k] = scan_rate(a, d, s, there);
+        rate[k] = scan_rate(a.A, a.S, d, s, there);
         dA[k] = 0.f;
         carry[k] = 0.f;
         if (a.nseg > 1) carry[k] = there ? a.carries[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;

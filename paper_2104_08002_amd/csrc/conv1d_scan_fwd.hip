@@ -100,7 +100,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int s = K * p + k;
-        rate[k] = scan_rate(a, d, s, there);
+        rate[k] = scan_rate(a.A, a.S, d, s, there);
         h[k] = 0.f;
         if (ENDS) continue;
         if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(ScanStepArgs a) {
         if (!there || s >= a.S) continue;
         if (!whole) h[k] = state[s];
         const float b = load_elem<BF16>(a.B, n * a.b_sn + g * a.b_sg + s), c = load_elem<BF16>(a.C, n * a.c_sn + g * a.c_sg + s);
-        h[k] = fmaf(exp2_hw(e * (a.A[d * a.S + s] * kLog2e)), h[k], ex * b);
+        h[k] = fmaf(exp2_hw(e * rate_of(a.A[d * a.S + s])), h[k], ex * b);
         y = fmaf(c, h[k], y);
         if (!whole) state[s] = h[k];
     }

@@ -310,6 +310,27 @@ def test_padding_is_not_read(seq, dtype, L):
         assert torch.equal(a, b)
 
 
+def test_rates_without_bound(seq):
+    """A rate of the type's lowest value, or minus infinity: the state is forgotten by a step above 0 and kept by one of 0, also where
+    the padding has its steps of 0."""
+    gen = _gen(21)
+    for lowest in (torch.finfo(torch.float32).min, -math.inf):
+        for L in (40, 1500):
+            c = _scan_case(gen, torch.float32, 2, 3, L, 4, 1)
+            c.update(softplus=False, dt=torch.ones(2, 3, L, device="cuda"), dt_bias=None, z=None, skip=None)
+            c["A"][:, 1] = lowest
+            lengths = torch.tensor([L - 7, 0], dtype=torch.int32, device="cuda")
+            y, final, saved = seq.conv1d_scan_fwd(**c, lengths=lengths, want_final=True, save=True)
+            assert y.isfinite().all() and torch.equal(final[1], c["init"][1])
+            assert torch.equal(final[0, :, 1], c["x"][0, :, L - 8] * c["B"][0, 0, 1, L - 8])
+            g = seq.conv1d_scan_bwd(torch.ones_like(y), saved, **c, lengths=lengths, want_init=True)
+            assert g.dx.isfinite().all() and g.dinit.isfinite().all() and not g.dinit[:, :, 1].any()
+            state = c["init"].clone()
+            seq.conv1d_scan_step(c["x"][:, :, 0].contiguous(), torch.zeros(2, 3, device="cuda"), c["A"], c["B"][..., 0].contiguous(),
+                                 c["C"][..., 0].contiguous(), state)
+            assert torch.equal(state, c["init"])
+
+
 def test_lengths_outside_the_tensor_are_brought_into_it(seq):
     gen = _gen(8)
     c = _scan_case(gen, torch.float32, 2, 3, 50, 16, 1)
