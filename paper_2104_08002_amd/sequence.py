@@ -9,8 +9,8 @@ allocated for that stream, and the caller sees to the order between it and the s
 """
 from __future__ import annotations
 
-import ctypes
 import functools
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -22,15 +22,9 @@ SCAN_SOFTPLUS = 1
 MOST_TAPS, MOST_STATES = 8, 64
 
 
-class _Causal(ctypes.Structure):
-    _fields_ = ([(k, ctypes.c_void_p) for k in ("x", "w", "bias", "init", "lengths")] + [(k, ctypes.c_long) for k in ("x_sn", "x_sc")] +
-                [(k, ctypes.c_int) for k in ("N", "C", "L", "S", "dtype", "flags")])
-
-
-class _Scan(ctypes.Structure):
-    _fields_ = ([(k, ctypes.c_void_p) for k in ("x", "dt", "B", "C", "z", "A", "skip", "dt_bias", "init", "lengths")] +
-                [(k, ctypes.c_long) for k in ("x_sn", "x_sd", "dt_sn", "dt_sd", "z_sn", "z_sd", "b_sn", "b_sg", "b_ss", "c_sn", "c_sg", "c_ss")] +
-                [(k, ctypes.c_int) for k in ("N", "D", "L", "S", "G", "dtype", "flags")])
+# conv1d_causal_t and conv1d_scan_t, packed (a ctypes structure takes three times as long to fill)
+_CAUSAL = struct.Struct("5P2l6i")
+_SCAN = struct.Struct("10P12l7i4x")
 
 
 class ScanGrads(NamedTuple):
@@ -91,18 +85,18 @@ def _whole(t, name, shape, dtype, device):
 
 
 def _like(x):
-    return torch.empty_like(x, memory_format=torch.contiguous_format)
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _output(out, x, ins):
     """The caller's `out`, checked, or a new tensor as x."""
     if out is None:
-        return torch.empty_like(x, memory_format=torch.contiguous_format)
+        return _like(x)
     return _apart(_spread(_rows(out, "out", x.shape, x.dtype, x.device), "out"), ins)
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
 def _spread(t, name):
@@ -146,8 +140,8 @@ def _causal(x, w, bias, silu, init, lengths, step=False):
         _whole(init, "init", (N, C, S - 1), t, dev)
     if lengths is not None:
         _whole(lengths, "lengths", (N,), torch.int32, dev)
-    return _Causal(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(init), _ptr(lengths), x.stride(0), 0 if step else x.stride(1), N, C, L, S, code,
-                   CAUSAL_SILU if silu else 0)
+    return _CAUSAL.pack(x.data_ptr(), w.data_ptr(), _ptr(bias), _ptr(init), _ptr(lengths), x.stride(0), 0 if step else x.stride(1), N, C, L, S, code,
+                        CAUSAL_SILU if silu else 0), N, C, L, S
 
 
 @_on_device
@@ -157,10 +151,10 @@ def conv1d_causal_fwd(x, w, bias=None, silu: bool = False, init=None, lengths=No
     init, final [N, C, S - 1]: the inputs before the sequence, and those that the position behind it needs.
     lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there.
     """
-    p = _causal(x, w, bias, silu, init, lengths)
+    p, N, C, _, S = _causal(x, w, bias, silu, init, lengths)
     y = _output(out, x, (x, w, bias, init, lengths))
-    final = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=x.device) if want_final else None
-    binding._check(binding.load().conv1d_causal_fwd(ctypes.byref(p), y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), binding._current_stream()))
+    final = x.new_empty((N, C, S - 1)) if want_final else None
+    binding._check(binding.load().conv1d_causal_fwd(p, y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), binding._current_stream()))
     return (y, final) if want_final else y
 
 
@@ -168,18 +162,18 @@ def conv1d_causal_fwd(x, w, bias=None, silu: bool = False, init=None, lengths=No
 def conv1d_causal_bwd(dy, x, w, bias=None, silu: bool = False, init=None, lengths=None, dfinal=None, want_init: bool = False, workspace=None):
     """(dx, dw, dbias, dinit) of conv1d_causal_fwd(x, w, bias, silu, init, lengths): dx and dinit in x's type, dw [C, S] and dbias [C]
     in float32.  dbias is None without a bias, dinit unless wanted."""
-    p, dev = _causal(x, w, bias, silu, init, lengths), x.device
+    (p, N, C, L, S), dev = _causal(x, w, bias, silu, init, lengths), x.device
     _rows(dy, "dy", x.shape, x.dtype, dev)
     if dfinal is not None:
-        _whole(dfinal, "dfinal", (p.N, p.C, p.S - 1), x.dtype, dev)
+        _whole(dfinal, "dfinal", (N, C, S - 1), x.dtype, dev)
     lib = binding.load()
     if workspace is None:
-        workspace = torch.empty(max(lib.conv1d_causal_bwd_workspace_bytes(p.N, p.C, p.L, p.S), 4), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(lib.conv1d_causal_bwd_workspace_bytes(N, C, L, S) or 4, dtype=torch.uint8, device=dev)
     dx = _like(x)
-    dw = torch.empty((p.C, p.S), dtype=torch.float32, device=dev)
-    db = None if bias is None else torch.empty(p.C, dtype=torch.float32, device=dev)
-    di = torch.empty((p.N, p.C, p.S - 1), dtype=x.dtype, device=dev) if want_init else None
-    binding._check(lib.conv1d_causal_bwd(ctypes.byref(p), dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), dx.data_ptr(), dw.data_ptr(),
+    dw = _like(w) if w.dtype == torch.float32 else torch.empty((C, S), dtype=torch.float32, device=dev)
+    db = None if bias is None else _like(bias)
+    di = x.new_empty((N, C, S - 1)) if want_init else None
+    binding._check(lib.conv1d_causal_bwd(p, dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), dx.data_ptr(), dw.data_ptr(),
                                          _ptr(db), _ptr(di), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                          binding._current_stream()))
     return dx, dw, db, di
@@ -189,10 +183,10 @@ def conv1d_causal_bwd(dy, x, w, bias=None, silu: bool = False, init=None, length
 def conv1d_causal_step(x, w, state, bias=None, silu: bool = False, out=None):
     """y[N, C] for one position x[N, C] of every sequence; state [N, C, S - 1], as conv1d_causal_fwd leaves it in `final`, is
     moved on by that position."""
-    p = _causal(x, w, bias, silu, None, None, step=True)
-    _whole(state, "state", (p.N, p.C, p.S - 1), x.dtype, x.device)
+    p, N, C, _, S = _causal(x, w, bias, silu, None, None, step=True)
+    _whole(state, "state", (N, C, S - 1), x.dtype, x.device)
     y = _output(out, x, (x, w, bias, state))
-    binding._check(binding.load().conv1d_causal_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    binding._check(binding.load().conv1d_causal_step(p, state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
     return y
 
 
@@ -226,9 +220,9 @@ def _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths, step=False)
         _whole(lengths, "lengths", (N,), torch.int32, dev)
     xs, ds, bs, cs = x.stride(), dt.stride(), B.stride(), C.stride()
     zs = (0, 0) if z is None else z.stride()
-    return _Scan(x.data_ptr(), dt.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(z), A.data_ptr(), _ptr(skip), _ptr(dt_bias), _ptr(init), _ptr(lengths),
-                 xs[0], xs[1], ds[0], ds[1], zs[0], zs[1], bs[0], bs[1], bs[2], cs[0], cs[1], cs[2], N, D, L, S, G, code,
-                 SCAN_SOFTPLUS if softplus else 0)
+    return _SCAN.pack(x.data_ptr(), dt.data_ptr(), B.data_ptr(), C.data_ptr(), _ptr(z), A.data_ptr(), _ptr(skip), _ptr(dt_bias), _ptr(init), _ptr(lengths),
+                      xs[0], xs[1], ds[0], ds[1], zs[0], zs[1], bs[0], bs[1], bs[2], cs[0], cs[1], cs[2], N, D, L, S, G, code,
+                      SCAN_SOFTPLUS if softplus else 0), N, D, L, S, G
 
 
 def _scratch(nbytes, device):
@@ -245,14 +239,14 @@ def conv1d_scan_fwd(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: b
     saved: what conv1d_scan_bwd needs of this call, with `save`; None without.
     lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there and the state stays.
     """
-    p, dev = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device
+    (p, N, D, L, S, G), dev = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device
     lib = binding.load()
     y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, init, lengths))
-    final = torch.empty((p.N, p.D, p.S), dtype=torch.float32, device=dev) if want_final else None
-    saved = _scratch(lib.conv1d_scan_saved_bytes(p.N, p.D, p.L, p.S), dev) if save else None
+    final = A.new_empty((N, D, S)) if want_final else None
+    saved = _scratch(lib.conv1d_scan_saved_bytes(N, D, L, S), dev) if save else None
     if workspace is None:
-        workspace = _scratch(lib.conv1d_scan_fwd_workspace_bytes(p.N, p.D, p.L, p.S, p.G), dev)
-    binding._check(lib.conv1d_scan_fwd(ctypes.byref(p), y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), _ptr(saved), _ptr(workspace),
+        workspace = _scratch(lib.conv1d_scan_fwd_workspace_bytes(N, D, L, S, G), dev)
+    binding._check(lib.conv1d_scan_fwd(p, y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), _ptr(saved), _ptr(workspace),
                                        0 if workspace is None else workspace.numel() * workspace.element_size(), binding._current_stream()))
     return y, final, saved
 
@@ -262,18 +256,18 @@ def conv1d_scan_bwd(dy, saved, x, dt, A, B, C, skip=None, z=None, dt_bias=None, 
                     want_init: bool = False, workspace=None) -> ScanGrads:
     """Gradients of the call of conv1d_scan_fwd that had the same arguments and left `saved`: those of x, dt, B, C and z in their
     type, of A, skip, dt_bias and init in float32."""
-    p, dev, t = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device, x.dtype
+    (p, N, D, L, S, G), dev, t = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths), x.device, x.dtype
     lib = binding.load()
     _rows(dy, "dy", x.shape, t, dev)
     if dfinal is not None:
-        _whole(dfinal, "dfinal", (p.N, p.D, p.S), torch.float32, dev)
-    _whole(saved, "saved", (lib.conv1d_scan_saved_bytes(p.N, p.D, p.L, p.S),), torch.uint8, dev)
+        _whole(dfinal, "dfinal", (N, D, S), torch.float32, dev)
+    _whole(saved, "saved", (lib.conv1d_scan_saved_bytes(N, D, L, S),), torch.uint8, dev)
     if workspace is None:
-        workspace = _scratch(lib.conv1d_scan_bwd_workspace_bytes(p.N, p.D, p.L, p.S, p.G), dev)
+        workspace = _scratch(lib.conv1d_scan_bwd_workspace_bytes(N, D, L, S, G), dev)
 
     g = ScanGrads(_like(x), _like(x), _like(A), _like(B), _like(C), None if skip is None else _like(skip), None if z is None else _like(x),
-                  None if dt_bias is None else _like(dt_bias), torch.empty((p.N, p.D, p.S), dtype=torch.float32, device=dev) if want_init else None)
-    binding._check(lib.conv1d_scan_bwd(ctypes.byref(p), dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), saved.data_ptr(), *map(_ptr, g),
+                  None if dt_bias is None else _like(dt_bias), A.new_empty((N, D, S)) if want_init else None)
+    binding._check(lib.conv1d_scan_bwd(p, dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), saved.data_ptr(), *map(_ptr, g),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
                                        binding._current_stream()))
     return g
@@ -283,8 +277,8 @@ def conv1d_scan_bwd(dy, saved, x, dt, A, B, C, skip=None, z=None, dt_bias=None, 
 def conv1d_scan_step(x, dt, A, B, C, state, skip=None, z=None, dt_bias=None, softplus: bool = False, out=None):
     """y[N, D] for one position of every sequence: x, dt, z [N, D], B and C [N, G, S]; state [N, D, S] float32, as conv1d_scan_fwd
     leaves it in `final`, is moved on by that position."""
-    p = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, None, None, step=True)
-    _whole(state, "state", (p.N, p.D, p.S), torch.float32, x.device)
+    p, N, D, _, S, _ = _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, None, None, step=True)
+    _whole(state, "state", (N, D, S), torch.float32, x.device)
     y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, state))
-    binding._check(binding.load().conv1d_scan_step(ctypes.byref(p), state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    binding._check(binding.load().conv1d_scan_step(p, state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
     return y

@@ -4,6 +4,7 @@ import ctypes
 import pytest
 
 from paper_2104_08002_amd import binding, sequence
+from sequence_structs import Causal, Scan
 
 FAKE = 0x10000          # never dereferenced: every call below fails its checks
 EINVAL, EUNSUPPORTED, EWORKSPACE = -1, -2, -3
@@ -17,7 +18,7 @@ def lib():
 def _causal(**kw):
     f = dict(x=FAKE, w=FAKE, bias=None, init=None, lengths=None, x_sn=1000, x_sc=100, N=2, C=3, L=100, S=4, dtype=0, flags=0)
     f.update(kw)
-    return ctypes.byref(sequence._Causal(**f))
+    return ctypes.byref(Causal(**f))
 
 
 @pytest.mark.parametrize("bad,status", [
@@ -55,7 +56,7 @@ def test_causal_refusals_of_outputs(lib):
 def _scan(**kw):
     f = dict(x=FAKE, dt=FAKE, B=FAKE, C=FAKE, z=None, A=FAKE, skip=None, dt_bias=None, init=None, lengths=None, N=2, D=6, L=100, S=16, G=2, dtype=0, flags=1)
     f.update(kw)
-    return ctypes.byref(sequence._Scan(**f))
+    return ctypes.byref(Scan(**f))
 
 
 def _scan_bwd(lib, p, *, dy=FAKE, saved=FAKE, dx=FAKE, dA=FAKE, dskip=None, dz=None, ddt_bias=None, ws=FAKE, ws_bytes=1 << 40):
@@ -136,3 +137,11 @@ def test_tensors_on_the_host_are_refused():
                  lambda: sequence.conv1d_scan_fwd(x, x, w, x, x), lambda: gradients.conv1d_grad_norm([x]), lambda: gradients.conv1d_grad_clip([x], 1.0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_structures_are_packed_as_declared():
+    """The binding packs the structures by itself: the same size and places as a C compiler's."""
+    for packed, declared in ((sequence._CAUSAL, Causal), (sequence._SCAN, Scan)):
+        values = [1000 + i for i in range(len(declared._fields_))]
+        made = declared.from_buffer_copy(packed.pack(*values))
+        assert packed.size == ctypes.sizeof(declared) and [getattr(made, k) for k, _ in declared._fields_] == values

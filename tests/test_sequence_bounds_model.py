@@ -9,6 +9,8 @@ import sys
 
 import pytest
 
+from sequence_structs import Causal, Scan
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, os.path.join(HERE, "hostmodel"))
 
@@ -82,13 +84,11 @@ def _lengths(mem, N, L, kind):
 
 
 def _causal_case(lib, c):
-    from paper_2104_08002_amd import sequence as q
-
     N, C, L, S, dtype, kind, opt, at_end = c
     mem, e = Memory(at_end), 2 if dtype else 4
     x_all = mem.tensor(2 * N * C * L * e, e)
     state = [mem.tensor(N * C * (S - 1) * e, e) if opt and S > 1 else None for _ in range(4)]
-    p = q._Causal(x_all + C * L * e, mem.tensor(C * S * e, e), mem.tensor(4 * C, 4) if opt else None, state[0], _lengths(mem, N, L, kind), 2 * C * L, L,
+    p = Causal(x_all + C * L * e, mem.tensor(C * S * e, e), mem.tensor(4 * C, 4) if opt else None, state[0], _lengths(mem, N, L, kind), 2 * C * L, L,
                   N, C, L, S, dtype, opt)
     y, dy, dx = mem.tensor(N * C * L * e, e), mem.tensor(N * C * L * e, e), mem.tensor(N * C * L * e, e)
     st = lib.conv1d_causal_fwd(ctypes.byref(p), y, C * L, L, state[1], None)
@@ -113,8 +113,6 @@ def test_causal_stays_in_bounds(model):
 
 
 def _scan_case(lib, c):
-    from paper_2104_08002_amd import sequence as q
-
     N, Dg, L, S, G, dtype, kind, opt, at_end = c
     D, mem, e = G * Dg, Memory(at_end), 2 if dtype else 4
     rows = N * D * L * e
@@ -124,7 +122,7 @@ def _scan_case(lib, c):
 
     xz, bc, dt = mem.tensor(2 * rows, e), mem.tensor(2 * N * G * S * L * e, e), mem.tensor(rows, e)
     gate = bool(opt & 1)
-    p = q._Scan(xz, dt, bc, bc + G * S * L * e, xz + D * L * e if gate else None, floats(D * S), floats(D, opt & 2), floats(D, opt & 2),
+    p = Scan(xz, dt, bc, bc + G * S * L * e, xz + D * L * e if gate else None, floats(D * S), floats(D, opt & 2), floats(D, opt & 2),
                 floats(N * D * S, opt & 4), _lengths(mem, N, L, kind), 2 * D * L, L, D * L, L, 2 * D * L, L, 2 * G * S * L, S * L, L, 2 * G * S * L,
                 S * L, L, N, D, L, S, G, dtype, 1)
     y, ns = mem.tensor(rows, e), lib.conv1d_scan_saved_bytes(N, D, L, S)
