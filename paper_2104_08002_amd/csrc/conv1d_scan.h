@@ -204,22 +204,22 @@ template <bool BACK>
 __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const float* sums, const float* first, const float* A, int N, int D,
                                                          int S, int SP, int nseg, int chunks) {
     __shared__ float run_decay[1024], run_add[1024], last[1024];
-    const int per_row = SP * chunks;
-    const long row = static_cast<long>(blockIdx.x) * (blockDim.x / per_row) + threadIdx.x / per_row;
-    const bool there = row < static_cast<long>(N) * D;
+    const unsigned per_row = SP * chunks, row = blockIdx.x * (blockDim.x / per_row) + threadIdx.x / per_row;  // (N D < 2^25)
+    const bool there = row < static_cast<unsigned>(N) * D;
     const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP, base = threadIdx.x - in_row + s;
-    const long n = there ? row / D : 0, d = there ? row - n * D : 0;
+    const unsigned n = there ? row / D : 0, d = there ? row - n * D : 0;
     const float rate = scan_rate(A, S, d, s, there);
-    float h = there && first && s < S ? first[(n * D + d) * S + s] : 0.f;
+    float h = there && first && s < S ? first[static_cast<long>(row) * S + s] : 0.f;
     for (int from = 0; from < nseg; from += kRun * chunks) {
         float f[kRun], v[kRun], decay = 1.f, add = 0.f;
-        const int i0 = from + kRun * chunk;
+        const int i0 = from + kRun * chunk, real = there ? nseg - i0 : 0;  // segments of the run that are there
+        const long at = (static_cast<long>(n) * nseg + (BACK ? nseg - 1 - i0 : i0)) * D + d, next = BACK ? -D : D;
+        const float* sum = sums + at;
+        float* to = value + at * SP + s;
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const bool real = there && i0 + i < nseg;
-            const long at = (n * nseg + (!real ? 0 : BACK ? nseg - 1 - (i0 + i) : i0 + i)) * D + d;
-            f[i] = real ? sums[at] : 0.f;
-            v[i] = real ? value[at * SP + s] : 0.f;
+            f[i] = i < real ? sum[i * next] : 0.f;
+            v[i] = i < real ? to[i * next * SP] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
         for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            if (there && i0 + i < nseg) value[((n * nseg + (BACK ? nseg - 1 - (i0 + i) : i0 + i)) * D + d) * SP + s] = h;
+            if (i < real) to[i * next * SP] = h;
             h = fmaf(f[i], h, v[i]);
         }
         if (from + kRun * chunks >= nseg) break;  // (of the whole workgroup)
