@@ -258,7 +258,7 @@ inline hipError_t scan_join_launch(float* value, const float* sums, const float*
 struct ScanPlan {
     int K, P, waves, blocks_d, nseg, seg_len, chunks;
 };
-ScanPlan scan_plan(int N, int D, int L, int S, int G);
+ScanPlan scan_plan(int N, int D, int L, int S, int G, bool back);
 hipError_t scan_fwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, hipStream_t st);
 hipError_t scan_bwd_launch(const ScanArgs& a, const ScanPlan& p, int bf16, float* dA, float* dskip, float* dbias, hipStream_t st);
 

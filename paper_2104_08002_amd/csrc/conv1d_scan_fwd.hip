@@ -331,7 +331,9 @@ int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; 
 // Segments: as many as give the chip's 1024 SIMDs 8 waves each (2 to 3 turns of what fits beside each other: the turns even out),
 // none shorter than a tile; one where the rows alone do.  A wave alone on its SIMD issues an instruction in 8 clocks, so that
 // few rows want short segments: N = 3, D = 49, L = 4999, S = 5 in FP32 takes 18 us backwards in segments of 16 steps, 39 in 128.
-ScanPlan scan_plan(int N, int D, int L, int S, int G) {
+// Two launches more are worth it from 5 tiles on forwards, 3 backwards (S = 16: a tile takes 4 and 11 us, a cut sequence 14 and
+// 25 in all, and a launch 3 of the host's).
+ScanPlan scan_plan(int N, int D, int L, int S, int G, bool back) {
     ScanPlan p{};
     const int SP = padded_states(S);
     p.K = SP < 16 ? SP / 4 : 4;
@@ -346,7 +348,7 @@ ScanPlan scan_plan(int N, int D, int L, int S, int G) {
     const long tiles = cdiv(L, unit);
     long nseg = room / waves;
     if (nseg > tiles) nseg = tiles;
-    if (nseg < 1) nseg = 1;
+    if (nseg < 1 || tiles < (back ? 3 : 5)) nseg = 1;
     p.seg_len = unit * cdiv(tiles, nseg);
     p.nseg = cdiv(L, p.seg_len);
     return p;
@@ -370,7 +372,7 @@ extern "C" {
 
 size_t conv1d_scan_fwd_workspace_bytes(int N, int D, int L, int S, int G) {
     if (N < 1 || D < 1 || L < 1 || S < 1 || S > kMostStates || G < 1 || D % G) return 0;
-    return split_bytes(N, D, scan_plan(N, D, L, S, G));
+    return split_bytes(N, D, scan_plan(N, D, L, S, G, false));
 }
 
 size_t conv1d_scan_saved_bytes(int N, int D, int L, int S) {
@@ -384,7 +386,7 @@ int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float
     if (!seq_aligned(y, p->dtype == CONV1D_BF16 ? 2 : 4) || !seq_aligned(final, 4) || !seq_aligned(saved, 16) || !seq_aligned(workspace, 256))
         return CONV1D_EINVAL;
     if (!scan_sizes_ok(p)) return CONV1D_EUNSUPPORTED;
-    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G);
+    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G, false);
     const size_t need = split_bytes(p->N, p->D, plan);
     if (need && (!workspace || workspace_bytes < need)) return CONV1D_EWORKSPACE;
     ScanArgs a = scan_args(p, plan);
@@ -398,7 +400,7 @@ int conv1d_scan_fwd(const conv1d_scan_t* p, void* y, long y_sn, long y_sd, float
 
 size_t conv1d_scan_bwd_workspace_bytes(int N, int D, int L, int S, int G) {
     if (N < 1 || D < 1 || L < 1 || S < 1 || S > kMostStates || G < 1 || D % G) return 0;
-    return bwd_space(N, D, L, S, G, scan_plan(N, D, L, S, G)).total;
+    return bwd_space(N, D, L, S, G, scan_plan(N, D, L, S, G, true)).total;
 }
 
 int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_sd, const float* dfinal, const void* saved, void* dx,
@@ -415,7 +417,7 @@ int conv1d_scan_bwd(const conv1d_scan_t* p, const void* dy, long dy_sn, long dy_
         if (!seq_aligned(v, 4)) return CONV1D_EINVAL;
     if (!seq_aligned(saved, 16) || !seq_aligned(workspace, 256)) return CONV1D_EINVAL;
     if (!scan_sizes_ok(p)) return CONV1D_EUNSUPPORTED;
-    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G);
+    const ScanPlan plan = scan_plan(p->N, p->D, p->L, p->S, p->G, true);
     const BwdSpace w = bwd_space(p->N, p->D, p->L, p->S, p->G, plan);
     if (!workspace || workspace_bytes < w.total) return CONV1D_EWORKSPACE;
     char* ws = static_cast<char*>(workspace);

@@ -80,9 +80,9 @@ def test_scan_refusals_of_outputs(lib):
     assert fwd(_scan(), None, 1, 1, None, None, FAKE, 1 << 40, None) == EINVAL
     assert fwd(_scan(), FAKE, 1, 1, None, FAKE + 4, FAKE, 1 << 40, None) == EINVAL          # saved: 16-byte aligned
     assert fwd(_scan(), FAKE, 1, 1, None, None, FAKE + 16, 1 << 40, None) == EINVAL         # workspace: 256-byte aligned
-    need = lib.conv1d_scan_fwd_workspace_bytes(2, 6, 100, 16, 2)
-    assert need > 0 and fwd(_scan(), FAKE, 1, 1, None, None, FAKE, need - 1, None) == EWORKSPACE
-    assert fwd(_scan(), FAKE, 1, 1, None, None, None, 0, None) == EWORKSPACE
+    need = lib.conv1d_scan_fwd_workspace_bytes(2, 6, 1000, 16, 2)
+    assert need > 0 and fwd(_scan(L=1000), FAKE, 1, 1, None, None, FAKE, need - 1, None) == EWORKSPACE
+    assert fwd(_scan(L=1000), FAKE, 1, 1, None, None, None, 0, None) == EWORKSPACE
     assert _scan_bwd(lib, _scan(), dy=None) == EINVAL
     assert _scan_bwd(lib, _scan(), saved=None) == EINVAL
     assert _scan_bwd(lib, _scan(), dA=None) == EINVAL
@@ -101,7 +101,7 @@ def test_scan_sizes(lib):
     assert lib.conv1d_scan_saved_bytes(2, 6, 100, 16) == 4 * 2 * 13 * 6 * 16                # every 8 steps
     assert lib.conv1d_scan_saved_bytes(2, 6, 8, 5) == 4 * 2 * 1 * 6 * 8                     # states padded to 4, 8, 16, 32 or 64
     assert lib.conv1d_scan_fwd_workspace_bytes(64, 2048, 1000, 16, 1) == 0                  # rows enough: not cut
-    assert lib.conv1d_scan_fwd_workspace_bytes(1, 3, 10, 16, 1) == 0                        # one tile
+    assert lib.conv1d_scan_fwd_workspace_bytes(1, 3, 100, 16, 1) == 0                       # a few tiles
     for bad in ((0, 6, 100, 16, 2), (2, 6, 100, 65, 2), (2, 6, 100, 16, 4)):
         assert lib.conv1d_scan_fwd_workspace_bytes(*bad) == 0 and lib.conv1d_scan_bwd_workspace_bytes(*bad) == 0
 
