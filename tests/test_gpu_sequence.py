@@ -379,6 +379,56 @@ def test_same_bits_again_and_on_another_stream(seq):
             assert a is None and b is None or torch.equal(a, b)
 
 
+def test_two_calls_at_once(seq):
+    """On two streams, each with its own outputs and workspaces."""
+    gen = _gen(22)
+    cases = [_scan_case(gen, torch.bfloat16, *shape) for shape in ((2, 70, 700, 16, 1), (1, 9, 2500, 8, 1))]
+    dys = [_normal(gen, *c["x"].shape).bfloat16() for c in cases]
+
+    def run(c, dy, stream=None):
+        y, final, saved = seq.conv1d_scan_fwd(**c, want_final=True, save=True, stream=stream)
+        return [y, final, *seq.conv1d_scan_bwd(dy, saved, **c, stream=stream)]
+
+    want = [run(c, dy) for c, dy in zip(cases, dys)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = [[run(c, dy, st) for c, dy, st in zip(cases, dys, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for turn in got:
+        for a, b in zip(turn, want):
+            assert all(u is None and v is None or torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_more_sums_than_a_launch_has_waves(seq):
+    """8.4 million channels: 42 million sums over samples, one wave each."""
+    gen = _gen(23)
+    N, C, L, S = 2, 8400001, 2, 4
+    x, dy = _normal(gen, N, C, L), _normal(gen, N, C, L)
+    w, bias = _normal(gen, C, S), _normal(gen, C)
+    dx, dw, db, _ = seq.conv1d_causal_bwd(dy, x, w, bias=bias)
+    ref = dy.double().sum((0, 2))
+    assert ((db.double() - ref).abs() <= 4 * U32 * dy.double().abs().sum((0, 2))).all()
+    ref = (dy.double() * x.double()).sum((0, 2))
+    assert ((dw[:, 3].double() - ref).abs() <= 6 * U32 * (dy * x).double().abs().sum((0, 2))).all() and not dw[:, :2].any()
+
+
+def test_expanded_inputs(seq):
+    """One sequence read by every sample, one B by every group: strides of 0."""
+    gen = _gen(24)
+    c = _scan_case(gen, torch.float32, 3, 4, 90, 16, 2)
+    x1, B1 = c["x"][:1], c["B"][:, :1]
+    dy = _normal(gen, 1, 8, 1).expand(3, 8, 90)
+    wide = {**c, "x": x1.expand(3, 8, 90), "B": B1.expand(3, 2, 16, 90)}
+    full = {**c, "x": wide["x"].contiguous(), "B": wide["B"].contiguous()}
+    a, b = (seq.conv1d_scan_fwd(**v, want_final=True, save=True) for v in (wide, full))
+    assert all(torch.equal(u, v) for u, v in zip(a, b))
+    with pytest.raises(ValueError):
+        seq.conv1d_scan_bwd(dy, a[2], **wide)  # (a gradient is contiguous along the sequence)
+    ga, gb = (seq.conv1d_scan_bwd(dy.contiguous(), a[2], **v) for v in (wide, full))
+    assert all(u is None and v is None or torch.equal(u, v) for u, v in zip(ga, gb))
+
+
 def test_captured_and_replayed(seq):
     """Two graphs, of a cut sequence and of another, replayed in turn with eager work between them."""
     gen = _gen(13)
