@@ -16,22 +16,28 @@ namespace {
 __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
 
-// Sums over the channels of a wave, of one value per lane for each of K states and 4 steps, value K step + state.  Every exchange
-// adds a pair of values and leaves each lane one of the two: between the halves of the wave, between its rows of 16, between
-// banks of 4 lanes (P <= 4), between halves of a row (P <= 8); a level that finds a single value adds it in all lanes.  The
-// kSums<K, P> values left are those of sum_value.
+// Sums over the channels of a wave, of one value per lane for each of K states and 4 steps, value K step + state.  Every level
+// adds a pair of values and leaves each lane one of the two; one that finds a single value adds it in all lanes.  Within a row
+// of 16 lanes an addition reads its neighbour's bank and writes some banks only: two instructions a pair, so those levels come
+// first, where the values are most.  Rows and halves of the wave take an exchange, which costs twice an addition, and an addition.
+// (Halves and rows first, banks by selections: 90 issue slots for 4 steps of 4 states, this way 66; the kernel took 4 % longer.)
+// The kSums<K, P> values left are those of sum_value.
 template <int K, int P>
 constexpr int kSums = P <= 4 ? 1 : P == 8 ? K / 2 : K;
 template <int K, int P>
 __device__ __forceinline__ int sum_value(int lane, int j) {
-    const int half = lane >> 5, row = (lane >> 4) & 1, bank = (lane >> 2) & 1, side = (lane >> 3) & 1;
-    if (P <= 4) return K == 4 ? half + 2 * row + 4 * bank + 8 * side : K == 2 ? half + 2 * row + 4 * bank : half + 2 * row;
-    return P == 8 ? half + 2 * row + 4 * side + 8 * j : half + 2 * row + 4 * j;
+    const int half = lane >> 5, row = (lane >> 4) & 1, bank = (lane >> 2) & 3, side = (lane >> 3) & 1;
+    if (P <= 4) return bank + (K > 1 ? 4 * half : 0) + (K > 2 ? 8 * row : 0);
+    return P == 8 ? side + 2 * half + 4 * row + 8 * j : half + 2 * row + 4 * j;
 }
 #ifdef HOSTMODEL
-inline float rows_sum(const float* v) { return v[0]; }
+template <int P>
+inline void four_sums(float* v, float* w, float& sv, float& sw) {
+    sv = v[0];
+    sw = w[0];
+}
 template <int K, int P>
-inline void row_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
+inline void step_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
     for (float& o : out) o = q[0];
 }
 #else
@@ -43,30 +49,66 @@ __device__ __forceinline__ float swap16_add(float u, float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(u), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-// v in the banks (4 lanes each) of MASK, u in the others
-template <int MASK>
-__device__ __forceinline__ float by_bank(float u, float v) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(u), __float_as_int(v), 0xE4, 0xf, MASK, false));
-}
-// u of a lane's own and the other bank of a pair in the banks outside MASK, v in those of MASK; CTRL brings the other bank's
-template <int CTRL, int MASK>
-__device__ __forceinline__ float pair_sum(float u, float v) {
-    const float other = by_bank<MASK>(v, u);
-    return by_bank<MASK>(u, v) + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(other), CTRL, 0xf, 0xf, true));
-}
-// four values over the rows of the wave
-__device__ __forceinline__ float rows_sum(const float* v) { return swap16_add(swap32_add(v[0], v[1]), swap32_add(v[2], v[3])); }
-// K of those over the channels within a row
-template <int K, int P>
-__device__ __forceinline__ void row_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
-    // row_ror:4 pairs every bank with the one before it, row_ror:8 with the one after the next: all four in two steps
+// Four values each of v and w: over the four banks of a row (P <= 4; bank b is left with value b: row_ror:4 adds to every bank
+// the one before it, row_ror:8 the two before those), over its two sides (P = 8) and the halves of the wave, over rows and
+// halves (P = 16).  A vector instruction's result may be read from another lane two wait states later: the pairs of v and w
+// alternate, and the ends, whose neighbours the compiler places, wait.
+template <int P>
+__device__ __forceinline__ void four_sums(float* v, float* w, float& sv, float& sw) {
     if constexpr (P <= 4) {
-        if constexpr (K == 4) out[0] = pair_sum<0x128, 0xC>(pair_sum<0x124, 0xA>(q[0], q[1]), pair_sum<0x124, 0xA>(q[2], q[3]));
-        if constexpr (K == 2) out[0] = add_dpp<0x128>(pair_sum<0x124, 0xA>(q[0], q[1]));
-        if constexpr (K == 1) out[0] = add_dpp<0x128>(add_dpp<0x124>(q[0]));
+        float a = v[0], b = v[2], c = w[0], d = w[2];
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %2, %2 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %3, %3, %3 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %4, %4 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+            "v_add_f32_dpp %2, %6, %6 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+            "v_add_f32_dpp %1, %5, %5 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+            "v_add_f32_dpp %3, %7, %7 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "v_add_f32_dpp %2, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "s_nop 1"
+            : "+&v"(a), "+&v"(b), "+&v"(c), "+&v"(d)
+            : "v"(v[1]), "v"(v[3]), "v"(w[1]), "v"(w[3]));
+        sv = a;
+        sw = c;
+    } else if constexpr (P == 8) {
+        float a = v[0], b = v[2], c = w[0], d = w[2];
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %3, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %4, %4 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "v_add_f32_dpp %2, %6, %6 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "v_add_f32_dpp %1, %5, %5 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "v_add_f32_dpp %3, %7, %7 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "s_nop 1"
+            : "+&v"(a), "+&v"(b), "+&v"(c), "+&v"(d)
+            : "v"(v[1]), "v"(v[3]), "v"(w[1]), "v"(w[3]));
+        sv = swap32_add(a, b);
+        sw = swap32_add(c, d);
+    } else {
+        sv = swap16_add(swap32_add(v[0], v[1]), swap32_add(v[2], v[3]));
+        sw = swap16_add(swap32_add(w[0], w[1]), swap32_add(w[2], w[3]));
+    }
+}
+// the K of those that 4 steps have, over the rest of the wave
+template <int K, int P>
+__device__ __forceinline__ void step_sums(const float (&q)[K], float (&out)[kSums<K, P>]) {
+    if constexpr (P <= 4) {
+        if constexpr (K == 4) {
+            out[0] = swap16_add(swap32_add(q[0], q[1]), swap32_add(q[2], q[3]));
+        } else {
+            const float v = swap32_add(q[0], q[K - 1]);
+            out[0] = swap16_add(v, v);
+        }
     } else if constexpr (P == 8) {
 #pragma unroll
-        for (int i = 0; i < K / 2; ++i) out[i] = pair_sum<0x128, 0xC>(q[2 * i], q[2 * i + 1]);
+        for (int i = 0; i < K / 2; ++i) out[i] = swap16_add(q[2 * i], q[2 * i + 1]);
     } else {
 #pragma unroll
         for (int i = 0; i < K; ++i) out[i] = q[i];
@@ -330,14 +372,11 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
                     out_y[i] = y;
                     out_x[i] = gb * e[i];
                     out_e[i] = fmaf(gb, x[i], qa * (1.f / kLog2e));
-                    if (K * i % 4 == 0) {  // four values are there
-                        qB[K * i / 4] = rows_sum(vB + K * i);
-                        qC[K * i / 4] = rows_sum(vC + K * i);
-                    }
+                    if (K * i % 4 == 0) four_sums<P>(vB + K * i, vC + K * i, qB[K * i / 4], qC[K * i / 4]);
                 }
                 float out_B[kSums<K, P>], out_C[kSums<K, P>];
-                row_sums<K, P>(qB, out_B);
-                row_sums<K, P>(qC, out_C);
+                step_sums<K, P>(qB, out_B);
+                step_sums<K, P>(qC, out_C);
 #pragma unroll
                 for (int i = 0; i < kSums<K, P>; ++i) {
                     const int value = sum_value<K, P>(lane, i), to = (K * p + value % K) * R::RS + t + j + value / K;
