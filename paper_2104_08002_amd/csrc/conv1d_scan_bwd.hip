@@ -16,6 +16,13 @@ namespace {
 __device__ __forceinline__ void reload_lds() { asm volatile("" ::: "memory"); }
 
 
+template <int K>
+__device__ __forceinline__ void load_states(const float* from, float (&v)[K]) {
+    const States<K> s = states_at<K>(from);
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = s[k];
+}
+
 // Sums over the channels of a wave, of one value per lane for each of K states and 4 steps, value K step + state.  Every level
 // adds a pair of values and leaves each lane one of the two; one that finds a single value adds it in all lanes.  Within a row
 // of 16 lanes an addition reads its neighbour's bank and writes some banks only: two instructions a pair, so those levels come
@@ -302,6 +309,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         else if (a.dfinal && there && s < a.S) carry[k] = a.dfinal[(at.n * a.D + d) * a.S + s];
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
+    // the states that the forward pass kept, from the segment's last; each is loaded while the steps behind it are walked
+    const float* kept_at = a.saved + ((at.n * a.chunks + (t_end - 1) / kSub) * a.D + d) * SP + K * p;
+    float next[K] = {};
+    if (there) load_states<K>(kept_at, next);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
         const bool inside = t0 + T <= len && full;
         states.begin(t0, len);
@@ -316,12 +327,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             if (t0 + t >= a.L) continue;
             float first[K], h[kSub][K], decay[kSub][K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) first[k] = 0.f;
-            if (there) {
-                const States<K> v = states_at<K>(a.saved + ((at.n * a.chunks + (t0 + t) / kSub) * a.D + d) * SP + K * p);
-#pragma unroll
-                for (int k = 0; k < K; ++k) first[k] = v[k];
-            }
+            for (int k = 0; k < K; ++k) first[k] = next[k];
 #pragma unroll
             for (int j = 0; j < kSub; j += 4) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -340,6 +346,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
 #pragma unroll
             for (int j = kSub - 4; j >= 0; j -= 4) {
                 reload_lds();
+                if (j == 0 && there && t0 + t > t_begin) {
+                    kept_at -= static_cast<long>(a.D) * SP;
+                    load_states<K>(kept_at, next);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 const scan_f32x4 e = *reinterpret_cast<const scan_f32x4*>(e_row + t + j), x = *reinterpret_cast<const scan_f32x4*>(x_row + t + j),
                                  dy = *reinterpret_cast<const scan_f32x4*>(dy_row + t + j);
