@@ -27,8 +27,8 @@ struct ScanArgs {
     void* out;
     float* final;      // [N][D][S] or nullptr
     float* saved;      // [N][chunks][D][K P]: the state before every kSub-th step, or nullptr
-    float* starts;     // [N][nseg][D][K P]: state before each segment (split only)
-    float* sums;       // [N][nseg][D]: sum of e over each segment
+    float* starts;     // [N][D][nseg][K P]: state before each segment (split only)
+    float* sums;       // [N][D][nseg]: sum of e over each segment
     int N, D, L, S, G, Dg, softplus;
     long x_sn, x_sd, dt_sn, dt_sd, z_sn, z_sd, out_sn, out_sd;
     long b_sn, b_sg, b_ss, c_sn, c_sg, c_ss;
@@ -43,7 +43,7 @@ struct ScanArgs {
     void *dx, *ddt, *dz, *dB, *dC;   // contiguous, in the type of x
     float* part_bc;    // [2][blocks_d][N][G][S][L]: sums over a workgroup's channels (blocks_d > 1)
     float* part_p;     // [N * nseg][D * (K P + 2)]: what a segment adds to the gradients of A, then of skip, then of dt_bias
-    float* carries;    // [N][nseg][D][K P]: what the later segments send into each (split only)
+    float* carries;    // [N][D][nseg][K P]: what the later segments send into each (split only)
     float* dinit;      // [N][D][S] or nullptr
 };
 
@@ -199,7 +199,10 @@ __device__ __forceinline__ void lds_get8(const float* from, float (&v)[8]) {
 // One (sample, channel) row of segment values joined along the sequence: value[seg] holds what a segment adds, and becomes
 // what comes into it from the segments before (BACK: behind) it, `first` into the first; sums[seg]: exp(A sum) is a segment's
 // decay.  SP states times `chunks` runs of kRun segments at a time: a run is joined in registers, the runs through LDS.
-constexpr int kRun = 8;
+// Bound by latency and by how much of every line it uses, so that a row's segments lie together: N = 8, D = 128 in 125 segments
+// takes 6.0 us, 9.8 with the channels of a segment together.  Runs of 16 join up to 1024 segments of 16 states at once (N = 1,
+// D = 128 in 938: 6.6 us, 8.8 with runs of 8, which are no faster at fewer).
+constexpr int kRun = 16;
 template <bool BACK>
 __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const float* sums, const float* first, const float* A, int N, int D,
                                                          int S, int SP, int nseg, int chunks) {
@@ -207,19 +210,21 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
     const unsigned per_row = SP * chunks, row = blockIdx.x * (blockDim.x / per_row) + threadIdx.x / per_row;  // (N D < 2^25)
     const bool there = row < static_cast<unsigned>(N) * D;
     const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP, base = threadIdx.x - in_row + s;
-    const unsigned n = there ? row / D : 0, d = there ? row - n * D : 0;
+    const unsigned d = there ? row % D : 0;
     const float rate = scan_rate(A, S, d, s, there);
     float h = there && first && s < S ? first[static_cast<long>(row) * S + s] : 0.f;
     for (int from = 0; from < nseg; from += kRun * chunks) {
         float f[kRun], v[kRun], decay = 1.f, add = 0.f;
         const int i0 = from + kRun * chunk, real = there ? nseg - i0 : 0;  // segments of the run that are there
-        const long at = (static_cast<long>(n) * nseg + (BACK ? nseg - 1 - i0 : i0)) * D + d, next = BACK ? -D : D;
+        const long at = static_cast<long>(row) * nseg + (BACK ? nseg - 1 - i0 : i0);
+        constexpr int next = BACK ? -1 : 1;
+        const int step = next * SP;
         const float* sum = sums + at;
         float* to = value + at * SP + s;
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             f[i] = i < real ? sum[i * next] : 0.f;
-            v[i] = i < real ? to[i * next * SP] : 0.f;
+            v[i] = i < real ? to[i * step] : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
@@ -234,7 +239,7 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
         for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            if (i < real) to[i * next * SP] = h;
+            if (i < real) to[i * step] = h;
             h = fmaf(f[i], h, v[i]);
         }
         if (from + kRun * chunks >= nseg) break;  // (of the whole workgroup)

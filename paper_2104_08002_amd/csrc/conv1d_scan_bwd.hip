@@ -274,7 +274,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
         __syncthreads();
     }
     if (!there) return;
-    const long i = (at.n * a.nseg + at.seg) * a.D + d;
+    const long i = (at.n * a.D + d) * a.nseg + at.seg;
     put_states<K>(a.carries + i * SP + K * p, carry);
     if (p == 0) a.sums[i] = sum;
 }
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
         rate[k] = scan_rate(a.A, a.S, d, s, there);
         dA[k] = 0.f;
         carry[k] = 0.f;
-        if (a.nseg > 1) carry[k] = there ? a.carries[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
+        if (a.nseg > 1) carry[k] = there ? a.carries[((at.n * a.D + d) * a.nseg + at.seg) * SP + s] : 0.f;
         else if (a.dfinal && there && s < a.S) carry[k] = a.dfinal[(at.n * a.D + d) * a.S + s];
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);

@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
         rate[k] = scan_rate(a.A, a.S, d, s, there);
         h[k] = 0.f;
         if (ENDS) continue;
-        if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.nseg + at.seg) * a.D + d) * SP + s] : 0.f;
+        if (a.nseg > 1) h[k] = there ? a.starts[((at.n * a.D + d) * a.nseg + at.seg) * SP + s] : 0.f;
         else if (a.init && there && s < a.S) h[k] = a.init[(at.n * a.D + d) * a.S + s];
     }
     FwdRow<BF16, P, T, ENDS> row(a, at, base, lane);
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     }
     if (!there) return;
     if (ENDS) {
-        const long i = (at.n * a.nseg + at.seg) * a.D + d;
+        const long i = (at.n * a.D + d) * a.nseg + at.seg;
         put_states<K>(a.starts + i * SP + K * p, h);
         if (p == 0) a.sums[i] = sum;
     } else if (a.final && at.seg == a.nseg - 1) {
