@@ -95,9 +95,12 @@ def test_training_step(ops, dtype, N, L, ragged):
     before = {k: v.grad.clone() for k, v in p.items()}
     got = ops[2].conv1d_grad_clip([v.grad for v in p.values()], 0.25)
     assert abs(float(got) - float(norm)) <= 2.0 ** -23 * float(norm)
+    # the norm is rounded to float (2^-24), so is the factor, and the product to the gradient's type (eps / 2): in float 3 2^-24,
+    # more than the eps of 2 2^-24 that stood here
+    bound = lambda t: 1.01 * (torch.finfo(t).eps / 2 + 2 * 2.0 ** -24)  # noqa: E731
     for k, v in p.items():
         want = before[k].double() * min(1.0, 0.25 / (float(norm) + 1e-6))
-        assert ((v.grad.double() - want).abs() <= torch.finfo(v.dtype).eps * want.abs() + 1e-37).all(), k
+        assert ((v.grad.double() - want).abs() <= bound(v.dtype) * want.abs() + 1e-37).all(), k
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
