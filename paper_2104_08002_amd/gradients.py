@@ -9,6 +9,7 @@ import array
 import math
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding
 
@@ -55,6 +56,8 @@ class _Tensors:
         lib = binding.load()
         if workspace is None:
             workspace = torch.empty(max(lib.conv1d_grad_norm_workspace_bytes(*self.args[1::2]), 8), dtype=torch.uint8, device=self.device)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous, on the device of the gradients")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
         binding._check(lib.conv1d_grad_norm(*self.args, kind, norm.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                             binding._current_stream()))
@@ -97,6 +100,7 @@ def conv1d_grad_clip(grads, max_norm: float, norm_type: float = 2.0, norm=None, 
         elif total.dtype != torch.float32 or total.numel() != 1 or total.device != t.device:
             raise ValueError("norm must be a float32 scalar on the gradients' device")
         binding._check(binding.load().conv1d_grad_clip(*t.args, total.data_ptr(), max_norm, binding._current_stream()))
+        increment_version(t.grads)
         return total
 
     return _run(grads, stream, fn)

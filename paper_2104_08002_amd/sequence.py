@@ -14,6 +14,7 @@ import struct
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding
 
@@ -92,7 +93,21 @@ def _output(out, x, ins):
     """The caller's `out`, checked, or a new tensor as x."""
     if out is None:
         return _like(x)
-    return _apart(_spread(_rows(out, "out", x.shape, x.dtype, x.device), "out"), ins)
+    increment_version(_apart(_spread(_rows(out, "out", x.shape, x.dtype, x.device), "out"), ins))
+    return out
+
+
+def _room(workspace, nbytes, device):
+    """The caller's workspace, checked (its size by the call), or a new one; None for no bytes."""
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the device of the tensors")
+    return workspace
+
+
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _ptr(t):
@@ -167,15 +182,13 @@ def conv1d_causal_bwd(dy, x, w, bias=None, silu: bool = False, init=None, length
     if dfinal is not None:
         _whole(dfinal, "dfinal", (N, C, S - 1), x.dtype, dev)
     lib = binding.load()
-    if workspace is None:
-        workspace = torch.empty(lib.conv1d_causal_bwd_workspace_bytes(N, C, L, S) or 4, dtype=torch.uint8, device=dev)
+    workspace = _room(workspace, lib.conv1d_causal_bwd_workspace_bytes(N, C, L, S), dev)
     dx = _like(x)
     dw = _like(w) if w.dtype == torch.float32 else torch.empty((C, S), dtype=torch.float32, device=dev)
     db = None if bias is None else _like(bias)
     di = x.new_empty((N, C, S - 1)) if want_init else None
     binding._check(lib.conv1d_causal_bwd(p, dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), dx.data_ptr(), dw.data_ptr(),
-                                         _ptr(db), _ptr(di), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                         binding._current_stream()))
+                                         _ptr(db), _ptr(di), _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return dx, dw, db, di
 
 
@@ -187,6 +200,7 @@ def conv1d_causal_step(x, w, state, bias=None, silu: bool = False, out=None):
     _whole(state, "state", (N, C, S - 1), x.dtype, x.device)
     y = _output(out, x, (x, w, bias, state))
     binding._check(binding.load().conv1d_causal_step(p, state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    increment_version(state)
     return y
 
 
@@ -225,10 +239,6 @@ def _scan(x, dt, A, B, C, skip, z, dt_bias, softplus, init, lengths, step=False)
                       SCAN_SOFTPLUS if softplus else 0), N, D, L, S, G
 
 
-def _scratch(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
 @_on_device
 def conv1d_scan_fwd(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool = False, init=None, lengths=None, want_final: bool = False,
                     save: bool = False, out=None, workspace=None):
@@ -243,11 +253,10 @@ def conv1d_scan_fwd(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: b
     lib = binding.load()
     y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, init, lengths))
     final = A.new_empty((N, D, S)) if want_final else None
-    saved = _scratch(lib.conv1d_scan_saved_bytes(N, D, L, S), dev) if save else None
-    if workspace is None:
-        workspace = _scratch(lib.conv1d_scan_fwd_workspace_bytes(N, D, L, S, G), dev)
+    saved = _room(None, lib.conv1d_scan_saved_bytes(N, D, L, S), dev) if save else None
+    workspace = _room(workspace, lib.conv1d_scan_fwd_workspace_bytes(N, D, L, S, G), dev)
     binding._check(lib.conv1d_scan_fwd(p, y.data_ptr(), y.stride(0), y.stride(1), _ptr(final), _ptr(saved), _ptr(workspace),
-                                       0 if workspace is None else workspace.numel() * workspace.element_size(), binding._current_stream()))
+                                       _bytes(workspace), binding._current_stream()))
     return y, final, saved
 
 
@@ -262,14 +271,11 @@ def conv1d_scan_bwd(dy, saved, x, dt, A, B, C, skip=None, z=None, dt_bias=None, 
     if dfinal is not None:
         _whole(dfinal, "dfinal", (N, D, S), torch.float32, dev)
     _whole(saved, "saved", (lib.conv1d_scan_saved_bytes(N, D, L, S),), torch.uint8, dev)
-    if workspace is None:
-        workspace = _scratch(lib.conv1d_scan_bwd_workspace_bytes(N, D, L, S, G), dev)
-
+    workspace = _room(workspace, lib.conv1d_scan_bwd_workspace_bytes(N, D, L, S, G), dev)
     g = ScanGrads(_like(x), _like(x), _like(A), _like(B), _like(C), None if skip is None else _like(skip), None if z is None else _like(x),
                   None if dt_bias is None else _like(dt_bias), A.new_empty((N, D, S)) if want_init else None)
     binding._check(lib.conv1d_scan_bwd(p, dy.data_ptr(), dy.stride(0), dy.stride(1), _ptr(dfinal), saved.data_ptr(), *map(_ptr, g),
-                                       _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                       binding._current_stream()))
+                                       _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return g
 
 
@@ -281,4 +287,5 @@ def conv1d_scan_step(x, dt, A, B, C, state, skip=None, z=None, dt_bias=None, sof
     _whole(state, "state", (N, D, S), torch.float32, x.device)
     y = _output(out, x, (x, dt, A, B, C, skip, z, dt_bias, state))
     binding._check(binding.load().conv1d_scan_step(p, state.data_ptr(), y.data_ptr(), y.stride(0), binding._current_stream()))
+    increment_version(state)
     return y

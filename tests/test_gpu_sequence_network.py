@@ -138,6 +138,37 @@ def test_prompt_then_positions(ops, dtype):
             at += 1
 
 
+def test_what_is_written_in_place_is_known_to_autograd(ops):
+    """A state that a graph keeps and that is then moved on, a gradient that a graph keeps and that is then clipped: refused, not wrong."""
+    autograd, sequence, gradients = ops
+    gen = _gen(8)
+    N, D, L, S = 2, 3, 5, 4
+    new = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+    x, A, B, w = new(N, D, L).requires_grad_(True), -torch.rand(D, S, generator=gen, device="cuda"), new(N, 1, S, L), new(D, S)
+    state, before = new(N, D, S), new(N, D, S - 1)
+    y = autograd.conv1d_scan(x, x, A, B, B, init=state)
+    sequence.conv1d_scan_step(x[:, :, 0].detach().contiguous(), x[:, :, 0].detach().contiguous(), A, B[..., 0].contiguous(), B[..., 0].contiguous(), state)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    y = autograd.conv1d_causal(x, w, init=before)
+    sequence.conv1d_causal_step(x[:, :, 0].detach().contiguous(), w, before)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    g = new(4)
+    y = (x[0, 0, :4] * g).sum()
+    gradients.conv1d_grad_clip([g], 0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    out, seen = new(N, D, L), new(N, D, L).requires_grad_(True)
+    y = (seen * out).sum()
+    sequence.conv1d_causal_fwd(x.detach(), w, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():
+        sequence.conv1d_causal_step(new(N, D), w, new(N, D, S - 1))
+        gradients.conv1d_grad_clip([new(4)], 0.1)
+
+
 def test_autograd_of_broadcast_and_unusual_inputs(ops):
     """An input expanded over the batch, a transposed one, a gradient that is expanded, parameters in other types, only some inputs
     that want a gradient."""

@@ -139,6 +139,17 @@ def test_tensors_on_the_host_are_refused():
             call()
 
 
+def test_workspaces_elsewhere_are_refused():
+    import torch
+
+    room, here, there = sequence._room, torch.device("cpu"), torch.device("meta")
+    assert room(None, 0, here) is None and room(None, 8, here).numel() == 8
+    assert sequence._bytes(room(torch.empty(3), 8, here)) == 12
+    for bad in (torch.empty(64, device=there), torch.empty(8, 8)[:, 0]):
+        with pytest.raises(ValueError):
+            room(bad, 8, here)
+
+
 def test_structures_are_packed_as_declared():
     """The binding packs the structures by itself: the same size and places as a C compiler's."""
     for packed, declared in ((sequence._CAUSAL, Causal), (sequence._SCAN, Scan)):
