@@ -141,12 +141,12 @@ class ScanFunction(torch.autograd.Function):
     """(y, final) of sequence.conv1d_scan_fwd; its gradients are not differentiable again."""
 
     @staticmethod
-    def forward(ctx, x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus: bool, want_final: bool):
+    def forward(ctx, x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus: bool, want_final: bool, graph: bool):
         x, dt, B, C, z = (_along(t) for t in (x, dt, B, C, z))
         ctx.types = [None if t is None else t.dtype for t in (A, skip, dt_bias, init)]
         A, skip, dt_bias, init = (None if t is None else t.contiguous().float() for t in (A, skip, dt_bias, init))
         y, final, saved = sequence.conv1d_scan_fwd(x, dt, A, B, C, skip=skip, z=z, dt_bias=dt_bias, softplus=softplus, init=init,
-                                                   lengths=lengths, want_final=want_final, save=any(ctx.needs_input_grad))
+                                                   lengths=lengths, want_final=want_final, save=graph and any(ctx.needs_input_grad))
         ctx.save_for_backward(x, dt, A, B, C, skip, z, dt_bias, init, lengths, saved)
         ctx.softplus = softplus
         ctx.set_materialize_grads(False)
@@ -161,10 +161,11 @@ class ScanFunction(torch.autograd.Function):
         g = sequence.conv1d_scan_bwd(gy, saved, x, dt, A, B, C, skip=skip, z=z, dt_bias=dt_bias, softplus=ctx.softplus, init=init,
                                      lengths=lengths, dfinal=gfinal, want_init=init is not None)
         dA, dskip, ddt_bias, dinit = (None if v is None else v.to(t) for v, t in zip((g.dA, g.dskip, g.ddt_bias, g.dinit), ctx.types))
-        return g.dx, g.ddt, dA, g.dB, g.dC, dskip, g.dz, ddt_bias, dinit, None, None, None
+        return g.dx, g.ddt, dA, g.dB, g.dC, dskip, g.dz, ddt_bias, dinit, None, None, None, None
 
 
 def conv1d_scan(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool = False, init=None, lengths=None, want_final: bool = False):
     """y[N, D, L] of the selective scan (sequence.conv1d_scan_fwd); (y, final) with want_final."""
-    y, final = ScanFunction.apply(x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus, want_final)
+    # (a parameter wants a gradient under no_grad too, as far as forward can see: the states are kept for a graph alone)
+    y, final = ScanFunction.apply(x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus, want_final, torch.is_grad_enabled())
     return (y, final) if want_final else y

@@ -138,6 +138,27 @@ def test_prompt_then_positions(ops, dtype):
             at += 1
 
 
+def test_states_are_kept_for_a_graph_alone(ops):
+    autograd, sequence, _ = ops
+    gen = _gen(9)
+    N, D, L, S = 2, 64, 4096, 16
+    new = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")  # noqa: E731
+    x, A, B = new(N, D, L), (-torch.rand(D, S, generator=gen, device="cuda")).requires_grad_(True), new(N, 1, S, L)
+    saved = sequence.conv1d_scan_fwd(x, x, A.detach(), B, B, softplus=True, save=True)[2].numel()
+
+    def most(fn):
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        out = fn()
+        return torch.cuda.max_memory_allocated() - before, out
+
+    with_graph, y = most(lambda: autograd.conv1d_scan(x, x, A, B, B, softplus=True))
+    with torch.no_grad():
+        without, y0 = most(lambda: autograd.conv1d_scan(x, x, A, B, B, softplus=True))
+    assert y.requires_grad and not y0.requires_grad and torch.equal(y, y0)
+    assert with_graph - without >= saved - 4096
+
+
 def test_what_is_written_in_place_is_known_to_autograd(ops):
     """A state that a graph keeps and that is then moved on, a gradient that a graph keeps and that is then clipped: refused, not wrong."""
     autograd, sequence, gradients = ops
