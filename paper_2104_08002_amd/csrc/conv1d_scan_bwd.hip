@@ -146,16 +146,16 @@ struct BackRow {
         z = a.z ? scan_row<BF16>(a.z, a.z_sn, a.z_sd, p.n, d) : nullptr;
         bias = a.dt_bias ? a.dt_bias[d] : 0.f;
     }
-    // e, dy and (WITH_X) x of the tile at t0 into LDS.  INSIDE: it lies within the sequence, the wave's channels are all there.
+    // e, dy and (WITH_X) x of the tile at t0 into LDS.  INSIDE: it lies within the sequence.  A lane without a channel (there are
+    // some if not `full`) goes along with the group's first, without a gradient: it adds nothing to the sums over channels.
     template <bool INSIDE, bool WITH_X>
-    __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, float* sE, float* sX, float* sY) const {
-        const int end = real ? len : 0;
+    __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, bool full, float* sE, float* sX, float* sY) const {
         if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
         float v[8], g[8], u[8], w[8];
-        scan_load8<BF16, INSIDE>(dt, t0 + c, end, v);
-        scan_load8<BF16, INSIDE>(dout, t0 + c, end, g);
-        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, end, w);
-        if (WITH_X) scan_load8<BF16, INSIDE>(x, t0 + c, end, u);
+        scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
+        scan_load8<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
+        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
+        if (WITH_X) scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += bias;
         if (a.softplus) {
@@ -164,12 +164,16 @@ struct BackRow {
         }
         if (!INSIDE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < end ? v[i] : 0.f;
+            for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < len ? v[i] : 0.f;
         }
         lds_put8(sE + at, v);
         if (z) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] *= w[i] * sigmoid_of(w[i]);
+        }
+        if (!full) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = real ? g[i] : 0.f;
         }
         lds_put8(sY + at, g);
         if (WITH_X) lds_put8(sX + at, u);
@@ -183,10 +187,10 @@ struct BackRow {
         const int end = INSIDE ? t0 + c + 8 : a.L;
         const float skip = a.skip ? a.skip[d] : 0.f;
         float u[8], v[8], g[8], w[8];
-        scan_load8<BF16, INSIDE>(x, t0 + c, len, u);
-        scan_load8<BF16, INSIDE>(dout, t0 + c, len, g);
-        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, w);
-        if (a.softplus) scan_load8<BF16, INSIDE>(dt, t0 + c, len, v);
+        scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
+        scan_load8<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
+        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
+        if (a.softplus) scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
         if (z) {
             float y[8];
             lds_get8(sY + at, y);
@@ -235,11 +239,11 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
     const int p = lane & (P - 1), cl = lane / P;
     const int len = seq_length(a.lengths, at.n, a.L);
     const int base = (at.cb * waves + wave) * R::CW;
-    const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
+    const bool there = base + cl < a.Dg;
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
     const BackRow<BF16, P, T> line(a, at, base, lane);
     using E = typename RowElem<BF16>::type;
-    ScanStates<BF16, SP, T, false> states{static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, nullptr, a.c_ss, 0, a.S, {}};
+    ScanStates<BF16, SP, T, false> states{static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, nullptr, a.c_ss, 0, a.S, a.L, {}};
     float rate[K], carry[K], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -247,11 +251,13 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_adjoint_kernel(S
         carry[k] = 0.f;
     }
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
-    for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
+    const int t_last = t_begin + (t_end - 1 - t_begin) / T * T;
+    for (int t0 = t_last; t0 >= t_begin; t0 -= T) {
         states.begin(t0, len);
-        if (t0 + T <= len && full) line.template stage<true, false>(a, t0, len, sE[wave], nullptr, sY[wave]);
-        else line.template stage<false, false>(a, t0, len, sE[wave], nullptr, sY[wave]);
+        if (t0 + T <= len) line.template stage<true, false>(a, t0, len, true, sE[wave], nullptr, sY[wave]);
+        else line.template stage<false, false>(a, t0, len, true, sE[wave], nullptr, sY[wave]);
         states.finish(t0, len, sC, nullptr);
+        if (t0 == t_last) make_rates(rate);
         __syncthreads();
         const float *e_row = sE[wave] + cl * R::RS, *dy_row = sY[wave] + cl * R::RS;
 #pragma unroll 1
@@ -297,12 +303,12 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     const BackRow<BF16, P, T> line(a, at, base, lane);
     using E = typename RowElem<BF16>::type;
     ScanStates<BF16, SP, T, true> states{static_cast<const E*>(a.B) + at.n * a.b_sn + at.g * a.b_sg,
-                                         static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, {}};
+                                         static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, a.L, {}};
     float rate[K], carry[K], dA[K], dskip = 0.f, dbias = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int s = K * p + k;
-        rate[k] = scan_rate(a.A, a.S, d, s, there);
+        rate[k] = rate_of(scan_rate(a.A, a.S, d, s, there));
         dA[k] = 0.f;
         carry[k] = 0.f;
         if (a.nseg > 1) carry[k] = there ? a.carries[((at.n * a.D + d) * a.nseg + at.seg) * SP + s] : 0.f;
@@ -314,10 +320,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
     float next[K] = {};
     if (there) load_states<K>(kept_at, next);
     for (int t0 = t_begin + (t_end - 1 - t_begin) / T * T; t0 >= t_begin; t0 -= T) {
-        const bool inside = t0 + T <= len && full;
+        const bool inside = t0 + T <= len;
         states.begin(t0, len);
-        if (inside) line.template stage<true, true>(a, t0, len, sE[wave], sX[wave], sY[wave]);
-        else line.template stage<false, true>(a, t0, len, sE[wave], sX[wave], sY[wave]);
+        if (inside) line.template stage<true, true>(a, t0, len, full, sE[wave], sX[wave], sY[wave]);
+        else line.template stage<false, true>(a, t0, len, full, sE[wave], sX[wave], sY[wave]);
         states.finish(t0, len, sB, sC);
         __syncthreads();
         float dA_tile[K] = {};

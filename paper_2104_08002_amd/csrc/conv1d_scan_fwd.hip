@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The lane's row of a tile.  INSIDE: the tile lies within the sequence, the wave's channels are all there: no masks.
+// The lane's row of a tile.  INSIDE: the tile lies within the sequence: no masks.
 template <bool BF16, int P, int T, bool ENDS>
 struct FwdRow {
     using R = ScanRows<P, T>;
@@ -38,12 +38,11 @@ struct FwdRow {
     // e and e x into LDS
     template <bool INSIDE>
     __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, float* sE, float* sX) {
-        const int end = real ? len : 0;
         if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
         float e[8], ex[8];
-        scan_load8<BF16, INSIDE>(x, t0 + c, end, u);
-        scan_load8<BF16, INSIDE>(dt, t0 + c, end, e);
-        if (!ENDS && z) scan_load8<BF16, INSIDE>(z, t0 + c, end, w);
+        scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
+        scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, e);
+        if (!ENDS && z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] += bias;
         if (a.softplus) {
@@ -52,7 +51,7 @@ struct FwdRow {
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (!INSIDE) e[i] = t0 + c + i < end ? e[i] : 0.f;
+            if (!INSIDE) e[i] = t0 + c + i < len ? e[i] : 0.f;
             ex[i] = u[i] * e[i];
         }
         lds_put8(sE + at, e);
@@ -93,7 +92,7 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     const int p = lane & (P - 1), cl = lane / P;
     const int len = seq_length(a.lengths, at.n, a.L);
     const int base = (at.cb * waves + wave) * R::CW;      // first channel of the wave, within its group
-    const bool there = base + cl < a.Dg, full = base + R::CW <= a.Dg;
+    const bool there = base + cl < a.Dg;                  // (a lane without a channel goes along with the group's first)
     const long d = static_cast<long>(at.g) * a.Dg + (there ? base + cl : 0);
 
     float rate[K], h[K];
@@ -109,15 +108,16 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanA
     FwdRow<BF16, P, T, ENDS> row(a, at, base, lane);
     using E = typename RowElem<BF16>::type;
     ScanStates<BF16, SP, T, !ENDS> states{static_cast<const E*>(a.B) + at.n * a.b_sn + at.g * a.b_sg,
-                                          static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, {}};
+                                          static_cast<const E*>(a.C) + at.n * a.c_sn + at.g * a.c_sg, a.b_ss, a.c_ss, a.S, a.L, {}};
     const int t_begin = at.seg * a.seg_len, t_end = min(a.L, t_begin + a.seg_len);
     float sum = 0.f;
     for (int t0 = t_begin; t0 < t_end; t0 += T) {
-        const bool inside = t0 + T <= len && full;        // of the whole wave: no masks
+        const bool inside = t0 + T <= len;                // no masks
         states.begin(t0, len);
         if (inside) row.template stage<true>(a, t0, len, sE[wave], sX[wave]);
         else row.template stage<false>(a, t0, len, sE[wave], sX[wave]);
         states.finish(t0, len, sB, sC);
+        if (t0 == t_begin) make_rates(rate);
         __syncthreads();
         float* e_row = sE[wave] + cl * R::RS;
         const float* ex_row = sX[wave] + cl * R::RS;
