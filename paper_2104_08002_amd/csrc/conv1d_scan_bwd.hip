@@ -147,7 +147,7 @@ struct BackRow {
         bias = a.dt_bias ? a.dt_bias[d] : 0.f;
     }
     // e, dy and (WITH_X) x of the tile at t0 into LDS.  INSIDE: it lies within the sequence.  A lane without a channel (there are
-    // some if not `full`) goes along with the group's first, without a gradient: it adds nothing to the sums over channels.
+    // some if not `full`) goes along with the group's first, x and dy of 0: it adds nothing to the sums over channels.
     template <bool INSIDE, bool WITH_X>
     __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, bool full, float* sE, float* sX, float* sY) const {
         if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
@@ -173,7 +173,10 @@ struct BackRow {
         }
         if (!full) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] = real ? g[i] : 0.f;
+            for (int i = 0; i < 8; ++i) {
+                g[i] = real ? g[i] : 0.f;
+                if (WITH_X) u[i] = real ? u[i] : 0.f;
+            }
         }
         lds_put8(sY + at, g);
         if (WITH_X) lds_put8(sX + at, u);
