@@ -116,6 +116,8 @@ def _ptr(t):
 
 def _spread(t, name):
     """An output: no two of its elements in one place."""
+    if t.is_contiguous():
+        return t
     last, strides = 1, sorted((t.stride(i), t.shape[i]) for i in range(t.dim()) if t.shape[i] > 1)
     for stride, size in strides:
         if stride < last:
@@ -125,16 +127,17 @@ def _spread(t, name):
 
 
 def _span(t):
-    return t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+    first = t.data_ptr()
+    return first, first + (t.nbytes if t.is_contiguous() else t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))))
 
 
 def _apart(out, ins):
     """An output given by the caller: no memory between its first and last element may be an input's."""
     first, last = _span(out)
     for t in ins:
-        if t is not None and t.numel():
+        if t is not None:
             t0, t1 = _span(t)
-            if t0 < last and first < t1:
+            if first < t1 and t0 < min(last, t1):
                 raise ValueError("out shares memory with an input")
     return out
 
