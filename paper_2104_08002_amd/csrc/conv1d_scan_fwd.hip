@@ -81,9 +81,9 @@ struct FwdRow {
     }
 };
 
-// ENDS: no output but the state each segment adds and the sum of its steps.
+// ENDS: no output but the state each segment adds and the sum of its steps.  (P = 16: LDS holds three workgroups of a CU.)
 template <bool BF16, int K, int P, bool ENDS>
-__global__ __launch_bounds__(kScanWaves* kSeqWave, 4) void scan_fwd_kernel(ScanArgs a) {
+__global__ __launch_bounds__(kScanWaves* kSeqWave, P == 16 ? 3 : 4) void scan_fwd_kernel(ScanArgs a) {
     constexpr int SP = K * P, T = scan_tile(P);
     using R = ScanRows<P, T>;
     __shared__ __align__(16) float sE[kScanWaves][R::CW * R::RS], sX[kScanWaves][R::CW * R::RS];  // e (then y) and e x
