@@ -357,6 +357,27 @@ def test_a_bad_sample_stays_alone(seq):
     assert torch.equal(y[1, :2], clean[0][1, :2])
 
 
+@pytest.mark.parametrize("L", [90, 700])
+@pytest.mark.parametrize("G", [1, 2])
+def test_a_bad_channel_stays_alone(seq, L, G):
+    """NaN in the first channel of a group that does not fill a wave: of the group, dB and dC alone have it."""
+    gen = _gen(25)
+    c = _scan_case(gen, torch.float32, 2, 5, L, 16, G)
+    dy = _normal(gen, 2, 5 * G, L)
+    y0, _, saved = seq.conv1d_scan_fwd(**c, save=True)
+    g0 = seq.conv1d_scan_bwd(dy, saved, **c)
+    c["x"] = c["x"].clone()
+    c["x"][:, 0, L // 2] = math.nan
+    y, _, saved = seq.conv1d_scan_fwd(**c, save=True)
+    g = seq.conv1d_scan_bwd(dy, saved, **c)
+    assert torch.equal(y[:, 1:], y0[:, 1:]) and y[:, 0, L // 2:].isnan().all()
+    for k in ("dx", "ddt", "dz"):
+        assert torch.equal(getattr(g, k)[:, 1:], getattr(g0, k)[:, 1:]), k
+    for k in ("dA", "dskip", "ddt_bias"):
+        assert torch.equal(getattr(g, k)[1:], getattr(g0, k)[1:]), k
+    assert torch.equal(g.dB[:, 1:], g0.dB[:, 1:]) and torch.equal(g.dC[:, 1:], g0.dC[:, 1:]) and g.dC[:, 0].isnan().any()
+
+
 # ---- streams, graphs, order ------------------------------------------------------------------------------------------------
 def test_same_bits_again_and_on_another_stream(seq):
     gen = _gen(12)
