@@ -7,8 +7,8 @@
 // Lanes.  P neighbouring lanes have one channel, K states each, in registers (S is padded to K P with zeros): 4 lanes of 1, 2 or
 // 4 states up to S = 16, 8 or 16 lanes of 4 beyond; a wave has 64 / P channels.  One step costs a lane K exponentials (half the
 // rate of a product) and 4 K products, which is what bounds the scan.  (With 4 states a lane for every S, S = 8 has 32 channels a
-// wave and room in LDS for 16 steps of them: it took as long as S = 16.)  Rows lie along the sequence, states across lanes: a tile of steps goes through
-// LDS, loaded and stored along rows (8 elements a lane), read 4 steps at a time.
+// wave and room in LDS for 16 steps of them: it took as long as S = 16.)  Rows lie along the sequence, states across lanes: a tile
+// of steps goes through LDS, loaded and stored along rows (up to 8 elements a lane), read 4 steps at a time.
 // Positions behind a sequence's length have e = 0 and e x = 0, which leaves the state as it is.
 #pragma once
 
@@ -74,8 +74,8 @@ __device__ __forceinline__ void put_states(float* p, const float (&h)[K]) {
     *reinterpret_cast<States<K>*>(p) = s;
 }
 
-// steps of a tile: forwards the 64 lanes stage 8 elements each of a wave's 64 / P rows (half of them for P = 16); backwards the
-// sums over waves want LDS too
+// steps of a tile, of which the 64 lanes stage the same number of elements each (8, 8, 4 for P = 4, 8, 16; backwards 8, 2, 1: the
+// sums over waves want LDS too; with 8 elements on fewer lanes, N = 4, D = 256, L = 8192, S = 64 took 658 us backwards for 579)
 constexpr int scan_tile(int P) { return P == 4 ? 32 : 64; }
 constexpr int scan_tile_back(int P) { return P == 4 ? 32 : 16; }
 // floats of a row in LDS: 16 rows of 4 steps lie in distinct banks
@@ -137,21 +137,45 @@ __device__ __forceinline__ const typename RowElem<BF16>::type* scan_row(const vo
     return static_cast<const typename RowElem<BF16>::type*>(base) + n * sn + d * sd;
 }
 
-// Steps t .. t + 7 of a row.  INSIDE: they all count; else those from `end` on are 0, every load comes from one of the row's L
+// Steps t .. t + V - 1 of a row.  INSIDE: they all count; else those from `end` on are 0, every load comes from one of the row's L
 // elements, and none waits for a branch: a launch of single tiles takes as long as its last one.  (With that and the rates made
 // behind the first loads, N = 3, D = 49, L = 4999, S = 5 in FP32 takes 53 us forwards and backwards, 57 before.)
-template <bool BF16, bool INSIDE>
-__device__ __forceinline__ void scan_load8(const void* row, int t, int end, int L, float (&v)[8]) {
-    if constexpr (INSIDE) {
+template <bool BF16, bool INSIDE, int V>
+__device__ __forceinline__ void scan_load(const void* row, int t, int end, int L, float (&v)[V]) {
+    if constexpr (INSIDE && V == 8) {
         row_load8_inside<BF16>(row, t, v);
+    } else if constexpr (INSIDE) {
+        typename RowElem<BF16>::type u[V];
+        __builtin_memcpy(u, static_cast<const typename RowElem<BF16>::type*>(row) + t, sizeof u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = load_elem<BF16>(u, e);
     } else if (wave_all(t >= end)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        for (int e = 0; e < V; ++e) v[e] = 0.f;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = load_elem<BF16>(row, min(t + e, L - 1));
+        for (int e = 0; e < V; ++e) v[e] = load_elem<BF16>(row, min(t + e, L - 1));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = t + e < end ? v[e] : 0.f;
+        for (int e = 0; e < V; ++e) v[e] = t + e < end ? v[e] : 0.f;
+    }
+}
+// those of them that lie before `end`
+template <bool BF16, int V>
+__device__ __forceinline__ void scan_store(void* row, int t, int end, const float (&v)[V]) {
+    if constexpr (V == 8) {
+        row_store8<BF16>(row, t, end, v);
+    } else {
+        typename RowElem<BF16>::type u[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) store_elem<BF16>(u, e, v[e]);
+        auto* to = static_cast<typename RowElem<BF16>::type*>(row) + t;
+        if (t + V <= end) {
+            __builtin_memcpy(to, u, sizeof u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (t + e < end) to[e] = u[e];
+        }
     }
 }
 
@@ -171,8 +195,8 @@ struct ScanStates {
         const bool which = BOTH && i >= kItems;
         if (s < S) {
             const E* row = (which ? second : first) + s * (which ? second_ss : first_ss);
-            if (t0 + T <= end) scan_load8<BF16, true>(row, t0 + 8 * c, end, L, v);
-            else scan_load8<BF16, false>(row, t0 + 8 * c, end, L, v);
+            if (t0 + T <= end) scan_load<BF16, true>(row, t0 + 8 * c, end, L, v);
+            else scan_load<BF16, false>(row, t0 + 8 * c, end, L, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -195,23 +219,35 @@ struct ScanStates {
     }
 };
 
-// the lane's part in loading and storing rows: row lane / LPR of the wave, 8 elements from 8 (lane % LPR) on
+// the lane's part in loading and storing a tile's rows: row lane / LPR of the wave, V elements from V (lane % LPR) on
 template <int P, int T>
 struct ScanRows {
-    static constexpr int CW = kSeqWave / P, LPR = T / 8, RS = scan_stride(T);
-    static_assert(CW * LPR <= kSeqWave, "a wave stages a tile at once");
+    static constexpr int CW = kSeqWave / P, V = CW * T / kSeqWave, LPR = T / V, RS = scan_stride(T);
+    static_assert(CW * LPR == kSeqWave && V <= 8, "a wave stages a tile at once");
 };
 
-__device__ __forceinline__ void lds_put8(float* to, const float (&v)[8]) {
-    *reinterpret_cast<scan_f32x4*>(to) = scan_f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<scan_f32x4*>(to + 4) = scan_f32x4{v[4], v[5], v[6], v[7]};
-}
-__device__ __forceinline__ void lds_get8(const float* from, float (&v)[8]) {
-    const scan_f32x4 a = *reinterpret_cast<const scan_f32x4*>(from), b = *reinterpret_cast<const scan_f32x4*>(from + 4);
+template <int V>
+__device__ __forceinline__ void lds_put(float* to, const float (&v)[V]) {
+    if constexpr (V >= 4) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        v[e] = a[e];
-        v[4 + e] = b[e];
+        for (int e = 0; e < V; e += 4) *reinterpret_cast<scan_f32x4*>(to + e) = scan_f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) to[e] = v[e];
+    }
+}
+template <int V>
+__device__ __forceinline__ void lds_get(const float* from, float (&v)[V]) {
+    if constexpr (V >= 4) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const scan_f32x4 a = *reinterpret_cast<const scan_f32x4*>(from + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i + e] = a[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = from[e];
     }
 }
 

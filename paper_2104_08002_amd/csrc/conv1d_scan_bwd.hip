@@ -130,6 +130,7 @@ __device__ __forceinline__ void step_sums(const float (&q)[K], float (&out)[kSum
 template <bool BF16, int P, int T>
 struct BackRow {
     using R = ScanRows<P, T>;
+    static constexpr int V = R::V;
     using E = typename RowElem<BF16>::type;
     const E *x, *dt, *dout, *z;
     float bias;
@@ -139,9 +140,9 @@ struct BackRow {
 
     __device__ __forceinline__ BackRow(const ScanArgs& a, const ScanPlace& p, int base, int lane) {
         const int row = lane / R::LPR;
-        c = 8 * (lane % R::LPR);
+        c = V * (lane % R::LPR);
         at = row * R::RS + c;
-        real = row < R::CW && base + row < a.Dg;
+        real = base + row < a.Dg;
         d = static_cast<long>(p.g) * a.Dg + (real ? base + row : 0);
         x = scan_row<BF16>(a.x, a.x_sn, a.x_sd, p.n, d);
         dt = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, p.n, d);
@@ -153,36 +154,35 @@ struct BackRow {
     // some if not `full`) goes along with the group's first, x and dy of 0: it adds nothing to the sums over channels.
     template <bool INSIDE, bool WITH_X>
     __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, bool full, float* sE, float* sX, float* sY) const {
-        if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
-        float v[8], g[8], u[8], w[8];
-        scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
-        scan_load8<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
-        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
-        if (WITH_X) scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
+        float v[V], g[V], u[V], w[V];
+        scan_load<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
+        scan_load<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
+        if (z) scan_load<BF16, INSIDE>(z, t0 + c, len, a.L, w);
+        if (WITH_X) scan_load<BF16, INSIDE>(x, t0 + c, len, a.L, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += bias;
+        for (int i = 0; i < V; ++i) v[i] += bias;
         if (a.softplus) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = softplus_of(v[i]);
+            for (int i = 0; i < V; ++i) v[i] = softplus_of(v[i]);
         }
         if (!INSIDE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = t0 + c + i < len ? v[i] : 0.f;
+            for (int i = 0; i < V; ++i) v[i] = t0 + c + i < len ? v[i] : 0.f;
         }
-        lds_put8(sE + at, v);
+        lds_put(sE + at, v);
         if (z) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] *= w[i] * sigmoid_of(w[i]);
+            for (int i = 0; i < V; ++i) g[i] *= w[i] * sigmoid_of(w[i]);
         }
         if (!full) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < V; ++i) {
                 g[i] = real ? g[i] : 0.f;
                 if (WITH_X) u[i] = real ? u[i] : 0.f;
             }
         }
-        lds_put8(sY + at, g);
-        if (WITH_X) lds_put8(sX + at, u);
+        lds_put(sY + at, g);
+        if (WITH_X) lds_put(sX + at, u);
     }
     // the gradients of x, dt and z from what the walk back left in LDS
     template <bool INSIDE>
@@ -190,45 +190,45 @@ struct BackRow {
                                            const float* sY, float& dskip, float& dbias) const {
         if (!real || t0 + c >= a.L) return;
         const long o = (p.n * a.D + d) * a.L;
-        const int end = INSIDE ? t0 + c + 8 : a.L;
+        const int end = INSIDE ? t0 + c + V : a.L;
         const float skip = a.skip ? a.skip[d] : 0.f;
-        float u[8], v[8], g[8], w[8];
-        scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
-        scan_load8<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
-        if (z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
-        if (a.softplus) scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
+        float u[V], v[V], g[V], w[V];
+        scan_load<BF16, INSIDE>(x, t0 + c, len, a.L, u);
+        scan_load<BF16, INSIDE>(dout, t0 + c, len, a.L, g);
+        if (z) scan_load<BF16, INSIDE>(z, t0 + c, len, a.L, w);
+        if (a.softplus) scan_load<BF16, INSIDE>(dt, t0 + c, len, a.L, v);
         if (z) {
-            float y[8];
-            lds_get8(sY + at, y);
+            float y[V];
+            lds_get(sY + at, y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < V; ++i) {
                 const float sig = sigmoid_of(w[i]), zs = w[i] * sig;
                 y[i] = g[i] * fmaf(skip, u[i], y[i]) * fmaf(zs, 1.f - sig, sig);
                 g[i] *= zs;
                 if (!INSIDE) y[i] = t0 + c + i < len ? y[i] : 0.f;
             }
-            row_store8<BF16>(static_cast<E*>(a.dz) + o, t0 + c, end, y);
+            scan_store<BF16>(static_cast<E*>(a.dz) + o, t0 + c, end, y);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dskip = fmaf(g[i], u[i], dskip);
-        lds_get8(sE + at, u);
+        for (int i = 0; i < V; ++i) dskip = fmaf(g[i], u[i], dskip);
+        lds_get(sE + at, u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < V; ++i) {
             g[i] = fmaf(skip, g[i], u[i]);
             if (!INSIDE) g[i] = t0 + c + i < len ? g[i] : 0.f;
         }
-        row_store8<BF16>(static_cast<E*>(a.dx) + o, t0 + c, end, g);
-        lds_get8(sX + at, u);
+        scan_store<BF16>(static_cast<E*>(a.dx) + o, t0 + c, end, g);
+        lds_get(sX + at, u);
         if (a.softplus) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] *= sigmoid_of(v[i] + bias);
+            for (int i = 0; i < V; ++i) u[i] *= sigmoid_of(v[i] + bias);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < V; ++i) {
             if (!INSIDE) u[i] = t0 + c + i < len ? u[i] : 0.f;
             dbias += u[i];
         }
-        row_store8<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, end, u);
+        scan_store<BF16>(static_cast<E*>(a.ddt) + o, t0 + c, end, u);
     }
 };
 

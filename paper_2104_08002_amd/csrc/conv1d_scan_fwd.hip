@@ -15,19 +15,20 @@ constexpr int kThreads = 256;
 template <bool BF16, int P, int T, bool ENDS>
 struct FwdRow {
     using R = ScanRows<P, T>;
+    static constexpr int V = R::V;
     using E = typename RowElem<BF16>::type;
     const E *x, *dt, *z;
     E* out;
     float bias, skip;
     bool real;
     int c, at;          // first step of the lane within the tile, its place in LDS
-    float u[8], w[8];   // x and z of the tile
+    float u[V], w[V];   // x and z of the tile
 
     __device__ __forceinline__ FwdRow(const ScanArgs& a, const ScanPlace& p, int base, int lane) {
         const int row = lane / R::LPR;
-        c = 8 * (lane % R::LPR);
+        c = V * (lane % R::LPR);
         at = row * R::RS + c;
-        real = row < R::CW && base + row < a.Dg;
+        real = base + row < a.Dg;
         const long d = static_cast<long>(p.g) * a.Dg + (real ? base + row : 0);
         x = scan_row<BF16>(a.x, a.x_sn, a.x_sd, p.n, d);
         dt = scan_row<BF16>(a.dt, a.dt_sn, a.dt_sd, p.n, d);
@@ -40,43 +41,42 @@ struct FwdRow {
     // e and e x into LDS
     template <bool INSIDE>
     __device__ __forceinline__ void stage(const ScanArgs& a, int t0, int len, float* sE, float* sX) {
-        if (R::CW * R::LPR < kSeqWave && at >= R::CW * R::RS) return;
-        float e[8], ex[8];
-        scan_load8<BF16, INSIDE>(x, t0 + c, len, a.L, u);
-        scan_load8<BF16, INSIDE>(dt, t0 + c, len, a.L, e);
-        if (!ENDS && z) scan_load8<BF16, INSIDE>(z, t0 + c, len, a.L, w);
+        float e[V], ex[V];
+        scan_load<BF16, INSIDE>(x, t0 + c, len, a.L, u);
+        scan_load<BF16, INSIDE>(dt, t0 + c, len, a.L, e);
+        if (!ENDS && z) scan_load<BF16, INSIDE>(z, t0 + c, len, a.L, w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] += bias;
+        for (int i = 0; i < V; ++i) e[i] += bias;
         if (a.softplus) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = softplus_of(e[i]);
+            for (int i = 0; i < V; ++i) e[i] = softplus_of(e[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < V; ++i) {
             if (!INSIDE) e[i] = t0 + c + i < len ? e[i] : 0.f;
             ex[i] = u[i] * e[i];
         }
-        lds_put8(sE + at, e);
-        lds_put8(sX + at, ex);
+        lds_put(sE + at, e);
+        lds_put(sX + at, ex);
     }
     // the output from the sums in LDS
     template <bool INSIDE>
     __device__ __forceinline__ void finish(const ScanArgs& a, int t0, int len, const float* sY) const {
         if (!real || t0 + c >= a.L) return;
-        float y[8];
-        lds_get8(sY + at, y);
+        float y[V];
+        lds_get(sY + at, y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = fmaf(skip, u[i], y[i]);
+        for (int i = 0; i < V; ++i) y[i] = fmaf(skip, u[i], y[i]);
         if (z) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] *= w[i] * sigmoid_of(w[i]);
+            for (int i = 0; i < V; ++i) y[i] *= w[i] * sigmoid_of(w[i]);
         }
         if (!INSIDE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
-            row_store8<BF16>(out, t0 + c, a.L, y);
+            for (int i = 0; i < V; ++i) y[i] = t0 + c + i < len ? y[i] : 0.f;
+            scan_store<BF16>(out, t0 + c, a.L, y);
         } else {
-            row_store8<BF16>(out, t0 + c, t0 + c + 8, y);
+            scan_store<BF16>(out, t0 + c, t0 + c + V, y);
         }
     }
 };
