@@ -307,7 +307,8 @@ int conv1d_causal_step(const conv1d_causal_t* p, void* state, void* y, long y_sn
  *   e[t] = dt[n][d][t] + dt_bias[d], through log(1 + exp(.)) with CONV1D_SCAN_SOFTPLUS
  *   h[s] = exp(e[t] A[d][s]) h[s] + e[t] x[n][d][t] B[n][g][s][t],   h = init before the first position
  *   y[t] = (sum_s C[n][g][s][t] h[s] + skip[d] x[n][d][t]) * (z ? z[n][d][t] sigmoid(z[n][d][t]) : 1)
- * The D channels are G groups of D / G neighbours, which share B and C. */
+ * The D channels are G groups of D / G neighbours, which share B and C.  The decay exp(e A) of one step is a float (e A up to 88); those
+ * of many steps may multiply to any size, as long as the states and gradients that they lead to are floats. */
 #define CONV1D_SCAN_SOFTPLUS 1
 typedef struct {
     const void *x, *dt;              /* [N][D][L] dtype */

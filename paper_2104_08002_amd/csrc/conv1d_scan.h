@@ -251,17 +251,45 @@ __device__ __forceinline__ void lds_get(const float* from, float (&v)[V]) {
     }
 }
 
+// 2^x as m 2^n, 1 <= m < 2.  Where e A adds up to more than 88 over a segment (a state that grows), 2^x is no float, and as infinity
+// would make NaN of a state of 0 before it, or of the shrinking behind it; m 2^n times a state is infinite only if the product is.
+// Exponents end at 2^26, far behind those of any state, so that 16 of them add up in an int.  (NaN stays in m.)  A wave whose decays
+// are all at most 1, which is the rule, takes them as floats: N = 1, D = 128 in 938 segments takes 7.1 us so and 7.9 otherwise,
+// N = 8, D = 128 in 125 segments 6.0 and 6.3.
+struct Decay {
+    float m;
+    int n;
+};
+__device__ __forceinline__ Decay decay_of(float x) {
+    constexpr float most = 1 << 26;
+    const float c = x > most ? most : x < -most ? -most : x, f = floorf(c);
+    return Decay{exp2_hw(c - f), static_cast<int>(fmaxf(f, -most))};
+}
+__device__ __forceinline__ float decayed(const Decay& d, float h, float add) { return fmaf(d.m, ldexpf(h, d.n), add); }
+// both, one behind the other, up to 16 of them: m is below 2^16 and is brought back by `normal`
+__device__ __forceinline__ void decay_more(Decay& d, const Decay& by) {
+    d.m *= by.m;
+    d.n += by.n;
+}
+__device__ __forceinline__ Decay normal(const Decay& d) {
+    const int up = static_cast<int>(__float_as_uint(d.m) >> 23) - 127;
+    return Decay{ldexpf(d.m, -up), d.n + up};
+}
+
 // One (sample, channel) row of segment values joined along the sequence: value[seg] holds what a segment adds, and becomes
 // what comes into it from the segments before (BACK: behind) it, `first` into the first; sums[seg]: exp(A sum) is a segment's
-// decay.  SP states times `chunks` runs of kRun segments at a time: a run is joined in registers, the runs through LDS.
+// decay, and those of a run multiply to a run's.  SP states times `chunks` runs of kRun segments at a time: a run is joined in
+// registers, the runs through LDS.
 // Bound by latency and by how much of every line it uses, so that a row's segments lie together: N = 8, D = 128 in 125 segments
 // takes 6.0 us, 9.8 with the channels of a segment together.  Runs of 16 join up to 1024 segments of 16 states at once (N = 1,
-// D = 128 in 938: 6.6 us, 8.8 with runs of 8, which are no faster at fewer).
+// D = 128 in 938: 7.1 us, 2.2 more with runs of 8, which are no faster at fewer).
 constexpr int kRun = 16;
 template <bool BACK>
 __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const float* sums, const float* first, const float* A, int N, int D,
                                                          int S, int SP, int nseg, int chunks) {
     __shared__ float run_decay[1024], run_add[1024], last[1024];
+    __shared__ int run_shift[1024];              // the n of a run's decay
+    __shared__ bool shrinking[1024 / kSeqWave];  // of every wave
     const unsigned per_row = SP * chunks, row = blockIdx.x * (blockDim.x / per_row) + threadIdx.x / per_row;  // (N D < 2^25)
     const bool there = row < static_cast<unsigned>(N) * D;
     const int in_row = threadIdx.x % per_row, s = in_row % SP, chunk = in_row / SP, base = threadIdx.x - in_row + s;
@@ -269,7 +297,8 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
     const float rate = rate_of(scan_rate(A, S, d, s, there));
     float h = there && first && s < S ? first[static_cast<long>(row) * S + s] : 0.f;
     for (int from = 0; from < nseg; from += kRun * chunks) {
-        float f[kRun], v[kRun], decay = 1.f, add = 0.f;
+        Decay f[kRun], decay{1.f, 0};
+        float x[kRun], v[kRun], add = 0.f;
         const int i0 = from + kRun * chunk, real = there ? nseg - i0 : 0;  // segments of the run that are there
         const long at = static_cast<long>(row) * nseg + (BACK ? nseg - 1 - i0 : i0);
         constexpr int next = BACK ? -1 : 1;
@@ -278,24 +307,55 @@ __global__ __launch_bounds__(1024) void scan_join_kernel(float* value, const flo
         float* to = value + at * SP + s;
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            f[i] = i < real ? sum[i * next] : 0.f;
-            v[i] = i < real ? to[i * step] : 0.f;
+            x[i] = i < real - 1 ? sum[i * next] : 0.f;  // (nothing comes behind the last segment, which has left no values)
+            v[i] = i < real - 1 ? to[i * step] : 0.f;
         }
+        bool shrinks = true;
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            f[i] = exp2_hw(rate * f[i]);
-            add = fmaf(f[i], add, v[i]);
-            decay *= f[i];
+            x[i] *= rate;
+            shrinks = shrinks && x[i] <= 0.f;
         }
-        run_decay[threadIdx.x] = decay;
+        shrinks = wave_all(shrinks);
+        if (shrinks) {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                f[i] = Decay{exp2_hw(x[i]), 0};
+                add = fmaf(f[i].m, add, v[i]);
+                decay.m *= f[i].m;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                f[i] = decay_of(x[i]);
+                add = decayed(f[i], add, v[i]);
+                decay_more(decay, f[i]);
+            }
+            decay = normal(decay);
+        }
+        run_decay[threadIdx.x] = decay.m;
+        run_shift[threadIdx.x] = decay.n;
         run_add[threadIdx.x] = add;
+        if (threadIdx.x % kSeqWave == 0) shrinking[threadIdx.x / kSeqWave] = shrinks;
         __syncthreads();
+        if (wave_all(shrinking[threadIdx.x % (blockDim.x / kSeqWave)])) {
 #pragma unroll 8
-        for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
+            for (int c = 0; c < chunk; ++c) h = fmaf(run_decay[base + c * SP], h, run_add[base + c * SP]);
+        } else {
+            for (int c = 0; c < chunk; ++c) h = decayed(Decay{run_decay[base + c * SP], run_shift[base + c * SP]}, h, run_add[base + c * SP]);
+        }
+        if (shrinks) {
 #pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            if (i < real) to[i * step] = h;
-            h = fmaf(f[i], h, v[i]);
+            for (int i = 0; i < kRun; ++i) {
+                if (i < real) to[i * step] = h;
+                h = fmaf(f[i].m, h, v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                if (i < real) to[i * step] = h;
+                h = decayed(f[i], h, v[i]);
+            }
         }
         if (from + kRun * chunks >= nseg) break;  // (of the whole workgroup)
         if (chunk == chunks - 1) last[base] = h;
