@@ -421,6 +421,10 @@ __global__ __launch_bounds__(kScanWaves* kSeqWave, 3) void scan_bwd_kernel(ScanA
             if (s >= a.S || t >= a.L) continue;
             scan_f32x4 v = *reinterpret_cast<const scan_f32x4*>(&red[0][which][s * R::RS + step]);
             for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const scan_f32x4*>(&red[w][which][s * R::RS + step]);
+            if (!inside) {  // 0 behind the end also where 0 has met an infinite state or gradient
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = t + e < len ? v[e] : 0.f;
+            }
             const long o = ((at.n * a.G + at.g) * a.S + s) * a.L + t;
             if (a.blocks_d > 1) {
                 float* to = a.part_bc + (static_cast<long>(which) * a.blocks_d + at.cb) * a.N * a.G * a.S * a.L + o;
