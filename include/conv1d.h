@@ -353,7 +353,7 @@ int conv1d_grad_norm(void* const* data, const size_t* counts, const int* dtypes,
 
 /* Scales every element in place by min(1, most / (norm + 1e-6)), the factor rounded to float: 0 for an infinite norm, NaN for
  * NaN.  norm: device, one float, as conv1d_grad_norm leaves it (or summed over ranks since).  CONV1D_EINVAL where two of the
- * tensors share memory. */
+ * tensors share memory, or one with the norm. */
 int conv1d_grad_clip(void* const* data, const size_t* counts, const int* dtypes, int tensors, const float* norm, float most, void* stream);
 
 #ifdef __cplusplus

@@ -164,15 +164,17 @@ bool tensors_ok(void* const* data, const size_t* counts, const int* dtypes, int 
     return true;
 }
 
-// whether two of the tensors share memory: -1 if that cannot be found out
-int overlap(void* const* data, const size_t* counts, const int* dtypes, int tensors) {
+// whether two of the tensors share memory, or one with the norm, which every workgroup reads: -1 if that cannot be found out
+int overlap(void* const* data, const size_t* counts, const int* dtypes, int tensors, const float* norm) {
     struct Range {
         uintptr_t from, to;
     };
-    if (tensors < 2) return 0;
-    Range* r = new (std::nothrow) Range[tensors];
+    if (tensors < 1) return 0;
+    Range* r = new (std::nothrow) Range[tensors + 1];
     if (!r) return -1;
     int n = 0;
+    const uintptr_t norm_at = reinterpret_cast<uintptr_t>(norm);
+    r[n++] = Range{norm_at, norm_at + sizeof(float)};
     for (int i = 0; i < tensors; ++i) {
         if (!counts[i]) continue;
         const uintptr_t at = reinterpret_cast<uintptr_t>(data[i]);
@@ -244,7 +246,7 @@ int conv1d_grad_norm(void* const* data, const size_t* counts, const int* dtypes,
 
 int conv1d_grad_clip(void* const* data, const size_t* counts, const int* dtypes, int tensors, const float* norm, float most, void* stream) {
     if (!tensors_ok(data, counts, dtypes, tensors) || !norm || !seq_aligned(norm, 4) || !(most >= 0.f)) return CONV1D_EINVAL;
-    if (overlap(data, counts, dtypes, tensors)) return CONV1D_EINVAL;
+    if (overlap(data, counts, dtypes, tensors, norm)) return CONV1D_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const hipError_t e = each_table(data, counts, dtypes, tensors, [&](const Table& t, long blocks, long) {
         return launch_kernel(grad_scale_kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, t, norm, most);

@@ -87,7 +87,7 @@ def conv1d_grad_clip(grads, max_norm: float, norm_type: float = 2.0, norm=None, 
     """Scales `grads` in place by min(1, max_norm / (norm + 1e-6)) and returns the norm they had, a float32 scalar on their device.
 
     norm: a norm found before (conv1d_grad_norm, then joined over ranks, say) in the place of this call's own.
-    Tensors that share memory are refused.  An infinite norm scales by 0, NaN by NaN: look at the norm before the update.
+    Tensors that share memory, with each other or with `norm`, are refused.  An infinite norm scales by 0, NaN by NaN: look at the norm before the update.
     """
     max_norm = float(max_norm)
     if not max_norm >= 0:
