@@ -131,13 +131,30 @@ def _span(t):
     return first, first + (t.nbytes if t.is_contiguous() else t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))))
 
 
+def _arc(t, period):
+    """Bytes that t takes up modulo `period`: axes that step by whole periods add none."""
+    size = t.element_size()
+    return size * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()) if s * size % period))
+
+
+def _interleaved(out, t):
+    """Whether the two lie in different parts of a period of out's strides, as the halves of a projection do."""
+    for stride in out.stride():
+        period = stride * out.element_size()
+        if period:
+            gap = (t.data_ptr() - out.data_ptr()) % period
+            if _arc(out, period) <= gap and gap + _arc(t, period) <= period:
+                return True
+    return False
+
+
 def _apart(out, ins):
-    """An output given by the caller: no memory between its first and last element may be an input's."""
+    """An output given by the caller: its elements may not lie where an input's do."""
     first, last = _span(out)
     for t in ins:
         if t is not None:
             t0, t1 = _span(t)
-            if first < t1 and t0 < min(last, t1):
+            if first < t1 and t0 < min(last, t1) and not _interleaved(out, t):
                 raise ValueError("out shares memory with an input")
     return out
 
