@@ -112,6 +112,13 @@ def test_causal_stays_in_bounds(model):
     _in_child(cases, lambda c: _causal_case(model, c))
 
 
+def test_causal_of_many_rows_stays_in_bounds(model):
+    """Rows enough for four steps a lane backwards, and for eight."""
+    cases = [(N, C, L, S, dt, kind, 1, at_end) for N, C, L, S in ((2, 1100, 2049, 2), (2, 1030, 2060, 8), (1, 4096, 600, 5), (2, 1100, 4099, 3), (1, 1400, 8200, 8))
+             for dt, kind, at_end in ((0, 0, True), (1, 2, True), (0, 2, False))]
+    _in_child(cases, lambda c: _causal_case(model, c))
+
+
 def _scan_case(lib, c):
     N, Dg, L, S, G, dtype, kind, opt, at_end = c
     D, mem, e = G * Dg, Memory(at_end), 2 if dtype else 4
@@ -154,6 +161,13 @@ def test_scan_stays_in_bounds(model):
         cases.append((rnd.randint(1, 4), rnd.choice((1, 2, 4, 5, 16, 17, 64, 70)), rnd.choice((1, 2, 15, 16, 31, 63, 64, 65, 130, 300, 777)),
                       rnd.choice((1, 4, 5, 8, 16, 17, 32, 64)), rnd.randint(1, 3), rnd.randint(0, 1), rnd.randint(0, 2), rnd.randint(0, 7),
                       rnd.random() < 0.5))
+    _in_child(cases, lambda c: _scan_case(model, c))
+
+
+def test_scan_of_many_segments_stays_in_bounds(model):
+    """More segments than are joined at once."""
+    cases = [(N, Dg, L, S, 1, dt, kind, 7, at_end) for N, Dg, L, S in ((1, 1, 40000, 16), (2, 1, 20000, 64), (1, 1, 36000, 24))
+             for dt, kind, at_end in ((0, 0, True), (1, 2, True), (0, 2, False))]
     _in_child(cases, lambda c: _scan_case(model, c))
 
 
