@@ -99,7 +99,7 @@ __device__ __forceinline__ void forward_step(const CausalArgs& a, const Piece& p
 }
 
 // One step a lane: waves enough hide the loads, more steps in flight only take registers (N = 8, C = 128, L = 20000, S = 4 in
-// bfloat16: 16 us, 5.1 TB/s, what a large copy reaches).
+// bfloat16: 16 to 18 us, 4.6 to 5.1 TB/s, what a large copy reaches).
 template <bool BF16, int S>
 __global__ __launch_bounds__(kThreads) void causal_fwd_kernel(CausalArgs a) {
     const Piece p = piece_of(a);

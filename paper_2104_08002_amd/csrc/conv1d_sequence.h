@@ -141,8 +141,9 @@ __device__ __forceinline__ int seq_length(const int* lengths, long n, int L) {
 __device__ __forceinline__ float sigmoid_of(float v) { return rcp_hw(1.f + exp2_hw(-v * kLog2e)); }
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + u), u = exp(-|v|), and log(1 + u) = 2 atanh(r) = r f(r^2), r = u / (2 + u) <= 1/3.
-// f is a polynomial with the least relative error on [0, 1/9], 4e-9 (fitted in 64 bits).  (The logarithm instruction has a
-// bound on its absolute error next to 1, which would leave few bits of the small steps that this is used for.)
+// f is a polynomial with the least relative error on [0, 1/9] (fitted in 64 bits): 8e-9 with its coefficients as floats.  (The
+// logarithm instruction has a bound on its absolute error next to 1, which would leave few bits of the small steps that this is
+// used for.)
 __device__ __forceinline__ float softplus_of(float v) {
     const float u = exp2_hw(-fabsf(v) * kLog2e);
     const float r = u * rcp_hw(2.f + u), q = r * r;
