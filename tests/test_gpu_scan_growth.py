@@ -141,3 +141,24 @@ def test_growth_is_the_same_cut_and_whole(seq):  # noqa: F811
     per = wide // D + 1
     _relative("y", y, y1[:, ::per].double(), 2 * (12 * 50 + 64))
     _relative("final", final, final1[:, ::per].double(), 2 * (12 * 50 + 64))
+
+
+@pytest.mark.parametrize("lowest", [torch.finfo(torch.float32).min, -float("inf")])
+def test_a_rate_without_bound_beside_a_growing_state(seq, lowest):  # noqa: F811
+    """Forgotten by every step, in a wave whose other states grow; also over 16 segments and more at once, and kept by steps of 0."""
+    gen = _gen(12)
+    L, S = 2048, 4
+    c = _case(gen, 1, L, S, N=2)
+    c["dt"][:] = 0.0078125
+    c["x"][:] = _pos(gen, 2, 3, L)
+    c["A"][:, 1] = lowest
+    c["init"] = _pos(gen, 2, 3, S)
+    _cut(c)
+    lengths = torch.tensor([L - 7, 0], dtype=torch.int32, device="cuda")
+    y, final, saved = seq.conv1d_scan_fwd(**c, lengths=lengths, want_final=True, save=True)
+    ex = c["dt"][0, :, L - 8] * c["x"][0, :, L - 8]
+    assert y.isfinite().all() and torch.equal(final[0, :, 1], ex * c["B"][0, 0, 1, L - 8])
+    assert torch.equal(final[1], c["init"][1])
+    g = seq.conv1d_scan_bwd(torch.ones_like(y), saved, **c, lengths=lengths, want_init=True)
+    assert g.dx.isfinite().all() and g.dinit.isfinite().all() and not g.dinit[:, :, 1].any()
+    assert (g.dinit[0, :, [0, 2, 3]] > 1e6).all()
