@@ -356,6 +356,75 @@ int conv1d_grad_norm(void* const* data, const size_t* counts, const int* dtypes,
  * tensors share memory, or one with the norm. */
 int conv1d_grad_clip(void* const* data, const size_t* counts, const int* dtypes, int tensors, const float* norm, float most, void* stream);
 
+/* ==== Around the layers ===========================================================
+ * What a network of layers has between them, in the same layout: the lookup of an
+ * embedding, group norm with an activation, dropout with the residual.  Rules as for
+ * the sequence operators (lengths among them); workspaces are 256-byte aligned. */
+
+/* Embedding lookup: y[n][d][l] = scale * table[tokens[n][l]][d], rounded once; 0 behind a sequence's end and where a token is outside
+ * [0, V), which has no gradient either.  D <= 2^20, V < 2^30, N * L <= 2^30 (more: CONV1D_EUNSUPPORTED). */
+#define CONV1D_EMBED_TOKENS64 1  /* tokens of 64 bits; else of 32 */
+typedef struct {
+    const void* tokens;   /* [N][L], signed; tok_sn apart */
+    const int* lengths;   /* [N] or NULL */
+    long tok_sn;
+    int N, D, L, V, dtype, flags;
+    float scale;
+} conv1d_embed_t;
+
+/* table: [V][D] dtype.  y: dtype, with positions (y_sl = 1) or channels (y_sd = 1) next to each other; L = 1: one token a sequence. */
+int conv1d_embed_fwd(const conv1d_embed_t* p, const void* table, void* y, long y_sn, long y_sd, long y_sl, void* stream);
+
+/* dtable: [V][D] float, all of it: scale * the sum of dy over the positions of each token (0 for a token that is not there), in an
+ * order that depends on the tokens alone.  dy: dtype, strides as for y. */
+size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype);
+int conv1d_embed_bwd(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy_sd, long dy_sl, float* dtable, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/* Group norm: the C channels are G groups of C / G neighbours.  Over a group's channels and the positions of sequence n, m values:
+ *   mean, var = their mean and the mean of (x - mean)^2,   rstd = 1 / sqrt(var + eps)
+ *   p = (x - mean) rstd weight[c] + bias[c],   y = p, max(p, 0) with CONV1D_NORM_RELU, or p * sigmoid(p) with CONV1D_NORM_SILU.
+ * x has positions (x_sl = 1) or channels (x_sc = 1) next to each other, and y, dy and dx have the same order, each with its strides.
+ * C <= 2^20, N * C <= 2^25, L <= 2^30, groups of 2^33 values and less (more: CONV1D_EUNSUPPORTED). */
+#define CONV1D_NORM_RELU 1
+#define CONV1D_NORM_SILU 2
+typedef struct {
+    const void* x;          /* [N][C][L] dtype */
+    const float* weight;    /* [C] or NULL: ones */
+    const float* bias;      /* [C] or NULL: zeros */
+    const int* lengths;     /* [N] or NULL */
+    long x_sn, x_sc, x_sl;
+    double eps;
+    int N, C, L, G, dtype, flags;
+} conv1d_norm_t;
+
+/* stats: [N][G][2] double, mean and rstd, for the backward pass; or NULL. */
+size_t conv1d_norm_fwd_workspace_bytes(int N, int C, int L, int G);
+int conv1d_norm_fwd(const conv1d_norm_t* p, void* y, long y_sn, long y_sc, long y_sl, double* stats, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* Gradients for dy of the call that p describes and that wrote stats: dx [N][C][L] dtype;  dweight, dbias [C] float, or NULL if not
+ * wanted.  The ReLU's gradient is 0 where p is 0 or less, found in 64 bits where p is next to 0. */
+size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G);
+int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_sc, long dy_sl, const double* stats, void* dx, long dx_sn,
+                    long dx_sc, long dx_sl, float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Dropout: y = residual + (kept ? x / (1 - p) : 0), rounded once.  Element (n, c, l) is kept where word l % 4 of block
+ * (n * C + c) * ceil(L / 4) + l / 4 is at least floor(p * 2^32); a block is Philox4x32 in seven rounds, its counter the block's number
+ * (low words first) and call + *counter, its key `key`.  The same call with the gradient in place of x, and no residual, is its
+ * backward pass.  What is dropped reaches nothing, an infinity or NaN neither.  0 <= p <= 1; N * C < 2^31, L <= 2^30. */
+typedef struct {
+    const void* x;          /* [N][C][L] dtype */
+    const void* residual;   /* [N][C][L] dtype, or NULL */
+    const int* lengths;     /* [N] or NULL */
+    const long* counter;    /* device, one number that is added to call (a captured graph's replays differ by it), or NULL */
+    long x_sn, x_sc, r_sn, r_sc;
+    unsigned long key, call;
+    double p;
+    int N, C, L, dtype;
+} conv1d_dropout_t;
+int conv1d_dropout(const conv1d_dropout_t* p, void* y, long y_sn, long y_sc, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

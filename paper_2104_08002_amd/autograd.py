@@ -1,4 +1,4 @@
-"""The layer, the causal convolution and the selective scan as ``torch.autograd.Function``s on top of the C-ABI binding.
+"""The layer, the sequence operators and the operators around the layers as ``torch.autograd.Function``s on top of the C-ABI binding.
 
 Glue only: every arithmetic step of the three passes and of the bias and ReLU around them runs in the library's kernels;
 torch supplies device memory, the stream and the autograd graph.  This is the interface the
@@ -13,7 +13,7 @@ import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
-from . import binding, sequence
+from . import binding, blocks, sequence
 
 
 def _has_tangent(t) -> bool:
@@ -169,3 +169,134 @@ def conv1d_scan(x, dt, A, B, C, skip=None, z=None, dt_bias=None, softplus: bool 
     # (a parameter wants a gradient under no_grad too, as far as forward can see: the states are kept for a graph alone)
     y, final = ScanFunction.apply(x, dt, A, B, C, skip, z, dt_bias, init, lengths, softplus, want_final, torch.is_grad_enabled())
     return (y, final) if want_final else y
+
+
+def _in_order(t, last=None):
+    """t with its positions or its channels contiguous; with `last`, its channels (True) or its positions (False)."""
+    channels = t.shape[1] == 1 or t.stride(1) == 1
+    positions = t.shape[2] == 1 or t.stride(2) == 1
+    if (channels or positions) if last is None else channels if last else positions:
+        return t
+    return t.transpose(1, 2).contiguous().transpose(1, 2) if last else t.contiguous()
+
+
+class EmbedFunction(torch.autograd.Function):
+    """blocks.conv1d_embed_fwd; its gradient is not differentiable again."""
+
+    @staticmethod
+    def forward(ctx, table, tokens, scale: float, lengths, channels_last: bool):
+        ctx.save_for_backward(tokens, lengths)
+        ctx.scale, ctx.V, ctx.type = scale, table.shape[0], table.dtype
+        return blocks.conv1d_embed_fwd(table.contiguous(), tokens, scale=scale, lengths=lengths, channels_last=channels_last)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        tokens, lengths = ctx.saved_tensors
+        dtable = blocks.conv1d_embed_bwd(_in_order(gy.resolve_neg().to(ctx.type)), tokens, ctx.V, scale=ctx.scale, lengths=lengths)
+        return dtable.to(ctx.type), None, None, None, None
+
+
+def conv1d_embed(table, tokens, scale: float = 1.0, lengths=None, channels_last: bool = False):
+    """y[N, D, L] = scale * table[tokens] (blocks.conv1d_embed_fwd)."""
+    return EmbedFunction.apply(table, tokens, scale, lengths, channels_last)
+
+
+class Embedding(torch.nn.Module):
+    """Tokens [N, L] to channels [N, D, L]: rows of a table of `tokens` rows, times `scale`."""
+
+    def __init__(self, tokens: int, channels: int, scale: float = 1.0, dtype=torch.float32, device="cuda"):
+        super().__init__()
+        self.scale = scale
+        self.weight = torch.nn.Parameter(torch.randn(tokens, channels, device=device).to(dtype))
+
+    def forward(self, tokens, lengths=None, channels_last: bool = False):
+        return conv1d_embed(self.weight, tokens, self.scale, lengths, channels_last)
+
+    def step(self, tokens):
+        """One token of every sequence, tokens[N]: [N, D]."""
+        with torch.no_grad():
+            return blocks.conv1d_embed_step(self.weight, tokens, scale=self.scale)
+
+
+class NormFunction(torch.autograd.Function):
+    """blocks.conv1d_norm_fwd; its gradients are not differentiable again."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups: int, relu: bool, silu: bool, eps: float, lengths):
+        x = _in_order(x)
+        ctx.types = [None if t is None else t.dtype for t in (weight, bias)]
+        weight, bias = (None if t is None else t.contiguous().float() for t in (weight, bias))
+        ctx.how = {"groups": groups, "relu": relu, "silu": silu, "eps": eps}
+        y, stats = blocks.conv1d_norm_fwd(x, weight=weight, bias=bias, lengths=lengths, want_stats=True, **ctx.how)
+        ctx.save_for_backward(x, weight, bias, lengths, stats)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        x, weight, bias, lengths, stats = ctx.saved_tensors
+        gy = _in_order(gy.resolve_neg().to(x.dtype), blocks._channels_last(x))
+        dx, dweight, dbias = blocks.conv1d_norm_bwd(gy, stats, x, weight=weight, bias=bias, lengths=lengths, **ctx.how)
+        dweight, dbias = (None if g is None else g.to(t) for g, t in zip((dweight, dbias), ctx.types))
+        return dx, dweight, dbias, None, None, None, None, None
+
+
+def conv1d_norm(x, groups: int, weight=None, bias=None, relu: bool = False, silu: bool = False, eps: float = 1e-5, lengths=None):
+    """y[N, C, L], the group norm of x[N, C, L] with an activation behind it (blocks.conv1d_norm_fwd)."""
+    return NormFunction.apply(x, weight, bias, groups, relu, silu, eps, lengths)
+
+
+class GroupNorm(torch.nn.Module):
+    """Group norm over `groups` groups of neighbouring channels, with weight and bias, and (relu, silu) an activation behind it."""
+
+    def __init__(self, groups: int, channels: int, eps: float = 1e-5, relu: bool = False, silu: bool = False, device="cuda"):
+        super().__init__()
+        self.groups, self.eps, self.relu, self.silu = groups, eps, relu, silu
+        self.weight = torch.nn.Parameter(torch.ones(channels, device=device))
+        self.bias = torch.nn.Parameter(torch.zeros(channels, device=device))
+
+    def forward(self, x, lengths=None):
+        return conv1d_norm(x, self.groups, self.weight, self.bias, self.relu, self.silu, self.eps, lengths)
+
+
+class DropoutFunction(torch.autograd.Function):
+    """blocks.conv1d_dropout: the backward pass finds the mask again; its gradients are not differentiable again."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p: float, key: int, call: int, counter, lengths):
+        ctx.save_for_backward(counter, lengths)
+        ctx.how, ctx.type = (p, key, call), x.dtype
+        return blocks.conv1d_dropout(_along(x), p, key, call, counter=counter, residual=_along(residual), lengths=lengths)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy):
+        counter, lengths = ctx.saved_tensors
+        gy = _along(gy.resolve_neg().to(ctx.type))
+        dx = blocks.conv1d_dropout(gy, *ctx.how, counter=counter, lengths=lengths) if ctx.needs_input_grad[0] else None
+        dr = None
+        if ctx.needs_input_grad[1]:
+            # behind a sequence's end y is 0, whatever the residual was
+            dr = gy if lengths is None else blocks.conv1d_dropout(gy, 0.0, 0, lengths=lengths)
+        return dx, dr, None, None, None, None, None
+
+
+def conv1d_dropout(x, p: float, key: int, call: int = 0, counter=None, residual=None, lengths=None):
+    """y[N, C, L] = residual + x / (1 - p) where an element is kept, residual elsewhere (blocks.conv1d_dropout)."""
+    return DropoutFunction.apply(x, residual, p, key, call, counter, lengths)
+
+
+class Dropout(torch.nn.Module):
+    """Dropout of a share `p`, with a residual: each call in training takes the next `call` of its key.  Layers have a key each.  A
+    captured step brings a `counter` that it moves on, since the calls' numbers are fixed in the graph."""
+
+    def __init__(self, p: float, key: int, call: int = 0):
+        super().__init__()
+        self.p, self.key, self.call = p, key, call
+
+    def forward(self, x, residual=None, lengths=None, counter=None):
+        if not self.training:
+            return conv1d_dropout(x, 0.0, 0, residual=residual, lengths=lengths)
+        self.call += 1
+        return conv1d_dropout(x, self.p, self.key, self.call - 1, counter, residual, lengths)

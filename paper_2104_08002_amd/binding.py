@@ -27,6 +27,9 @@ EXPORTS = (
     "conv1d_causal_fwd", "conv1d_causal_bwd_workspace_bytes", "conv1d_causal_bwd", "conv1d_causal_step",
     "conv1d_scan_fwd_workspace_bytes", "conv1d_scan_saved_bytes", "conv1d_scan_fwd", "conv1d_scan_bwd_workspace_bytes",
     "conv1d_scan_bwd", "conv1d_scan_step", "conv1d_grad_norm_workspace_bytes", "conv1d_grad_norm", "conv1d_grad_clip",
+    # what stands around the layers: marshalled in blocks.py
+    "conv1d_embed_fwd", "conv1d_embed_bwd_workspace_bytes", "conv1d_embed_bwd", "conv1d_norm_fwd_workspace_bytes", "conv1d_norm_fwd",
+    "conv1d_norm_bwd_workspace_bytes", "conv1d_norm_bwd", "conv1d_dropout",
 )
 
 _lib = None
@@ -100,6 +103,14 @@ def load() -> ctypes.CDLL:
         ("conv1d_grad_norm_workspace_bytes", sz, [vp, i]),
         ("conv1d_grad_norm", i, [vp, vp, vp, i, i, vp, vp, sz, vp]),
         ("conv1d_grad_clip", i, [vp, vp, vp, i, vp, f, vp]),
+        ("conv1d_embed_fwd", i, [vp, vp, vp, l, l, l, vp]),
+        ("conv1d_embed_bwd_workspace_bytes", sz, [i] * 5),
+        ("conv1d_embed_bwd", i, [vp, vp, l, l, l, vp, vp, sz, vp]),
+        ("conv1d_norm_fwd_workspace_bytes", sz, [i] * 4),
+        ("conv1d_norm_fwd", i, [vp, vp, l, l, l, vp, vp, sz, vp]),
+        ("conv1d_norm_bwd_workspace_bytes", sz, [i] * 4),
+        ("conv1d_norm_bwd", i, [vp, vp, l, l, l, vp, vp, l, l, l, vp, vp, vp, sz, vp]),
+        ("conv1d_dropout", i, [vp, vp, l, l, vp]),
     ):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = restype, argtypes
