@@ -376,7 +376,7 @@ typedef struct {
 int conv1d_embed_fwd(const conv1d_embed_t* p, const void* table, void* y, long y_sn, long y_sd, long y_sl, void* stream);
 
 /* dtable: [V][D] float, all of it: scale * the sum of dy over the positions of each token (0 for a token that is not there), in an
- * order that depends on the tokens alone.  dy: dtype, strides as for y. */
+ * order that depends on the tokens, the sizes and dy's strides alone.  dy: dtype, strides as for y. */
 size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype);
 int conv1d_embed_bwd(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy_sd, long dy_sl, float* dtable, void* workspace,
                      size_t workspace_bytes, void* stream);

@@ -115,7 +115,7 @@ def conv1d_embed_step(table, tokens, scale: float = 1.0, out=None):
 @_on_device
 def conv1d_embed_bwd(dy, tokens, V: int, scale: float = 1.0, lengths=None, workspace=None):
     """dtable [V, D] float32 for dy[N, D, L], positions or channels contiguous: scale times the sum of dy over the positions of each
-    token, in an order that depends on the tokens alone."""
+    token, in an order that depends on the tokens, the sizes and dy's strides alone."""
     if dy.dim() != 3 or 0 in dy.shape or V < 1:
         raise ValueError("dy must have the shape [N, D, L], none of it 0, and V be at least 1")
     (N, D, L), code, dev = dy.shape, binding._dtype_code(dy), dy.device

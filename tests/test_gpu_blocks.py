@@ -61,8 +61,13 @@ def _tokens(gen, N, L, V, kind, wide=True):
     return t.to(torch.int64 if wide else torch.int32)
 
 
+# Many tokens: 31 sums of up to 32 numbers in float and the product with the scale, 34 u.  Few: an instruction adds 32 products, each
+# addition cut off by less than 2 u of the magnitudes; up to 8 steps are added in float by each of four waves, and these; the scale: 75 u.
+GRAD = 75 * ref.U
+
 EMBED = [(1, 1, 1, 1), (2, 3, 7, 5), (3, 15, 1000, 5), (2, 64, 129, 255), (2, 65, 128, 256), (4, 16, 513, 257), (1, 17, 2049, 4000), (2, 130, 300, 70000), (5, 8, 64, 2),
-         (2, 2100, 40, 30), (1, 1, 40000, 3), (2, 512, 200, 1000)]
+         (2, 2100, 40, 30), (1, 1, 40000, 3), (2, 512, 200, 1000), (70, 20, 9, 300), (9, 40, 1000, 1024),
+         (3, 33, 700, 1025)]
 
 
 @TYPES
@@ -82,12 +87,12 @@ def test_embedding(blocks, dtype, last, kind, lengths, N, D, L, V):
     t = tokens.long()
     there = ((t >= 0) & (t < V))[:, None] & ref.inside(lengths, N, L)
     dy = torch.where(there, dy, float("nan"))
-    got = blocks.conv1d_embed_bwd(_put(dy, last, padded=True), tokens, V, scale=scale, lengths=lengths)
+    dy_in = _put(dy, last, padded=True)
+    got = blocks.conv1d_embed_bwd(dy_in, tokens, V, scale=scale, lengths=lengths)
     want, size = ref.embed_grad(torch.where(there, dy, 0.0), tokens, V, scale, lengths)
-    # 31 sums of up to 32 numbers in float, and the product with the scale
-    ref.near(got, want, 34 * ref.U * size, "dtable")
-    again = blocks.conv1d_embed_bwd(_put(dy, last), tokens, V, scale=scale, lengths=lengths)
-    assert torch.equal(got, again)
+    ref.near(got, want, GRAD * size, "dtable")
+    # the same call again; one channel is in either order, so that another stride may take another way
+    assert torch.equal(got, blocks.conv1d_embed_bwd(dy_in, tokens, V, scale=scale, lengths=lengths))
 
 
 @pytest.mark.parametrize("V", [255, 256, 65535, 65536, 1 << 20])
@@ -97,7 +102,7 @@ def test_embedding_of_as_many_tokens_as_digits_hold(blocks, V):
     tokens = torch.cat((torch.randint(0, V, (N, L - 3), generator=gen, device="cuda"), torch.tensor([[0, V - 1, V], [V - 1, 0, -1]], device="cuda")), 1)
     dy = _normal(gen, N, D, L)
     want, size = ref.embed_grad(dy, tokens, V, 1.0, None)
-    ref.near(blocks.conv1d_embed_bwd(dy, tokens, V), want, 34 * ref.U * size)
+    ref.near(blocks.conv1d_embed_bwd(dy, tokens, V), want, GRAD * size)
 
 
 def test_embedding_of_long_runs(blocks):
@@ -108,7 +113,29 @@ def test_embedding_of_long_runs(blocks):
     tokens[:, ::997] = torch.randint(0, V - 1, tokens[:, ::997].shape, generator=gen, device="cuda")
     dy = _normal(gen, N, D, L)
     want, size = ref.embed_grad(dy, tokens, V, 0.5, None)
-    ref.near(blocks.conv1d_embed_bwd(dy, tokens, V, scale=0.5), want, 34 * ref.U * size)
+    ref.near(blocks.conv1d_embed_bwd(dy, tokens, V, scale=0.5), want, GRAD * size)
+
+
+@TYPES
+@ORDER
+@pytest.mark.parametrize("V", [3, 40, 2000])
+def test_embedding_gradients_that_are_not_finite(blocks, dtype, last, V):
+    """They reach the rows of their own tokens alone, in their own channels."""
+    gen = _gen(V)
+    N, D, L = 2, 37, 600
+    tokens, dy = torch.randint(0, V, (N, L), generator=gen, device="cuda"), _normal(gen, N, D, L).to(dtype)
+    fine = blocks.conv1d_embed_bwd(_put(dy, last), tokens, V)
+    inf = float("inf")
+    for bad in ((float("nan"),), (inf,), (-inf,), (inf, inf), (inf, -inf), (torch.finfo(dtype).max,) * 2):
+        z, t, want = dy.clone(), tokens.clone(), fine.clone()
+        places = [(0, 5, 17), (1, 5, 599)][:len(bad)]
+        for (n, d, l), v in zip(places, bad):
+            z[n, d, l] = v
+            t[n, l] = 1
+        want = blocks.conv1d_embed_bwd(_put(dy, last), t, V)
+        want[1, 5] = sum(bad) if sum(bad) != sum(bad) or abs(sum(bad)) == inf else inf
+        got = blocks.conv1d_embed_bwd(_put(z, last), t, V)
+        assert torch.equal(got.nan_to_num(1e30, 2e30, 3e30), want.nan_to_num(1e30, 2e30, 3e30)), bad
 
 
 @TYPES
