@@ -39,7 +39,6 @@ inline int lds_add(int* p, int v) {
     *p += v;
     return old;
 }
-inline int global_add(int* p, int v) { return lds_add(p, v); }
 inline void lds_add(float* p, float v) { *p += v; }
 inline int popcount64(unsigned long v) { return __builtin_popcountl(v); }
 inline int first_bit(unsigned long v) { return __builtin_ctzl(v | (1UL << 63)); }
@@ -49,7 +48,6 @@ __device__ __forceinline__ unsigned long wave_ballot(bool v) { return __ballot(v
 __device__ __forceinline__ int lane_from(int v, int lane) { return __shfl(v, lane, kSeqWave); }
 __device__ __forceinline__ int lds_add(int* p, int v) { return atomicAdd(p, v); }
 __device__ __forceinline__ void lds_add(float* p, float v) { atomicAdd(p, v); }
-__device__ __forceinline__ int global_add(int* p, int v) { return atomicAdd(p, v); }
 __device__ __forceinline__ int popcount64(unsigned long v) { return __popcll(v); }
 __device__ __forceinline__ int first_bit(unsigned long v) { return __ffsll(static_cast<unsigned long long>(v)) - 1; }
 __device__ __forceinline__ int lane_up(int v, int by) { return __shfl_up(v, by, kSeqWave); }

@@ -77,21 +77,22 @@ __global__ __launch_bounds__(kThreads) void embed_turn_kernel(LookArgs a) {
 }
 
 // Few tokens: the workgroup's channels of the whole table, scaled and rounded, lie in LDS (and a row of zeros for no token); a lane has
-// 8 positions, whose tokens it keeps.
+// 8 positions, whose tokens (read side by side, and handed over in LDS) it keeps.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void embed_few_kernel(LookArgs a) {
     using T = typename RowElem<BF16>::type;
     extern __shared__ char dynamic[];
-    T* lds = reinterpret_cast<T*>(dynamic);
     const int unit = static_cast<int>(blockIdx.x) + static_cast<int>(a.first);
     const int nt = div31(unit, a.by_blocks), d0 = (unit - nt * a.blocks) * a.per_row, n = div31(nt, a.by_tiles);
     const int l = ((nt - n * a.tiles) * kThreads + static_cast<int>(threadIdx.x)) * 8;
     const int len = seq_length(a.lengths, n, a.L), many = min(a.per_row, a.D - d0);
-    int at[8];
+    const int first = l - 8 * static_cast<int>(threadIdx.x);
+    unsigned short* toks = reinterpret_cast<unsigned short*>(dynamic);  // 16 bits each
+    T* lds = reinterpret_cast<T*>(dynamic + 2 * 8 * kThreads);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int t = token_at(a.tokens, a.wide, n, a.tok_sn, l + e, len, a.V);
-        at[e] = (t < 0 ? a.V : t) * many;
+        const int p = e * kThreads + static_cast<int>(threadIdx.x), t = token_at(a.tokens, a.wide, n, a.tok_sn, first + p, len, a.V);
+        toks[p] = static_cast<unsigned short>(t < 0 ? a.V : t);
     }
     for (int i = static_cast<int>(threadIdx.x); i < (a.V + 1) * many; i += kThreads) {
         const int v = i / many;
@@ -100,9 +101,13 @@ __global__ __launch_bounds__(kThreads) void embed_few_kernel(LookArgs a) {
     }
     __syncthreads();
     if (l >= a.L) return;
+    const seq_u16x8 mine = *reinterpret_cast<const seq_u16x8*>(toks + 8 * threadIdx.x);
+    int at[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) at[e] = min(static_cast<int>(mine[e]), a.V) * many;
     T* y = static_cast<T*>(a.y) + n * a.y_sn + d0 * a.y_sd;
     typedef __attribute__((ext_vector_type(8), aligned(BF16 ? 2 : 4))) T vec8;
-#pragma unroll 2
+#pragma unroll 4
     for (int d = 0; d < many; ++d) {
         vec8 v;
 #pragma unroll
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 // B operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum
 // they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
 // running sum by an ordinary addition.  A value that is not finite would reach every token (0 * NaN): where a sum is not finite, the
-// wave goes through its positions again without such values, which are then added where they belong.
+// wave workgroup goes through its positions again without such values, which are then added where they belong.
 constexpr int kFewTokens = 1024;
 
 struct FewArgs {
@@ -162,27 +167,6 @@ typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 struct Tokens8 {
     unsigned t[4];
 };
-__device__ __forceinline__ Tokens8 tokens8(const FewArgs& a, long n, int l, int len) {
-    unsigned u[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const long at = n * a.tok_sn + min(l + e, a.L - 1);
-        bool fine = l + e < len;
-        if (a.wide) {
-            const long t = static_cast<const long*>(a.tokens)[at];
-            fine &= static_cast<unsigned long>(t) < static_cast<unsigned long>(a.V);
-            u[e] = static_cast<unsigned>(t);
-        } else {
-            u[e] = static_cast<unsigned>(static_cast<const int*>(a.tokens)[at]);
-            fine &= u[e] < static_cast<unsigned>(a.V);
-        }
-        u[e] = fine ? u[e] : 0xffffu;
-    }
-    Tokens8 r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.t[i] = u[2 * i] | (u[2 * i + 1] << 16);
-    return r;
-}
 // bfloat16 1 where a token is v, 0 elsewhere
 __device__ __forceinline__ u32x4 truth8(const Tokens8& k, int v) {
     const u16x2 vv = static_cast<u16x2>(static_cast<unsigned short>(v));
@@ -200,26 +184,55 @@ template <bool BF16>
 struct Parts {
     u32x4 p[BF16 ? 1 : 3];
 };
-template <bool BF16, bool FINITE>
-__device__ __forceinline__ Parts<BF16> parts8(const void* row, int l, int len) {
-    Parts<BF16> r;
-    if constexpr (BF16 && !FINITE) {
-        if (l + 8 <= len) {
-            const seq_u16x8 v = *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + l);
-            r.p[0] = __builtin_bit_cast(u32x4, v);
-            return r;
-        }
+// 8 positions of a channel as they lie in memory: all of them there, or those before len, 0 behind
+template <bool BF16>
+struct Raw8 {
+    u32x4 v[BF16 ? 1 : 2];
+};
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> raw8_inside(const void* row, int l) {
+    Raw8<BF16> r;
+    if constexpr (BF16) {
+        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + l));
+    } else {
+        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l));
+        r.v[1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l + 4));
     }
+    return r;
+}
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> raw8(const void* row, int l, int len) {
     float v[8];
     row_load8<BF16>(row, l, len, v);
-    if constexpr (FINITE) {
+    Raw8<BF16> r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+            r.v[0][i] = sp::pack_hi(v[2 * i], v[2 * i + 1]);
+        } else {
+            r.v[0][i] = __float_as_uint(v[i]);
+            r.v[1][i] = __float_as_uint(v[4 + i]);
+        }
     }
+    return r;
+}
+template <bool BF16, bool FINITE>
+__device__ __forceinline__ Parts<BF16> parts_of(const Raw8<BF16>& x) {
+    Parts<BF16> r;
     if constexpr (BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.p[0][i] = sp::pack_hi(v[2 * i], v[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) {
+            unsigned u = x.v[0][i];
+            if constexpr (FINITE) u = ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
+            r.p[0][i] = u;
+        }
     } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = __uint_as_float(x.v[e >> 2][e & 3]);
+            if constexpr (FINITE) v[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
+        }
         const sp::Split8 s = sp::split8(v);
         r.p[0] = s.l;
         r.p[1] = s.m;
@@ -228,59 +241,93 @@ __device__ __forceinline__ Parts<BF16> parts8(const void* row, int l, int len) {
     return r;
 }
 
-constexpr int kWaves = kThreads / kSeqWave;
-
-// A wave's steps of 32 positions: every kWaves-th of its chunk's.
-struct Steps {
-    int n0, from, to, per, all;  // first sample, positions of each, steps of a sample and of all
-};
-__device__ __forceinline__ Steps steps_of(const FewArgs& a, int chunk) {
-    Steps r;
-    const int of = div31(chunk, a.by_sample);
-    r.n0 = of * a.samples;
-    r.from = (chunk - of * a.per_sample) * a.chunk;
-    r.to = min(a.L, r.from + a.chunk);
-    r.per = (r.to - r.from + 31) >> 5;
-    r.all = r.per * min(a.samples, a.N - r.n0);
-    return r;
+__device__ __forceinline__ void floats_of(const Raw8<true>& x, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(x.v[0][i] << 16);
+        v[2 * i + 1] = __uint_as_float(x.v[0][i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void floats_of(const Raw8<false>& x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x.v[e >> 2][e & 3]);
 }
 
+constexpr int kWaves = kThreads / kSeqWave;
+
+// A chunk: positions [from, to) of `samples` samples from n0 on, taken in blocks of kWaves waves' U steps of 32 positions.
+struct Chunk {
+    int n0, samples, from, to;
+};
+__device__ __forceinline__ Chunk chunk_of(const FewArgs& a, int chunk) {
+    Chunk r;
+    const int of = div31(chunk, a.by_sample);
+    r.n0 = of * a.samples;
+    r.samples = min(a.samples, a.N - r.n0);
+    r.from = (chunk - of * a.per_sample) * a.chunk;
+    r.to = min(a.L, r.from + a.chunk);
+    return r;
+}
+template <bool BF16>
+constexpr int kU = BF16 ? 4 : 2;   // steps whose loads a wave has in flight
+constexpr int kMostBlock = 32 * kWaves * 4;
+
 template <bool BF16, bool FINITE, int VB, int DB>
-__device__ __forceinline__ void few_sums(const FewArgs& a, const Steps& t, int v0, int d0, f32x4 (&acc)[VB][DB]) {
+__device__ __forceinline__ void few_sums(const FewArgs& a, const Chunk& t, int v0, int d0, f32x4 (&acc)[VB][DB], unsigned short (*toks)[kMostBlock]) {
     using T = typename RowElem<BF16>::type;
-    const int lane = static_cast<int>(threadIdx.x) & (kSeqWave - 1);
+    constexpr int U = kU<BF16>, BLOCK = 32 * kWaves * U;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), wave = tid / kSeqWave;
 #pragma unroll
     for (int v = 0; v < VB; ++v)
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[v][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int i = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / kSeqWave), n = t.n0;
-    const T* rows[DB];
+    int turn = 0;
+    for (int n = t.n0; n < t.n0 + t.samples; ++n) {
+        const int len = min(t.to, seq_length(a.lengths, n, a.L));
+        const T* rows[DB];
 #pragma unroll
-    for (int d = 0; d < DB; ++d) rows[d] = static_cast<const T*>(a.dy) + n * a.dy_sn + min(d0 + 16 * d + (lane & 15), a.D - 1) * a.dy_sd;
-    for (int before = 0; i < t.all; i += kWaves) {
-        while (i - before >= t.per) {
-            before += t.per;
-            ++n;
+        for (int d = 0; d < DB; ++d) rows[d] = static_cast<const T*>(a.dy) + n * a.dy_sn + min(d0 + 16 * d + (lane & 15), a.D - 1) * a.dy_sd;
+        for (int l0 = t.from; l0 < len; l0 += BLOCK, turn ^= 1) {
+            const int mine = 32 * U * wave, l = l0 + mine + 8 * (lane >> 4);
+            Raw8<BF16> raw[U][DB];
+            if (l0 + BLOCK <= len) {
 #pragma unroll
-            for (int d = 0; d < DB; ++d) rows[d] += a.dy_sn;
-        }
-        const int len = min(t.to, seq_length(a.lengths, n, a.L)), l = t.from + 32 * (i - before) + 8 * (lane >> 4);
-        Parts<BF16> x[DB];
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) x[d] = parts8<BF16, FINITE>(rows[d], l, len);
-        const Tokens8 k = tokens8(a, n, l, len);
+                    for (int d = 0; d < DB; ++d) raw[u][d] = raw8_inside<BF16>(rows[d], l + 32 * u);
+            } else {
 #pragma unroll
-        for (int v = 0; v < VB; ++v) {
-            const u32x4 one = truth8(k, v0 + 16 * v + (lane & 15));
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                f32x4 s = sp::mfma(x[d].p[0], one, f32x4{0.f, 0.f, 0.f, 0.f});
-                if constexpr (!BF16) {
-                    s = sp::mfma(x[d].p[1], one, s);
-                    s = sp::mfma(x[d].p[2], one, s);
+                    for (int d = 0; d < DB; ++d) raw[u][d] = raw8<BF16>(rows[d], l + 32 * u, len);
+            }
+#pragma unroll
+            for (int p = tid; p < BLOCK; p += kThreads) {
+                const int tok = token_at(a.tokens, a.wide, n, a.tok_sn, l0 + p, len, a.V);
+                toks[turn][p] = static_cast<unsigned short>(tok);
+            }
+            __syncthreads();  // (the next block writes the other half, the one after that waits behind the next)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (l0 + mine + 32 * u >= len) break;
+                const Tokens8 k = *reinterpret_cast<const Tokens8*>(&toks[turn][mine + 32 * u + 8 * (lane >> 4)]);
+                Parts<BF16> x[DB];
+#pragma unroll
+                for (int d = 0; d < DB; ++d) x[d] = parts_of<BF16, FINITE>(raw[u][d]);
+#pragma unroll
+                for (int v = 0; v < VB; ++v) {
+                    const u32x4 one = truth8(k, v0 + 16 * v + (lane & 15));
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        f32x4 s = sp::mfma(x[d].p[0], one, f32x4{0.f, 0.f, 0.f, 0.f});
+                        if constexpr (!BF16) {
+                            s = sp::mfma(x[d].p[1], one, s);
+                            s = sp::mfma(x[d].p[2], one, s);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[v][d][e] += s[e];
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[v][d][e] += s[e];
             }
         }
     }
@@ -292,10 +339,14 @@ __global__ __launch_bounds__(kThreads) void embed_few_sums_kernel(FewArgs a) {
     __shared__ float lds[VB * 16][DB * 16 + 4];
     const int unit = static_cast<int>(blockIdx.x), cd = div31(unit, a.by_vgroups), v0 = (unit - cd * a.vgroups) * (16 * VB);
     const int chunk = div31(cd, a.by_dgroups), d0 = (cd - chunk * a.dgroups) * (16 * DB);
-    const Steps t = steps_of(a, chunk);
+    const Chunk t = chunk_of(a, chunk);
+    __shared__ unsigned short toks[2][kMostBlock];
+    __shared__ int bad;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), wave = tid / kSeqWave;
     f32x4 acc[VB][DB];
-    few_sums<BF16, false, VB, DB>(a, t, v0, d0, acc);
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    few_sums<BF16, false, VB, DB>(a, t, v0, d0, acc, toks);
     bool fine = true;
 #pragma unroll
     for (int v = 0; v < VB; ++v)
@@ -303,8 +354,10 @@ __global__ __launch_bounds__(kThreads) void embed_few_sums_kernel(FewArgs a) {
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) fine &= fabsf(acc[v][d][i]) < INFINITY;
-    const bool again = !wave_all(fine);
-    if (again) few_sums<BF16, true, VB, DB>(a, t, v0, d0, acc);
+    if (!fine) bad = 1;
+    __syncthreads();
+    const bool again = bad != 0;  // (of any wave: the tokens are staged by all)
+    if (again) few_sums<BF16, true, VB, DB>(a, t, v0, d0, acc, toks);
     for (int w = 0; w < kWaves; ++w) {
         if (w == wave) {
 #pragma unroll
@@ -319,14 +372,15 @@ __global__ __launch_bounds__(kThreads) void embed_few_sums_kernel(FewArgs a) {
         __syncthreads();
     }
     if (again) {  // a number added to one that is not finite, or two such numbers: any order gives the same
-        for (int i = wave; i < t.all; i += kWaves) {
-            const int n = t.n0 + i / t.per, l0 = t.from + 32 * (i % t.per), len = min(t.to, seq_length(a.lengths, n, a.L));
-            for (int j = lane; j < 32 * 16 * DB; j += kSeqWave) {
-                const int l = l0 + (j & 31), d = d0 + (j >> 5);
-                if (l >= len || d >= a.D) continue;
-                const int tok = token_at(a.tokens, a.wide, n, a.tok_sn, l, len, a.V);
+        for (int n = t.n0; n < t.n0 + t.samples; ++n) {
+            const int len = min(t.to, seq_length(a.lengths, n, a.L)), many = max(0, len - t.from);
+            for (long i = tid; i < static_cast<long>(many) * (16 * DB); i += kThreads) {
+                const int d = d0 + static_cast<int>(i / many), l = t.from + static_cast<int>(i % many);
+                if (d >= a.D) break;
                 const float v = load_elem<BF16>(static_cast<const T*>(a.dy) + n * a.dy_sn + d * a.dy_sd, l);
-                if (tok >= v0 && tok < v0 + 16 * VB && !(fabsf(v) < INFINITY)) lds_add(&lds[tok - v0][d - d0], v);
+                if (fabsf(v) < INFINITY) continue;
+                const int tok = token_at(a.tokens, a.wide, n, a.tok_sn, l, len, a.V);
+                if (tok >= v0 && tok < v0 + 16 * VB) lds_add(&lds[tok - v0][d - d0], v);
             }
         }
     }
@@ -359,10 +413,11 @@ __global__ __launch_bounds__(kFewJoin) void embed_few_join_kernel(FewArgs a) {
 }
 
 // ---- backward, many tokens: the positions in the order of their tokens ---------------------------------------------------------
-// Keys are tokens, V for no token: those come last.  A pass of the sort takes up to 8 bits.  The first launch counts the digits of each
-// tile of keys; each pass's launch finds where its tile's keys go (from the counts of all tiles, which are few, or made into places by
-// a launch between), puts them there in their order, and counts the next pass's digits where they went.  These launches wait for
-// memory most of the time: their other workgroups turn dy into rows and clear the gradient meanwhile.
+// Keys are tokens, V for no token: those come last.  A pass of the sort takes up to 8 bits, in two launches: one counts the digits of
+// each tile of keys; in the other each workgroup finds where its tile's keys go (from the counts of all tiles, which are few, or made
+// into places by a launch between) and puts them there in their order.  These launches wait for memory most of the time: their other
+// workgroups turn dy into rows and clear the gradient meanwhile.  (Counting the next pass's digits where the keys are put saves a
+// launch, but a frequent token's are all counted in one place: 56 us for 160000 positions, of which 18000 have the same token.)
 constexpr int kBins = 256;
 constexpr int kSort = 1024, kSortWaves = kSort / kSeqWave;
 constexpr int kKeys = 4;          // most keys of a lane
@@ -375,12 +430,11 @@ struct SortArgs {
     int wide, N, D, L, V, M;
     Div31 by_L;
     int *keys[2], *pos[2];        // pass p writes to [p & 1] and reads from the other; the first reads the tokens
-    int *counts, *totals;         // [passes][tiles][kBins], [kBins]
-    int *owners;                  // [0]: how many runs cross chunks (cleared here), then their chunks
+    int *counts, *totals;         // [tiles][kBins], [kBins]
     void* rows;                   // [M][8 * per_row]: dy's columns
     float* dtable;
     long zeros;                   // elements of dtable
-    int pass, passes, bits, tiles, per_lane, before;  // pass -1: count; before: counts hold places
+    int pass, count, bits, tiles, per_lane, before;  // count: this launch counts; before: counts hold places
     int sorts, turns, jobs, per_row;   // workgroups that sort, tiles to turn, these and pieces to clear
     int first_job, l_tiles, d_blocks;
     Div31 by_d_blocks, by_l_tiles;
@@ -396,14 +450,11 @@ __device__ __forceinline__ int key_at(const SortArgs& a, int m) {
 __device__ __forceinline__ void count_digits(const SortArgs& a, int* count) {
     const int tid = static_cast<int>(threadIdx.x), tile = static_cast<int>(blockIdx.x), bins = 1 << a.bits;
     if (tid < kBins) count[tid] = 0;
-    if (tile == 0 && tid == 0) a.owners[0] = 0;
-    for (int p = 1; p < a.passes; ++p)
-        if (tid < kBins) a.counts[(static_cast<long>(p) * a.tiles + tile) * kBins + tid] = 0;
     __syncthreads();
     const long first = static_cast<long>(tile) * a.per_lane * kSort;
     for (int k = 0; k < a.per_lane; ++k) {
         const long m = first + k * kSort + tid;
-        if (m < a.M) lds_add(&count[key_at(a, static_cast<int>(m)) & (bins - 1)], 1);
+        if (m < a.M) lds_add(&count[(key_at(a, static_cast<int>(m)) >> (a.pass * a.bits)) & (bins - 1)], 1);
     }
     __syncthreads();
     if (tid < kBins) a.counts[static_cast<long>(tile) * kBins + tid] = count[tid];
@@ -433,14 +484,15 @@ struct SortLds {
 __device__ __forceinline__ void put_keys(const SortArgs& a, SortLds& s) {
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), wave = tid / kSeqWave, tile = static_cast<int>(blockIdx.x);
     const int bins = 1 << a.bits, shift = a.pass * a.bits, digit_of = tid & (kBins - 1), slice = tid / kBins;
-    const int* counts = a.counts + static_cast<long>(a.pass) * a.tiles * kBins;
+    const int* counts = a.counts;
     const long first = static_cast<long>(tile) * a.per_lane * kSort + wave * (a.per_lane * kSeqWave) + lane;
-    int key[kKeys], mine[kKeys];
+    int key[kKeys], mine[kKeys], pos[kKeys];
 #pragma unroll
     for (int k = 0; k < kKeys; ++k) {
         if (k >= a.per_lane) break;
-        const long m = first + k * kSeqWave;
-        key[k] = key_at(a, static_cast<int>(m < a.M ? m : a.M - 1));
+        const int m = static_cast<int>(min(first + k * kSeqWave, a.M - 1L));
+        key[k] = key_at(a, m);
+        pos[k] = a.pass > 0 ? a.pos[(a.pass & 1) ^ 1][m] : m;
     }
 #pragma unroll
     for (int w = 0; w < kSortWaves; w += kSort / kBins) s.place[w + slice][digit_of] = 0;
@@ -505,14 +557,9 @@ __device__ __forceinline__ void put_keys(const SortArgs& a, SortLds& s) {
         const long m = first + k * kSeqWave;
         if (k >= a.per_lane || m >= a.M) break;
         const int to = s.place[wave][(key[k] >> shift) & (bins - 1)] + mine[k];
-        const int pos = a.pass > 0 ? a.pos[out ^ 1][m] : static_cast<int>(m);
-        if (to < 0 || to >= a.M || pos < 0 || pos >= a.M) continue;  // (never, as long as the tokens do not change meanwhile)
+        if (to < 0 || to >= a.M || pos[k] < 0 || pos[k] >= a.M) continue;  // (never, as long as the tokens do not change meanwhile)
         a.keys[out][to] = key[k];
-        a.pos[out][to] = pos;
-        if (a.pass + 1 < a.passes) {
-            const long tile_to = to / (a.per_lane * kSort), digit = (key[k] >> (shift + a.bits)) & (bins - 1);
-            global_add(&a.counts[((a.pass + 1L) * a.tiles + tile_to) * kBins + digit], 1);
-        }
+        a.pos[out][to] = pos[k];
     }
 }
 
@@ -520,7 +567,7 @@ __device__ __forceinline__ void put_keys(const SortArgs& a, SortLds& s) {
 __global__ __launch_bounds__(kSort) void embed_places_kernel(SortArgs a) {
     __shared__ int sum[kSort / 16][16];
     const int tid = static_cast<int>(threadIdx.x), o = tid & 15, share = tid >> 4, digit = 16 * static_cast<int>(blockIdx.x) + o;
-    int* counts = a.counts + static_cast<long>(a.pass) * a.tiles * kBins + digit;
+    int* counts = a.counts + digit;
     const int each = (a.tiles + kSort / 16 - 1) / (kSort / 16), from = min(a.tiles, share * each), to = min(a.tiles, from + each);
     int n = 0;
 #pragma unroll 4
@@ -583,7 +630,7 @@ __global__ __launch_bounds__(kSort) void embed_sort_kernel(SortArgs a) {
     } lds;
     const int block = static_cast<int>(blockIdx.x), tid = static_cast<int>(threadIdx.x);
     if (block < a.sorts) {
-        if (a.pass < 0) count_digits(a, lds.sort.place[0]);
+        if (a.count) count_digits(a, lds.sort.place[0]);
         else put_keys(a, lds.sort);
         return;
     }
@@ -604,13 +651,13 @@ __global__ __launch_bounds__(kSort) void embed_sort_kernel(SortArgs a) {
 struct SumArgs {
     const void* rows;        // row m is position m's, stride apart (samples: sample_stride)
     const int *keys, *pos;
-    int* owners;
-    float *head, *tail;      // [chunks][per_row * 8]: what of a chunk belongs to a run that began before it, that goes on behind it
+    float *head, *tail;      // [groups of chunks][per_row * 8]: what of a workgroup's rows belongs to a run that began before them, that goes on behind
     float* dtable;
     long sample_stride, stride;
     float scale;
-    int D, L, V, M, per_row, chunk, chunks, first, items;
-    Div31 by_row, by_L;
+    int D, L, V, M, per_row, chunk, first;
+    int cols, teams, blocks;  // vectors of a row that a workgroup has, its lane groups, workgroups of a row
+    Div31 by_blocks, by_L;
 };
 
 __device__ __forceinline__ void float_store8(float* row, int at, int end, const float (&v)[8], float scale) {
@@ -620,111 +667,222 @@ __device__ __forceinline__ void float_store8(float* row, int at, int end, const 
     row_store8<false>(row, at, end, s);
 }
 
-template <bool BF16, bool TURNED>
+// A workgroup has the chunks of kThreads / cols lane groups, cols of the vectors of a row each; their keys and positions, one behind the
+// other, go through LDS, so that a lane's loads of rows wait for nothing else.
+constexpr int kMostChunk = 32, kMostTeams = 64, kAheadRows = 8;
+__device__ __forceinline__ void keep(f32x4 (&at)[2], const float (&v)[8]) {
+    at[0] = f32x4{v[0], v[1], v[2], v[3]};
+    at[1] = f32x4{v[4], v[5], v[6], v[7]};
+}
+// Adds to `sum` the heads of chunk t and of those behind it that its run goes on in, in 64 bits; returns the last one.
+__device__ __forceinline__ int join_on(const f32x4 (*heads)[2], const int* passes, int at, int cols, int t, int last, float (&sum)[8]) {
+    double s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = sum[e];
+    for (;; ++t, at += cols) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += static_cast<double>(heads[at][e >> 2][e & 3]);
+        if (!passes[t] || t >= last) break;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = static_cast<float>(s[e]);
+    return t;
+}
+
+// Where a sum goes and when is found for every row: the code for it is kept short (one kind of store, no call), because it stands
+// kAheadRows times in the loop, and instructions come from memory as well.
+template <bool BF16, bool TURNED, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void embed_sums_kernel(SumArgs a) {
     using T = typename RowElem<BF16>::type;
-    const int item = static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x);
-    if (item >= a.items) return;
-    const int of = div31(item, a.by_row), chunk = a.first + of, d = 8 * (item - of * a.per_row);
-    const int from = chunk * a.chunk, to = min(a.M, from + a.chunk);
-    int key = a.keys[from];
-    if (key >= a.V) return;
-    bool began = from == 0 || a.keys[from - 1] != key;
-    const int width = 8 * a.per_row;
+    __shared__ int keys[kMostTeams * kMostChunk + 2], pos[kMostTeams * kMostChunk], passes[kMostTeams];
+    __shared__ f32x4 heads[kThreads][2];
+    const int tid = static_cast<int>(threadIdx.x), unit = static_cast<int>(blockIdx.x) + a.first, group = div31(unit, a.by_blocks), block = unit - group * a.blocks;
+    const int team = tid / a.cols, col = block * a.cols + tid - team * a.cols;
+    const int first = group * a.teams * a.chunk, rows = min(a.M - first, a.teams * a.chunk);
+    for (int i = tid; i < rows + 2; i += kThreads) {  // the keys before and behind too
+        const int m = first + i - 1;
+        keys[i] = m >= 0 && m < a.M ? a.keys[m] : a.V;
+        if (i < rows) pos[i] = a.pos[first + i];
+    }
+    __syncthreads();
+    const bool mine = team < a.teams && team * a.chunk < rows && col < a.per_row;
+    const int d = 8 * col, from = mine ? team * a.chunk : 0, to = mine ? min(rows, from + a.chunk) : 0, there = WHOLE ? 8 : min(8, a.D - d);
+    const long side = static_cast<long>(group) * (8 * a.per_row) + d;
+    int key = mine ? keys[1 + from] : a.V;
+    bool began = mine && (first + from == 0 || keys[from] != key);  // the run at hand began in this chunk
+    bool open = key < a.V;                                         // and is one
+    bool came = open && !began;                                    // the chunk's first run began before it
     float sum[8] = {};
-    constexpr int kAhead = 8;
-#pragma unroll 1
-    for (int i0 = from; i0 < to; i0 += kAhead) {
-        float v[kAhead][8];
-        int k[kAhead];
+    const auto put = [&](float* o, float scale, bool all, const float (&v)[8]) {
+        if constexpr (WHOLE) {
+            *reinterpret_cast<seq_f32x4*>(o) = seq_f32x4{v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale};
+            *reinterpret_cast<seq_f32x4*>(o + 4) = seq_f32x4{v[4] * scale, v[5] * scale, v[6] * scale, v[7] * scale};
+        } else {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int i = min(i0 + j, a.M - 1), m = a.pos[i];
-            k[j] = a.keys[i];
+            for (int e = 0; e < 8; ++e)
+                if (all || e < there) o[e] = v[e] * scale;
+        }
+    };
+#pragma unroll 1
+    for (int i0 = from; i0 < to && open; i0 += kAheadRows) {
+        Raw8<BF16> raw[kAheadRows];
+#pragma unroll
+        for (int j = 0; j < kAheadRows; ++j) {
+            const int m = clampi(pos[min(i0 + j, to - 1)], 0, a.M - 1);
             if constexpr (TURNED) {
-                row_load8_inside<BF16>(static_cast<const T*>(a.rows) + m * a.stride, d, v[j]);
+                raw[j] = raw8_inside<BF16>(static_cast<const T*>(a.rows) + m * a.stride, d);
             } else {
                 const int n = div31(m, a.by_L), l = m - n * a.L;
-                row_load8<BF16>(static_cast<const T*>(a.rows) + n * a.sample_stride + l * a.stride, d, a.D, v[j]);
+                const T* row = static_cast<const T*>(a.rows) + n * a.sample_stride + l * a.stride;
+                if constexpr (WHOLE) raw[j] = raw8_inside<BF16>(row, d);
+                else raw[j] = raw8<BF16>(row, d, a.D);
             }
         }
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (i0 + j >= to) break;
-            if (k[j] != key) {
-                if (began) float_store8(a.dtable + static_cast<long>(key) * a.D, d, a.D, sum, a.scale);
-                else float_store8(a.head + static_cast<long>(chunk) * width, d, width, sum, 1.f);
-                if (k[j] >= a.V) return;
-                key = k[j];
+        for (int j = 0; j < kAheadRows; ++j) {
+            const int k = i0 + j < to ? keys[1 + i0 + j] : key;
+            if (k != key && open) {
+                if (began) put(a.dtable + static_cast<long>(key) * a.D + d, a.scale, false, sum);
+                else keep(heads[tid], sum);
+                open = k < a.V;
+                key = k;
                 began = true;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = 0.f;
             }
+            float v[8];
+            floats_of(raw[j], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += v[j][e];
+            for (int e = 0; e < 8; ++e) sum[e] += i0 + j < to ? v[e] : 0.f;
         }
     }
-    if (!began) {
-        float_store8(a.head + static_cast<long>(chunk) * width, d, width, sum, 1.f);
-    } else if (to < a.M && a.keys[to] == key) {
-        float_store8(a.tail + static_cast<long>(chunk) * width, d, width, sum, 1.f);
-        if (d == 0) a.owners[1 + global_add(a.owners, 1)] = chunk;
-    } else {
-        float_store8(a.dtable + static_cast<long>(key) * a.D, d, a.D, sum, a.scale);
+    // what of a run lies in several chunks of the workgroup is put together here
+    const bool goes_on = open && first + to < a.M && keys[1 + to] == key;
+    if (open && !began) keep(heads[tid], sum);
+    const bool pass = came && !began && goes_on;  // the chunk lies within one run
+    if (tid - team * a.cols == 0 && team < a.teams) passes[team] = pass;
+    __syncthreads();
+    if (!mine) return;
+    const int last = (rows - 1) / a.chunk;  // the last chunk that is there
+    if (came && team == 0) {
+        float head[8] = {};
+        join_on(heads, passes, tid, a.cols, 0, last, head);
+        put(a.head + side, 1.f, true, head);
     }
+    if (!open || !began) return;
+    bool behind = goes_on;
+    if (goes_on && team < last) {
+        const int end = join_on(heads, passes, tid + a.cols, a.cols, team + 1, last, sum);
+        behind = passes[end];
+    }
+    put(behind ? a.tail + side : a.dtable + static_cast<long>(key) * a.D + d, behind ? 1.f : a.scale, behind, sum);
 }
 
-// Runs that cross chunks, in any order: what the chunks behind the one where a run begins have of it is added to that one's.
+// Runs that cross the rows of one workgroup, its chunk here: what the chunks behind the one where a run begins have of it is added to that one's, by that chunk's lane group
+// where those are few, by the whole workgroup where a run is long.
 struct JoinArgs {
-    const int *keys, *owners;
+    const int* keys;
     const float *head, *tail;
     float* dtable;
     float scale;
-    int D, V, M, per_row, chunk, chunks;
+    int D, V, M, per_row, chunk, chunks, first;
+    int cols, teams;  // vectors of a row that a lane group takes at a time, lane groups of a workgroup
 };
-// the first place of a key >= v
-__device__ __forceinline__ int place_of(const int* keys, int M, int v) {
-    int lo = 0, hi = M;
-    while (lo < hi) {
-        const int mid = lo + ((hi - lo) >> 1);
-        if (keys[mid] < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
+constexpr int kJoin = 256, kShort = 16;
+// whether the run at the end of `chunk` goes on in the first rows of chunk + i
+__device__ __forceinline__ bool goes_on(const JoinArgs& a, int key, long chunk, int i) {
+    const long at = (chunk + i) * a.chunk;
+    return at < a.M && a.keys[at] == key;
 }
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(JoinArgs a) {
-    __shared__ double lds[kThreads][8];
-    const int tid = static_cast<int>(threadIdx.x), width = 8 * a.per_row, cols = min(a.per_row, kThreads), teams = kThreads / cols, team = tid / cols;
-    const int many = min(a.owners[0], a.chunks - 1);
-    for (int i = static_cast<int>(blockIdx.x); i < many; i += static_cast<int>(gridDim.x)) {
-        const int chunk = clampi(a.owners[1 + i], 0, a.chunks - 2), key = a.keys[(chunk + 1) * a.chunk - 1];
-        const int last = max(chunk, (place_of(a.keys, a.M, key + 1) - 1) / a.chunk);  // the chunk where it ends
-        if (key < 0 || key >= a.V) continue;  // (never)
-        for (int c0 = 0; c0 < a.per_row; c0 += cols) {
-            const int d = 8 * (c0 + tid - team * cols);
-            double sum[8] = {};
-            if (team < teams && d < width) {
-#pragma unroll 4
-                for (int c = chunk + team; c <= last; c += teams) {
-                    float v[8];
-                    row_load8_inside<false>((c == chunk ? a.tail : a.head) + static_cast<long>(c) * width, d, v);
+// 8 columns of a chunk's share
+__device__ __forceinline__ void share(const JoinArgs& a, int c, bool first, int d, float (&v)[8]) {
+    row_load8_inside<false>((first ? a.tail : a.head) + static_cast<long>(c) * (8 * a.per_row), d, v);
+}
+__global__ __launch_bounds__(kJoin) void embed_join_kernel(JoinArgs a) {
+    __shared__ double lds[4][kJoin];
+    __shared__ int longs[kJoin];
+    const int tid = static_cast<int>(threadIdx.x), team = tid / a.cols, lane = tid - team * a.cols, first = a.first + static_cast<int>(blockIdx.x) * a.teams;
+    if (tid < a.teams) longs[tid] = 0;
+    __syncthreads();
+    const int chunk = first + team;
+    if (team < a.teams && chunk < a.chunks - 1) {
+        const long behind = (static_cast<long>(chunk) + 1) * a.chunk, from = behind - a.chunk;
+        const int key = a.keys[behind - 1];
+        const bool earlier = a.keys[from] == key && from > 0 && a.keys[from - 1] == key;
+        if (key >= 0 && key < a.V && a.keys[behind] == key && !earlier) {
+            bool on[kShort];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            for (int i = 0; i < kShort; ++i) on[i] = goes_on(a, key, chunk, i + 2);
+            int many = 1;  // chunks that it goes on in; kShort + 1: that many or more
+#pragma unroll
+            for (int i = 0; i < kShort; ++i) many += many == i + 1 && on[i];
+            if (many > kShort) {
+                if (lane == 0) longs[team] = 1;
+            } else {
+                for (int c0 = lane; c0 < a.per_row; c0 += a.cols) {
+                    double sum[8] = {};
+                    for (int c = 0; c <= many; c += 4) {  // four shares on their way at a time
+                        float v[4][8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) share(a, min(chunk + min(c + i, many), a.chunks - 1), c + i == 0, 8 * c0, v[i]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) sum[e] += c + i <= many ? static_cast<double>(v[i][e]) : 0.0;
+                    }
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(sum[e]);
+                    float_store8(a.dtable + static_cast<long>(key) * a.D, 8 * c0, a.D, v, a.scale);
                 }
             }
-            __syncthreads();
+        }
+    }
+    __syncthreads();
+    for (int t = 0; t < a.teams; ++t) {
+        if (!longs[t]) continue;
+        const int begin = first + t, key = clampi(a.keys[(static_cast<long>(begin) + 1) * a.chunk - 1], 0, a.V - 1);
+        int lo = begin + kShort, hi = a.chunks;  // its last chunk is lo or one up to hi - 1
+        while (hi - lo > 1) {  // a lane looks at each 64th of them
+            const int step = (hi - lo + kSeqWave - 1) / kSeqWave, at = lo + (tid & (kSeqWave - 1)) * step;
+            const int on = max(1, popcount64(wave_ballot(at < hi && a.keys[static_cast<long>(at) * a.chunk] == key)));
+            lo += (on - 1) * step;
+            hi = min(hi, lo + step);
+        }
+        for (int c0 = 0; c0 < a.per_row; c0 += a.cols) {
+            const bool there = team < a.teams && c0 + lane < a.per_row;
+            double sum[8] = {};
+            if (there) {
+#pragma unroll 4
+                for (int c = begin + team; c <= min(lo, a.chunks - 1); c += a.teams) {
+                    float v[8];
+                    share(a, c, c == begin, 8 * (c0 + lane), v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) lds[tid][e] = sum[e];
-            __syncthreads();
-            if (team == 0 && d < width) {
+                    for (int e = 0; e < 8; ++e) sum[e] += static_cast<double>(v[e]);
+                }
+            }
+            int half = 1;
+            while (half < a.teams) half *= 2;
+#pragma unroll
+            for (int e0 = 0; e0 < 8; e0 += 4) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lds[e][tid] = sum[e0 + e];
+                for (int h = half >> 1; h > 0; h >>= 1) {
+                    __syncthreads();
+                    if (team < h && team + h < a.teams) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) lds[e][tid] += lds[e][tid + h * a.cols];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e0 + e] = lds[e][tid];
+            }
+            if (team == 0 && there) {
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    double s = sum[e];
-                    for (int t = 1; t < teams; ++t) s += lds[tid + t * cols][e];
-                    v[e] = static_cast<float>(s);
-                }
-                float_store8(a.dtable + static_cast<long>(key) * a.D, d, a.D, v, a.scale);
+                for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(sum[e]);
+                float_store8(a.dtable + static_cast<long>(key) * a.D, 8 * (c0 + lane), a.D, v, a.scale);
             }
         }
     }
@@ -774,7 +932,7 @@ hipError_t look_up(const conv1d_embed_t* p, LookArgs& a, hipStream_t st) {
         a.per_row = 16;
         while (a.per_row > 4 && (static_cast<long>(p->N) * a.tiles * cdiv(p->D, a.per_row) < kFill || (p->V + 1L) * a.per_row > kFewElements)) a.per_row /= 2;
         a.blocks = cdiv(p->D, a.per_row);
-        lds = static_cast<size_t>(p->V + 1) * a.per_row * (BF16 ? 2 : 4);
+        lds = 2 * 8 * kThreads + static_cast<size_t>(p->V + 1) * a.per_row * (BF16 ? 2 : 4);
         kern = embed_few_kernel<BF16>;
     } else {
         const int DT = tile_channels(p->D);
@@ -831,8 +989,8 @@ bool is_few(int N, int D, int L, int V, bool turned) {
 }
 
 struct Plan {
-    int M, bits, passes, tiles, per_lane, chunk, chunks, per_row;
-    size_t keys[2], pos[2], counts, totals, owners, rows, head, tail, bytes;
+    int M, bits, passes, tiles, per_lane, chunk, per_row, cols, teams, span, spans;  // span: rows of a workgroup that adds
+    size_t keys[2], pos[2], counts, totals, rows, head, tail, bytes;
 };
 Plan plan_of(int N, int D, int L, int V, int dtype, bool turned) {
     Plan p{};
@@ -841,12 +999,15 @@ Plan plan_of(int N, int D, int L, int V, int dtype, bool turned) {
     while (bits < 31 && (1L << bits) <= V) ++bits;  // the keys 0 ... V
     p.passes = cdiv(bits, 8);
     p.bits = cdiv(bits, p.passes);
-    p.per_lane = p.M <= kFewTiles * kSort ? 1 : kKeys;
+    p.per_lane = p.M <= 64 * kSort ? 1 : kKeys;  // up to 64 tiles, or larger ones
     p.tiles = cdiv(p.M, p.per_lane * kSort);
     p.per_row = (D + 7) / 8;
     // chunks of 32 rows, of 16 where that leaves the chip idle
-    p.chunk = static_cast<long>(p.M) * p.per_row < 32L * kFill * kSeqWave ? 16 : 32;
-    p.chunks = cdiv(p.M, p.chunk);
+    p.chunk = static_cast<long>(p.M) * p.per_row < 16L * kFill * kSeqWave ? 16 : kMostChunk;
+    p.cols = p.per_row < kThreads ? p.per_row : kThreads;
+    p.teams = kThreads / p.cols < kMostTeams ? kThreads / p.cols : kMostTeams;
+    p.span = p.teams * p.chunk;
+    p.spans = cdiv(p.M, p.span);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -858,12 +1019,11 @@ Plan plan_of(int N, int D, int L, int V, int dtype, bool turned) {
         p.keys[i] = take(4 * M);
         p.pos[i] = take(4 * M);
     }
-    p.counts = take(4 * static_cast<size_t>(p.passes) * p.tiles * kBins);
+    p.counts = take(4 * static_cast<size_t>(p.tiles) * kBins);
     p.totals = take(4 * static_cast<size_t>(kBins));
-    p.owners = take(4 * (static_cast<size_t>(p.chunks) + 1));
     p.rows = take(turned ? M * width * (dtype == CONV1D_BF16 ? 2 : 4) : 0);
-    p.head = take(4 * width * p.chunks);
-    p.tail = take(4 * width * p.chunks);
+    p.head = take(4 * width * p.spans);
+    p.tail = take(4 * width * p.spans);
     p.bytes = at;
     return p;
 }
@@ -900,11 +1060,10 @@ hipError_t gradient(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy
     }
     a.counts = reinterpret_cast<int*>(ws + plan.counts);
     a.totals = reinterpret_cast<int*>(ws + plan.totals);
-    a.owners = reinterpret_cast<int*>(ws + plan.owners);
     a.rows = ws + plan.rows;
     a.dtable = dtable;
     a.zeros = static_cast<long>(p->V) * p->D;
-    a.passes = plan.passes; a.bits = plan.bits; a.tiles = plan.tiles; a.per_lane = plan.per_lane; a.per_row = plan.per_row;
+    a.bits = plan.bits; a.tiles = plan.tiles; a.per_lane = plan.per_lane; a.per_row = plan.per_row;
     a.before = plan.tiles > kFewTiles;
     a.l_tiles = cdiv(p->L, kTurn / DT);
     a.d_blocks = cdiv(p->D, DT);
@@ -915,11 +1074,13 @@ hipError_t gradient(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy
     a.turns = static_cast<int>(turns);
     void (*sort)(SortArgs) = DT == 16 ? embed_sort_kernel<BF16, 16> : embed_sort_kernel<BF16, 64>;
     long done = 0;
-    for (a.pass = -1; a.pass < plan.passes; ++a.pass) {
+    for (int launch = 0; launch < 2 * plan.passes; ++launch) {
+        a.pass = launch / 2;
+        a.count = launch % 2 == 0;
         hipError_t e = hipSuccess;
-        if (a.pass >= 0 && a.before) e = launch_kernel(embed_places_kernel, dim3(kBins / 16), dim3(kSort), 0, st, a);
+        if (!a.count && a.before) e = launch_kernel(embed_places_kernel, dim3(kBins / 16), dim3(kSort), 0, st, a);
         // the other work in equal shares, what is too much for a grid in grids of its own
-        const long upto = jobs * (a.pass + 2) / (plan.passes + 1);
+        const long upto = jobs * (launch + 1) / (2 * plan.passes);
         a.sorts = plan.tiles;
         do {
             const long some = upto - done < kMostBlocks - a.sorts ? upto - done : kMostBlocks - a.sorts;
@@ -933,28 +1094,33 @@ hipError_t gradient(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy
     const int last = (plan.passes - 1) & 1;
     SumArgs s{};
     s.rows = turned ? static_cast<const void*>(ws + plan.rows) : dy;
-    s.keys = a.keys[last]; s.pos = a.pos[last]; s.owners = a.owners;
+    s.keys = a.keys[last]; s.pos = a.pos[last];
     s.head = reinterpret_cast<float*>(ws + plan.head);
     s.tail = reinterpret_cast<float*>(ws + plan.tail);
     s.dtable = dtable;
     s.sample_stride = dy_sn;
     s.stride = turned ? 8L * plan.per_row : dy_sl;
-    s.scale = p->scale; s.D = p->D; s.L = p->L; s.V = p->V; s.M = plan.M; s.per_row = plan.per_row; s.chunk = plan.chunk; s.chunks = plan.chunks;
-    s.by_row = make_div31(plan.per_row);
+    s.scale = p->scale; s.D = p->D; s.L = p->L; s.V = p->V; s.M = plan.M; s.per_row = plan.per_row; s.chunk = plan.chunk;
     s.by_L = make_div31(p->L);
-    const long most = kMostItems / plan.per_row;
-    void (*sums)(SumArgs) = turned ? embed_sums_kernel<BF16, true> : embed_sums_kernel<BF16, false>;
-    for (long c = 0; c < plan.chunks; c += most) {
-        s.first = static_cast<int>(c);
-        s.items = static_cast<int>((plan.chunks - c < most ? plan.chunks - c : most) * plan.per_row);
-        const hipError_t e = launch_kernel(sums, dim3(static_cast<unsigned>(cdiv(s.items, kThreads))), dim3(kThreads), 0, st, s);
+    s.cols = plan.cols; s.teams = plan.teams;
+    s.blocks = cdiv(plan.per_row, s.cols);
+    s.by_blocks = make_div31(s.blocks);
+    const long units = static_cast<long>(plan.spans) * s.blocks;
+    if (units > kMostItems) return hipErrorInvalidValue;
+    void (*sums)(SumArgs) = p->D % 8 ? (turned ? embed_sums_kernel<BF16, true, false> : embed_sums_kernel<BF16, false, false>)
+                                     : (turned ? embed_sums_kernel<BF16, true, true> : embed_sums_kernel<BF16, false, true>);
+    for (long u = 0; u < units; u += kMostBlocks) {
+        s.first = static_cast<int>(u);
+        const hipError_t e = launch_kernel(sums, dim3(static_cast<unsigned>(units - u < kMostBlocks ? units - u : kMostBlocks)), dim3(kThreads), 0, st, s);
         if (e != hipSuccess) return e;
     }
-    if (plan.chunks < 2) return hipSuccess;
+    if (plan.spans < 2) return hipSuccess;
     JoinArgs j{};
-    j.keys = s.keys; j.owners = a.owners; j.head = s.head; j.tail = s.tail; j.dtable = dtable; j.scale = p->scale;
-    j.D = p->D; j.V = p->V; j.M = plan.M; j.per_row = plan.per_row; j.chunk = plan.chunk; j.chunks = plan.chunks;
-    return launch_kernel(embed_join_kernel, dim3(static_cast<unsigned>(plan.chunks - 1 < kFill ? plan.chunks - 1 : kFill)), dim3(kThreads), 0, st, j);
+    j.keys = s.keys; j.head = s.head; j.tail = s.tail; j.dtable = dtable; j.scale = p->scale;
+    j.D = p->D; j.V = p->V; j.M = plan.M; j.per_row = plan.per_row; j.chunk = plan.span; j.chunks = plan.spans;
+    j.cols = plan.per_row < kJoin ? plan.per_row : kJoin;
+    j.teams = kJoin / j.cols;
+    return launch_kernel(embed_join_kernel, dim3(static_cast<unsigned>(cdiv(plan.spans - 1, j.teams))), dim3(kJoin), 0, st, j);
 }
 
 }  // namespace
