@@ -43,6 +43,7 @@ inline void lds_add(float* p, float v) { *p += v; }
 inline int popcount64(unsigned long v) { return __builtin_popcountl(v); }
 inline int first_bit(unsigned long v) { return __builtin_ctzl(v | (1UL << 63)); }
 inline int lane_up(int v, int) { return v; }
+inline bool wave_any(bool v) { return v; }
 #else
 __device__ __forceinline__ unsigned long wave_ballot(bool v) { return __ballot(v); }
 __device__ __forceinline__ int lane_from(int v, int lane) { return __shfl(v, lane, kSeqWave); }
@@ -50,8 +51,89 @@ __device__ __forceinline__ int lds_add(int* p, int v) { return atomicAdd(p, v); 
 __device__ __forceinline__ void lds_add(float* p, float v) { atomicAdd(p, v); }
 __device__ __forceinline__ int popcount64(unsigned long v) { return __popcll(v); }
 __device__ __forceinline__ int first_bit(unsigned long v) { return __ffsll(static_cast<unsigned long long>(v)) - 1; }
+__device__ __forceinline__ bool wave_any(bool v) { return __any(v); }
 __device__ __forceinline__ int lane_up(int v, int by) { return __shfl_up(v, by, kSeqWave); }
 #endif
+
+// ---- vectors of 8 as they lie in memory ---------------------------------------------------------------------------------
+// A load that nothing is done with yet: turned into floats only when they are needed, so that the next loads go out before it has come.
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+template <bool BF16>
+struct Raw8 {
+    u32x4 v[BF16 ? 1 : 2];
+};
+// all of them there
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> raw8_inside(const void* row, int l) {
+    Raw8<BF16> r;
+    if constexpr (BF16) {
+        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + l));
+    } else {
+        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l));
+        r.v[1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l + 4));
+    }
+    return r;
+}
+// those before len, 0 behind; an element that is not there is read at a place that is (a row has one at least), without a branch
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> raw8(const void* row, int l, int len) {
+    Raw8<BF16> r;
+    const int last = max(len, 1) - 1;
+    if constexpr (BF16) {
+        const unsigned short* p = static_cast<const unsigned short*>(row);
+        unsigned u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = p[min(l + e, last)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[0][i] = (l + 2 * i < len ? u[2 * i] : 0u) | (l + 2 * i + 1 < len ? u[2 * i + 1] << 16 : 0u);
+    } else {
+        const unsigned* p = static_cast<const unsigned*>(row);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const unsigned u = p[min(l + e, last)];
+            r.v[e >> 2][e & 3] = l + e < len ? u : 0u;
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ void floats_of(const Raw8<true>& x, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(x.v[0][i] << 16);
+        v[2 * i + 1] = __uint_as_float(x.v[0][i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void floats_of(const Raw8<false>& x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x.v[e >> 2][e & 3]);
+}
+
+// A vector of a row of `all` elements from any l < all on.  WHOLE: the row is made of whole vectors.  Else it is loaded without a branch
+// from a place where all 8 are there, which may be up to 7 elements before l, and put right when it is turned into floats (what lies
+// behind the row's end is then some number of the row); rows of fewer than 8 elements are loaded one by one.
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ Raw8<BF16> raw8_row(const void* row, int l, int all) {
+    if constexpr (WHOLE) return raw8_inside<BF16>(row, l);
+    return all >= 8 ? raw8_inside<BF16>(row, min(l, all - 8)) : raw8<BF16>(row, l, all);
+}
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ void row_floats(const Raw8<BF16>& r, int l, int all, float (&v)[8]) {
+    floats_of(r, v);
+    if constexpr (!WHOLE) {
+        const int by = all >= 8 ? l - (all - 8) : 0;
+        if (wave_any(by > 0)) {
+#pragma unroll
+            for (int step = 4; step > 0; step >>= 1)
+#pragma unroll
+                for (int e = 0; e + step < 8; ++e) v[e] = by > 0 && (by & step) ? v[e + step] : v[e];
+        }
+    }
+}
+// the elements of at .. at + 7 that lie before end
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ void vector_store8(void* row, int at, int end, const float (&v)[8]) {
+    row_store8<BF16>(row, at, WHOLE ? at + 8 : end, v);
+}
 
 // The sums of a and b over a workgroup, in every thread, added in one order; lds: two doubles a wave.
 template <int THREADS>

@@ -159,7 +159,6 @@ struct FewArgs {
     Div31 by_vgroups, by_dgroups, by_sample;
 };
 
-typedef sp::u32x4 u32x4;
 typedef sp::f32x4 f32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
@@ -184,38 +183,6 @@ template <bool BF16>
 struct Parts {
     u32x4 p[BF16 ? 1 : 3];
 };
-// 8 positions of a channel as they lie in memory: all of them there, or those before len, 0 behind
-template <bool BF16>
-struct Raw8 {
-    u32x4 v[BF16 ? 1 : 2];
-};
-template <bool BF16>
-__device__ __forceinline__ Raw8<BF16> raw8_inside(const void* row, int l) {
-    Raw8<BF16> r;
-    if constexpr (BF16) {
-        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_u16x8*>(static_cast<const unsigned short*>(row) + l));
-    } else {
-        r.v[0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l));
-        r.v[1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const seq_f32x4*>(static_cast<const float*>(row) + l + 4));
-    }
-    return r;
-}
-template <bool BF16>
-__device__ __forceinline__ Raw8<BF16> raw8(const void* row, int l, int len) {
-    float v[8];
-    row_load8<BF16>(row, l, len, v);
-    Raw8<BF16> r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (BF16) {
-            r.v[0][i] = sp::pack_hi(v[2 * i], v[2 * i + 1]);
-        } else {
-            r.v[0][i] = __float_as_uint(v[i]);
-            r.v[1][i] = __float_as_uint(v[4 + i]);
-        }
-    }
-    return r;
-}
 template <bool BF16, bool FINITE>
 __device__ __forceinline__ Parts<BF16> parts_of(const Raw8<BF16>& x) {
     Parts<BF16> r;
@@ -239,18 +206,6 @@ __device__ __forceinline__ Parts<BF16> parts_of(const Raw8<BF16>& x) {
         r.p[2] = s.h;
     }
     return r;
-}
-
-__device__ __forceinline__ void floats_of(const Raw8<true>& x, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(x.v[0][i] << 16);
-        v[2 * i + 1] = __uint_as_float(x.v[0][i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void floats_of(const Raw8<false>& x, float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x.v[e >> 2][e & 3]);
 }
 
 constexpr int kWaves = kThreads / kSeqWave;

@@ -11,7 +11,7 @@
 namespace conv1d {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kJoinThreads = 512;
 enum { kNone = 0, kRelu = 1, kSilu = 2 };
 
 struct NormArgs {
@@ -28,8 +28,8 @@ struct NormArgs {
     int vecs, items;        // vectors of 8 of a row, of a group
     int pieces, piece;      // of a group, and its vectors
     int rows_pieces, rows_piece, lanes;  // backward: pieces of a row, their vectors, lanes that a piece has
-    int act, first;
-    Div31 by_vecs, by_pieces, by_G, by_C, by_rows_pieces;
+    int first, extra;       // extra: workgroups of the launch that add up channels (of one workgroup a group: whether they are wanted)
+    Div31 by_vecs, by_pieces, by_G, by_C, by_per, by_rows_pieces;
 };
 
 // a mean as two floats
@@ -64,21 +64,57 @@ __device__ __forceinline__ float back_of(float dy, float p) {
     return dy;
 }
 
-// x -> h and p for one channel: h = (x - hi) rstd - lo rstd, p = h w + b
+// One channel: with t = x - hi, h = t rstd + h0 and p = t a + b.
 struct Channel {
-    float hi, rstd, h0, w, b;
+    float hi, a, b, near;
 };
-__device__ __forceinline__ Channel channel_of(const Mean& m, const float* weight, const float* bias, int c) {
-    return Channel{m.hi, m.rstd, -m.lo * m.rstd, weight ? weight[c] : 1.f, bias ? bias[c] : 0.f};
+__device__ __forceinline__ float start_of(const Mean& m) { return -m.lo * m.rstd; }
+// near: the side of 0 that p lies on decides over the ReLU's gradient.  p is off by a few units of 2^-24 of t a, h0 w and the bias; next to
+// 0 |t a| is about |b|, and |h0 w| + |bias| is at most |b| + 2 |h0 w|: the sign of a larger p is right, smaller ones are found in 64 bits.
+__device__ __forceinline__ Channel channel_of(const Mean& m, float w, float b) {
+    const float h0w = start_of(m) * w, c = fmaf(start_of(m), w, b);
+    return Channel{m.hi, m.rstd * w, c, 1.9073486328125e-06f * (fabsf(c) + fabsf(h0w))};
 }
-__device__ __forceinline__ float h_of(float x, const Channel& k) { return fmaf(x - k.hi, k.rstd, k.h0); }
+__device__ __forceinline__ float weight_of(const NormArgs& a, int c) { return a.weight ? a.weight[c] : 1.f; }
+__device__ __forceinline__ float bias_of(const NormArgs& a, int c) { return a.bias ? a.bias[c] : 0.f; }
 
-// The side of 0 that p lies on decides over its gradient: next to 0 it is found in 64 bits.  p is off by a few units of 2^-24 of the
-// three numbers that it is added up from, so that the sign of a p of more than 2^-20 of them is right.
-__device__ __forceinline__ float relu_side(float p, float x, const Channel& k, double mean, double rstd) {
-    if (fabsf(p) <= 9.5367431640625e-07f * (fabsf(k.w) * (fabsf((x - k.hi) * k.rstd) + fabsf(k.h0)) + fabsf(k.b)))
-        p = static_cast<float>((static_cast<double>(x) - mean) * rstd * static_cast<double>(k.w) + static_cast<double>(k.b));
-    return p;
+// a number with the sign that p has in 64 bits
+__device__ __forceinline__ float side_of(const NormArgs& a, float x, long group, int c) {
+    const double p = (static_cast<double>(x) - a.stats[2 * group]) * a.stats[2 * group + 1] * static_cast<double>(weight_of(a, c)) + static_cast<double>(bias_of(a, c));
+    return p > 0.0 ? 1.f : p <= 0.0 ? -1.f : __builtin_nanf("");
+}
+
+// t = x - hi of 8 values, and dp in place of dy; channel e is k[STEP e], c + STEP e in group g[STEP e]
+template <int ACT, int STEP>
+__device__ __forceinline__ void back8(const NormArgs& a, const float (&x)[8], const Channel* k, const long* g, int c, float (&t)[8], float (&dy)[8]) {
+    float p[8];
+    bool near = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        t[e] = x[e] - k[STEP * e].hi;
+        p[e] = fmaf(t[e], k[STEP * e].a, k[STEP * e].b);
+        near |= fabsf(p[e]) <= k[STEP * e].near;
+    }
+    if (ACT == kRelu) {
+        if (wave_any(near)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = side_of(a, x[e], g[STEP * e], min(c + STEP * e, a.C - 1));
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dy[e] = back_of<ACT>(dy[e], p[e]);
+}
+
+// dx = rstd (dp w - s1 - h q1) = dp a + t q + s
+struct Back {
+    float q, s;
+};
+__device__ __forceinline__ Back back_const(const Mean& m, double s1, double q1) {
+    return Back{static_cast<float>(-q1 * m.rstd * m.rstd), static_cast<float>(-m.rstd * (s1 + q1 * start_of(m)))};
+}
+// sum of dp h, of the sums of dp t and of dp
+__device__ __forceinline__ double with_h(double dpt, double dp, double mean, double rstd) {
+    return rstd * (dpt + dp * (static_cast<double>(static_cast<float>(mean)) - mean));
 }
 
 // ---- positions contiguous -------------------------------------------------------------------------------------------------
@@ -91,36 +127,93 @@ __device__ __forceinline__ void* row_at(void* base, long n, long sn, int c, long
     return static_cast<typename RowElem<BF16>::type*>(base) + n * sn + c * sc;
 }
 
-constexpr int kAhead = 4;  // vectors that a lane has in flight
-
+// vectors that a lane has in flight
+constexpr int kAhead = 4;
 template <bool BF16>
+constexpr int kAheadBack = BF16 ? 4 : 2;  // of x and of dy
+
+// K vectors of a group, `step` apart from item i0 on (those behind the last are the last): channels, first positions and x
+template <bool BF16, int K>
+struct Batch {
+    Raw8<BF16> x[K];
+    int c[K], at[K];
+};
+template <bool BF16, int K>
+__device__ __forceinline__ void places_of(const NormArgs& a, int c0, int i0, int step, Batch<BF16, K>& r) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = min(i0 + k * step, a.items - 1), of = div31(i, a.by_vecs);
+        r.c[k] = c0 + of;
+        r.at[k] = 8 * (i - of * a.vecs);
+    }
+}
+template <bool BF16, bool WHOLE, int K>
+__device__ __forceinline__ void load_rows(const NormArgs& a, const void* base, int n, long sn, long sc, int len, const Batch<BF16, K>& at, Raw8<BF16> (&r)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (WHOLE || wave_any(at.at[k] < len)) r[k] = raw8_row<BF16, WHOLE>(row_at<BF16>(base, n, sn, at.c[k], sc), at.at[k], a.L);
+}
+
+// sums of x - shift and of its squares over one vector's values before len
+template <bool BF16, bool WHOLE>
+__device__ __forceinline__ void add_values(const NormArgs& a, const Raw8<BF16>& raw, int at, int len, double shift, double& s, double& q) {
+    float v[8];
+    row_floats<BF16, WHOLE>(raw, at, a.L, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double d = WHOLE || at + e < len ? static_cast<double>(v[e]) - shift : 0.0;
+        s += d;
+        q = fma(d, d, q);
+    }
+}
+// the group's first value; 0 for an empty sequence
+template <bool BF16>
+__device__ __forceinline__ double shift_of(const NormArgs& a, int n, int c0, int len) {
+    const float v = load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, c0, a.x_sc), 0);
+    return len > 0 ? v : 0.f;
+}
+
+// y of a vector
+template <bool BF16, int ACT, bool WHOLE>
+__device__ __forceinline__ void apply_vector(const NormArgs& a, const Raw8<BF16>& raw, const Channel& k, int n, int c, int at, int len) {
+    float v[8];
+    row_floats<BF16, WHOLE>(raw, at, a.L, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float y = act_of<ACT>(fmaf(v[e] - k.hi, k.a, k.b));
+        v[e] = WHOLE || at + e < len ? y : 0.f;
+    }
+    vector_store8<BF16, WHOLE>(row_at<BF16>(a.y, n, a.y_sn, c, a.y_sc), at, a.L, v);
+}
+
+struct Unit {
+    int n, group, c0, len, piece;
+};
+__device__ __forceinline__ Unit unit_of(const NormArgs& a, int unit) {
+    Unit r;
+    r.group = div31(unit, a.by_pieces);
+    r.piece = unit - r.group * a.pieces;
+    r.n = div31(r.group, a.by_G);
+    r.c0 = (r.group - r.n * a.G) * a.per;
+    r.len = seq_length(a.lengths, r.n, a.L);
+    return r;
+}
+
+template <bool BF16, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs a) {
     __shared__ double lds[2 * kThreads / kSeqWave];
-    const int unit = static_cast<int>(blockIdx.x) + a.first, group = div31(unit, a.by_pieces), piece = unit - group * a.pieces;
-    const int n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per, len = seq_length(a.lengths, n, a.L);
-    const int from = piece * a.piece, to = min(a.items, from + a.piece);
+    const int unit = static_cast<int>(blockIdx.x) + a.first;
+    const Unit u = unit_of(a, unit);
+    const int from = u.piece * a.piece, to = min(a.items, from + a.piece);
+    const double shift = shift_of<BF16>(a, u.n, u.c0, u.len);
     double s = 0.0, q = 0.0;
-    if (len > 0) {
-        const double shift = load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, c0, a.x_sc), 0);
-        for (int i0 = from + static_cast<int>(threadIdx.x); i0 < to; i0 += kThreads * kAhead) {
-            float v[kAhead][8];
-            int many[kAhead];
+    for (int i0 = from + static_cast<int>(threadIdx.x); i0 < to; i0 += kThreads * kAhead) {
+        Batch<BF16, kAhead> b;
+        places_of(a, u.c0, i0, kThreads, b);
+        load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int i = min(i0 + k * kThreads, a.items - 1), c = div31(i, a.by_vecs), at = 8 * (i - c * a.vecs);
-                many[k] = i0 + k * kThreads < to ? len - at : 0;
-                row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, c0 + c, a.x_sc), at, len, v[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const double d = e < many[k] ? static_cast<double>(v[k][e]) - shift : 0.0;
-                    s += d;
-                    q = fma(d, d, q);
-                }
-            }
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (i0 + k * kThreads < to) add_values<BF16, WHOLE>(a, b.x[k], b.at[k], u.len, shift, s, q);
     }
     block_sums<kThreads>(s, q, lds);
     if (threadIdx.x == 0) {
@@ -129,73 +222,102 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs a) {
     }
 }
 
-// joins the sums of a group's `many` pieces
-__device__ __forceinline__ void join_pieces(const double* part, int many, double& s, double& q, double* lds) {
-    s = q = 0.0;
-    for (int i = static_cast<int>(threadIdx.x); i < many; i += kThreads) {
+__device__ __forceinline__ void keep_stats(const NormArgs& a, int group, double mean, double rstd) {
+    if (a.stats && threadIdx.x == 0) {
+        a.stats[2L * group] = mean;
+        a.stats[2L * group + 1] = rstd;
+    }
+}
+
+// The first vectors are on their way while the group's sums are joined.
+template <bool BF16, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a) {
+    __shared__ double lds[2 * kThreads / kSeqWave];
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
+    const int from = u.piece * a.piece + static_cast<int>(threadIdx.x), to = min(a.items, (u.piece + 1) * a.piece);
+    Batch<BF16, kAhead> b;
+    places_of(a, u.c0, from, kThreads, b);
+    load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
+    const double shift = shift_of<BF16>(a, u.n, u.c0, u.len);
+    double s = 0.0, q = 0.0, mean, rstd;
+    const double* part = a.part + 2L * u.group * a.pieces;
+    for (int i = static_cast<int>(threadIdx.x); i < a.pieces; i += kThreads) {
         s += part[2L * i];
         q += part[2L * i + 1];
     }
     block_sums<kThreads>(s, q, lds);
-}
-
-template <bool BF16, int ACT>
-__global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a) {
-    __shared__ double lds[2 * kThreads / kSeqWave];
-    const int unit = static_cast<int>(blockIdx.x) + a.first, group = div31(unit, a.by_pieces), piece = unit - group * a.pieces;
-    const int n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per, len = seq_length(a.lengths, n, a.L);
-    double s, q, mean, rstd;
-    join_pieces(a.part + 2L * group * a.pieces, a.pieces, s, q, lds);
-    const double shift = len > 0 ? load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, c0, a.x_sc), 0) : 0.f;
-    stats_of(s, q, static_cast<double>(len) * a.per, shift, a.eps, mean, rstd);
-    if (a.stats && piece == 0 && threadIdx.x == 0) {
-        a.stats[2L * group] = mean;
-        a.stats[2L * group + 1] = rstd;
-    }
+    stats_of(s, q, static_cast<double>(u.len) * a.per, shift, a.eps, mean, rstd);
+    if (u.piece == 0) keep_stats(a, u.group, mean, rstd);
     const Mean m = mean_of(mean, rstd);
-    const int from = piece * a.piece, to = min(a.items, from + a.piece);
-    for (int i0 = from + static_cast<int>(threadIdx.x); i0 < to; i0 += kThreads * kAhead) {
-        float v[kAhead][8];
-        int at[kAhead], c[kAhead];
+    for (int i0 = from;;) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int i = min(i0 + k * kThreads, a.items - 1), of = div31(i, a.by_vecs);
-            at[k] = 8 * (i - of * a.vecs);
-            c[k] = c0 + of;
-            row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, c[k], a.x_sc), at[k], len, v[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (i0 + k * kThreads >= to) break;
-            const Channel ch = channel_of(m, a.weight, a.bias, c[k]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = act_of<ACT>(fmaf(h_of(v[k][e], ch), ch.w, ch.b));
-                v[k][e] = at[k] + e < len ? y : 0.f;
-            }
-            row_store8<BF16>(row_at<BF16>(a.y, n, a.y_sn, c[k], a.y_sc), at[k], a.L, v[k]);
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (i0 + k * kThreads < to)
+                apply_vector<BF16, ACT, WHOLE>(a, b.x[k], channel_of(m, weight_of(a, b.c[k]), bias_of(a, b.c[k])), u.n, b.c[k], b.at[k], u.len);
+        i0 += kThreads * kAhead;
+        if (i0 >= to) break;
+        places_of(a, u.c0, i0, kThreads, b);
+        load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     }
 }
 
-// p, h and dp of a vector
-template <int ACT>
-__device__ __forceinline__ void back8(const float (&x)[8], const float (&dy)[8], const Channel& ch, double mean, double rstd, int many, float (&h)[8],
-                                      float (&dp)[8]) {
+// A group whose values THREADS lanes hold in kAhead vectors each.
+template <bool BF16, int ACT, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_one_kernel(NormArgs a) {
+    __shared__ double lds[2 * THREADS / kSeqWave];
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
+    const int tid = static_cast<int>(threadIdx.x);
+    Batch<BF16, kAhead> b;
+    places_of(a, u.c0, tid, THREADS, b);
+    load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
+    const double shift = shift_of<BF16>(a, u.n, u.c0, u.len);
+    double s = 0.0, q = 0.0, mean, rstd;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (tid + k * THREADS < a.items) add_values<BF16, WHOLE>(a, b.x[k], b.at[k], u.len, shift, s, q);
+    block_sums<THREADS>(s, q, lds);
+    stats_of(s, q, static_cast<double>(u.len) * a.per, shift, a.eps, mean, rstd);
+    keep_stats(a, u.group, mean, rstd);
+    const Mean m = mean_of(mean, rstd);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (tid + k * THREADS < a.items)
+            apply_vector<BF16, ACT, WHOLE>(a, b.x[k], channel_of(m, weight_of(a, b.c[k]), bias_of(a, b.c[k])), u.n, b.c[k], b.at[k], u.len);
+}
+
+// sums of dp and dp t over a vector's positions before len
+template <bool BF16, int ACT, bool WHOLE>
+__device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, long group, int c, int at, int len,
+                                          float& s, float& q) {
+    float x[8], g[8], t[8];
+    row_floats<BF16, WHOLE>(xr, at, a.L, x);
+    row_floats<BF16, WHOLE>(gr, at, a.L, g);
+    back8<ACT, 0>(a, x, &k, &group, c, t, g);
+    s = q = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        h[e] = h_of(x[e], ch);
-        float p = fmaf(h[e], ch.w, ch.b);
-        if (ACT == kRelu) p = relu_side(p, x[e], ch, mean, rstd);
-        dp[e] = back_of<ACT>(dy[e], p);
-        if (e >= many) h[e] = dp[e] = 0.f;
+        s += WHOLE || at + e < len ? g[e] : 0.f;
+        q = WHOLE || at + e < len ? fmaf(g[e], t[e], q) : q;
     }
+}
+// dx of a vector
+template <bool BF16, int ACT, bool WHOLE>
+__device__ __forceinline__ void back_vector(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, const Back& back, int n, long group, int c,
+                                            int at, int len) {
+    float x[8], g[8], t[8];
+    row_floats<BF16, WHOLE>(xr, at, a.L, x);
+    row_floats<BF16, WHOLE>(gr, at, a.L, g);
+    back8<ACT, 0>(a, x, &k, &group, c, t, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = WHOLE || at + e < len ? fmaf(g[e], k.a, fmaf(t[e], back.q, back.s)) : 0.f;
+    vector_store8<BF16, WHOLE>(row_at<BF16>(a.dx, n, a.dx_sn, c, a.dx_sc), at, a.L, x);
 }
 
 // Sums of dp and dp h over each piece of a row, a.lanes lanes a piece (a power of two).
-template <bool BF16, int ACT>
+template <bool BF16, int ACT, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
     __shared__ double lds[2 * kThreads / kSeqWave];
+    constexpr int K = kAheadBack<BF16>;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (a.lanes - 1), teams = kThreads / a.lanes;
     const long unit = (static_cast<long>(blockIdx.x) + a.first) * teams + tid / a.lanes;
     const long units = static_cast<long>(a.N) * a.C * a.rows_pieces;
@@ -204,29 +326,27 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
     const int row = div31(u, a.by_rows_pieces), piece = u - row * a.rows_pieces, n = div31(row, a.by_C), c = row - n * a.C;
     const int len = seq_length(a.lengths, n, a.L);
     const long group = static_cast<long>(n) * a.G + c / a.per;
-    const double mean = a.stats[2 * group], rstd = a.stats[2 * group + 1];
-    const Channel ch = channel_of(mean_of(mean, rstd), a.weight, a.bias, c);
+    const int from = piece * a.rows_piece + lane, to = there ? min((len + 7) >> 3, (piece + 1) * a.rows_piece) : 0;
     const void *x = row_at<BF16>(a.x, n, a.x_sn, c, a.x_sc), *dy = row_at<BF16>(a.dy, n, a.dy_sn, c, a.dy_sc);
-    const int from = piece * a.rows_piece, to = there ? min((len + 7) >> 3, from + a.rows_piece) : 0;
+    const double mean = a.stats[2 * group], rstd = a.stats[2 * group + 1];
+    const float w = weight_of(a, c), bias = bias_of(a, c);
     double s = 0.0, q = 0.0;
-    for (int i0 = from + lane; i0 < to; i0 += a.lanes * 2) {
-        float v[2][8], g[2][8];
+    for (int i0 = from; i0 < to; i0 += a.lanes * K) {
+        Raw8<BF16> v[K], g[K];
+        int at[K];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = 8 * min(i0 + k * a.lanes, to - 1);
-            row_load8<BF16>(x, at, len, v[k]);
-            row_load8<BF16>(dy, at, len, g[k]);
+        for (int k = 0; k < K; ++k) {
+            at[k] = 8 * min(i0 + k * a.lanes, to - 1);
+            v[k] = raw8_row<BF16, WHOLE>(x, at[k], a.L);
+            g[k] = raw8_row<BF16, WHOLE>(dy, at[k], a.L);
         }
+        const Mean m = mean_of(mean, rstd);
+        const Channel ch = channel_of(m, w, bias);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float h[8], dp[8], s8 = 0.f, q8 = 0.f;
-            const int i = i0 + k * a.lanes;
-            back8<ACT>(v[k], g[k], ch, mean, rstd, i < to ? len - 8 * i : 0, h, dp);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s8 += dp[e];
-                q8 = fmaf(dp[e], h[e], q8);
-            }
+        for (int k = 0; k < K; ++k) {
+            if (i0 + k * a.lanes >= to) break;
+            float s8, q8;
+            back_sums<BF16, ACT, WHOLE>(a, v[k], g[k], ch, group, c, at[k], len, s8, q8);
             s += static_cast<double>(s8);
             q += static_cast<double>(q8);
         }
@@ -241,20 +361,22 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
     }
     if (there && lane == 0) {
         a.part[2 * unit] = s;
-        a.part[2 * unit + 1] = q;
+        a.part[2 * unit + 1] = len > 0 ? with_h(q, s, mean, rstd) : 0.0;
     }
 }
 
-// dweight and dbias of a channel: its rows' pieces over all samples, one wave a channel
-__device__ __forceinline__ void channel_sums(const NormArgs& a, int c, int lane, long n_step, int each) {
+// dweight and dbias of a channel: its rows' pieces over all samples, one wave a channel.  part: [N][C][each].
+__device__ __forceinline__ void channel_sums(const NormArgs& a, int c, const double* part, int each) {
+    const int lane = static_cast<int>(threadIdx.x) & (kSeqWave - 1), many = a.N * each;
     double s = 0.0, q = 0.0;
-    const int many = a.N * each;
+#pragma unroll 2
     for (int i = lane; i < many; i += kSeqWave) {
-        const int n = i / each;
-        const long at = n * n_step + static_cast<long>(c) * each + (i - n * each);
-        s += a.part[2 * at];
-        q += a.part[2 * at + 1];
+        const int n = each == 1 ? i : div31(i, a.by_rows_pieces);
+        const long at = (static_cast<long>(n) * a.C + c) * each + (i - n * each);
+        s += part[2 * at];
+        q += part[2 * at + 1];
     }
+#pragma unroll
     for (int m = 1; m < kSeqWave; m <<= 1) {
         s += lane_xor(s, m);
         q += lane_xor(q, m);
@@ -264,272 +386,284 @@ __device__ __forceinline__ void channel_sums(const NormArgs& a, int c, int lane,
         if (a.dweight) a.dweight[c] = static_cast<float>(q);
     }
 }
-__global__ __launch_bounds__(kThreads) void norm_channels_kernel(NormArgs a) {
+// the first `a.extra` workgroups of a launch
+__device__ __forceinline__ bool took_channels(const NormArgs& a, const double* part, int each) {
+    if (static_cast<int>(blockIdx.x) >= a.extra) return false;
     const int c = (static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x)) / kSeqWave;
-    if (c < a.C) channel_sums(a, c, threadIdx.x & (kSeqWave - 1), static_cast<long>(a.C) * a.rows_pieces, a.rows_pieces);
+    if (blockIdx.y == 0 && c < a.C) channel_sums(a, c, part, each);
+    return true;
 }
+__global__ __launch_bounds__(kThreads) void norm_channels_kernel(NormArgs a) { took_channels(a, a.part, 1); }
 
-// sums of dp weight and dp weight h over a group, of its channels' sums
-__device__ __forceinline__ void join_channels(const NormArgs& a, const double* part, int c0, int each, double& s, double& q, double* lds) {
-    s = q = 0.0;
-    for (int i = static_cast<int>(threadIdx.x); i < a.per * each; i += kThreads) {
-        const double w = a.weight ? a.weight[c0 + i / each] : 1.0;
+template <bool BF16, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_back_kernel(NormArgs a) {
+    __shared__ double lds[2 * kThreads / kSeqWave];
+    constexpr int K = kAheadBack<BF16>;
+    if (took_channels(a, a.part, a.rows_pieces)) return;
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) - a.extra + a.first);
+    const int from = u.piece * a.piece + static_cast<int>(threadIdx.x), to = min(a.items, (u.piece + 1) * a.piece);
+    Batch<BF16, K> b;
+    Raw8<BF16> g[K];
+    places_of(a, u.c0, from, kThreads, b);
+    load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
+    load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
+    const double mean = a.stats[2L * u.group], rstd = a.stats[2L * u.group + 1];
+    double s = 0.0, q = 0.0;
+    const double* part = a.part + 2 * (static_cast<long>(u.n) * a.C + u.c0) * a.rows_pieces;
+    for (int i = static_cast<int>(threadIdx.x); i < a.per * a.rows_pieces; i += kThreads) {
+        const double w = weight_of(a, u.c0 + div31(i, a.by_rows_pieces));
         s = fma(w, part[2L * i], s);
         q = fma(w, part[2L * i + 1], q);
     }
     block_sums<kThreads>(s, q, lds);
+    const double over = u.len > 0 ? 1.0 / (static_cast<double>(u.len) * a.per) : 0.0;
+    const Mean m = mean_of(mean, rstd);
+    const Back back = back_const(m, s * over, q * over);
+    for (int i0 = from;;) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (i0 + k * kThreads < to) {
+                const float w = weight_of(a, b.c[k]);
+                back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, u.group, b.c[k], b.at[k], u.len);
+            }
+        i0 += kThreads * K;
+        if (i0 >= to) break;
+        places_of(a, u.c0, i0, kThreads, b);
+        load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
+        load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
+    }
 }
 
-template <bool BF16, int ACT>
-__global__ __launch_bounds__(kThreads) void norm_back_kernel(NormArgs a) {
-    __shared__ double lds[2 * kThreads / kSeqWave];
-    const int unit = static_cast<int>(blockIdx.x) + a.first, group = div31(unit, a.by_pieces), piece = unit - group * a.pieces;
-    const int n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per, len = seq_length(a.lengths, n, a.L);
-    double s, q;
-    join_channels(a, a.part + 2 * (static_cast<long>(n) * a.C + c0) * a.rows_pieces, c0, a.rows_pieces, s, q, lds);
-    const double mean = a.stats[2L * group], rstd = a.stats[2L * group + 1], over = len > 0 ? 1.0 / (static_cast<double>(len) * a.per) : 0.0;
+// Backward of a group that THREADS lanes hold; its channels' sums go to part[n][c], for norm_channels_kernel.
+template <bool BF16, int ACT, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
+    constexpr int K = kAheadBack<BF16>;
+    __shared__ double lds[2 * THREADS / kSeqWave];
+    __shared__ float vector[K * THREADS][2];
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
+    const int tid = static_cast<int>(threadIdx.x);
+    Batch<BF16, K> b;
+    Raw8<BF16> g[K];
+    places_of(a, u.c0, tid, THREADS, b);
+    load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
+    load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
+    const double mean = a.stats[2L * u.group], rstd = a.stats[2L * u.group + 1];
     const Mean m = mean_of(mean, rstd);
-    const float s1 = static_cast<float>(s * over), q1 = static_cast<float>(q * over);
-    const int from = piece * a.piece, to = min(a.items, from + a.piece);
-    for (int i0 = from + static_cast<int>(threadIdx.x); i0 < to; i0 += kThreads * 2) {
-        float v[2][8], g[2][8];
-        int at[2], c[2];
+    double s = 0.0, q = 0.0;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = min(i0 + k * kThreads, a.items - 1), of = div31(i, a.by_vecs);
-            at[k] = 8 * (i - of * a.vecs);
-            c[k] = c0 + of;
-            row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, c[k], a.x_sc), at[k], len, v[k]);
-            row_load8<BF16>(row_at<BF16>(a.dy, n, a.dy_sn, c[k], a.dy_sc), at[k], len, g[k]);
+    for (int k = 0; k < K; ++k) {
+        const int i = tid + k * THREADS;
+        if (i >= a.items) break;
+        const float w = weight_of(a, b.c[k]);
+        float s8, q8;
+        back_sums<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), u.group, b.c[k], b.at[k], u.len, s8, q8);
+        vector[i][0] = s8;
+        vector[i][1] = q8;
+        s = fma(static_cast<double>(w), static_cast<double>(s8), s);
+        q = fma(static_cast<double>(w), static_cast<double>(q8), q);
+    }
+    block_sums<THREADS>(s, q, lds);  // (with barriers, behind which every vector's sums are there)
+    if (a.extra) {
+        // lanes of a channel: as many as there are for all of them, up to a wave
+        int lanes = 1;
+        while (lanes < kSeqWave && 2 * lanes * a.per <= THREADS) lanes *= 2;
+        for (int c0 = 0; c0 < a.per; c0 += THREADS / lanes) {
+            const int c = c0 + tid / lanes, lane = tid & (lanes - 1);
+            double cs = 0.0, cq = 0.0;
+            if (c < a.per)
+                for (int i = lane; i < a.vecs; i += lanes) {
+                    cs += static_cast<double>(vector[c * a.vecs + i][0]);
+                    cq += static_cast<double>(vector[c * a.vecs + i][1]);
+                }
+            for (int l = 1; l < lanes; l <<= 1) {
+                cs += lane_xor(cs, l);
+                cq += lane_xor(cq, l);
+            }
+            if (c < a.per && lane == 0) {
+                double* part = a.part + 2 * (static_cast<long>(u.n) * a.C + u.c0 + c);
+                part[0] = cs;
+                part[1] = u.len > 0 ? with_h(cq, cs, mean, rstd) : 0.0;
+            }
         }
+    }
+    const double over = u.len > 0 ? 1.0 / (static_cast<double>(u.len) * a.per) : 0.0;
+    const Back back = back_const(m, s * over, with_h(q, s, mean, rstd) * over);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (i0 + k * kThreads >= to) break;
-            const Channel ch = channel_of(m, a.weight, a.bias, c[k]);
-            float h[8], dp[8];
-            back8<ACT>(v[k], g[k], ch, mean, rstd, len - at[k], h, dp);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[k][e] = at[k] + e < len ? m.rstd * (fmaf(dp[e], ch.w, -s1) - h[e] * q1) : 0.f;
-            row_store8<BF16>(row_at<BF16>(a.dx, n, a.dx_sn, c[k], a.dx_sc), at[k], a.L, v[k]);
-        }
+    for (int k = 0; k < K; ++k) {
+        if (tid + k * THREADS >= a.items) break;
+        const float w = weight_of(a, b.c[k]);
+        back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, u.group, b.c[k], b.at[k], u.len);
     }
 }
 
 // ---- channels contiguous --------------------------------------------------------------------------------------------------
 // A workgroup has some positions of a sample and up to kWide channels; a lane has 8 neighbouring channels at every tall-th of the
-// positions.  Sums go to LDS and from there, a channel after the other, to part[n][piece][c].
+// positions.  Sums go through LDS to part[n][piece][c].
 constexpr int kWide = 8 * kThreads;
 
 struct Lane {
-    int c, l0, tall;   // first channel (C or more: none), first position and step
+    int c, l0, tall, vecs;   // first channel (C or more: none), first position and step, lanes of a position
 };
 __device__ __forceinline__ Lane lane_of(const NormArgs& a, int block) {
-    const int vecs = min(kThreads, (a.C - block * kWide + 7) >> 3), tid = static_cast<int>(threadIdx.x), tall = kThreads / vecs, l = tid / vecs;
-    return Lane{l < tall ? block * kWide + 8 * (tid - l * vecs) : a.C, l, tall};
-}
-
-// Adds up s and q of the lanes that have the same channels; the sums of channel c go to part[2 c], part[2 c + 1].
-__device__ __forceinline__ void channels_out(const NormArgs& a, const Lane& k, int block, const double (&s)[8], const double (&q)[8], double* part,
-                                             double (*lds)[2]) {
-    const int vecs = min(kThreads, (a.C - block * kWide + 7) >> 3), tid = static_cast<int>(threadIdx.x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        __syncthreads();
-        lds[tid][0] = s[e];
-        lds[tid][1] = q[e];
-        __syncthreads();
-        if (tid < vecs && k.c + e < a.C) {
-            double u = s[e], v = q[e];
-            for (int t = 1; t < k.tall; ++t) {
-                u += lds[tid + t * vecs][0];
-                v += lds[tid + t * vecs][1];
-            }
-            part[2L * (k.c + e)] = u;
-            part[2L * (k.c + e) + 1] = v;
-        }
-    }
-}
-
-// the channels' groups, from c on
-struct Groups {
-    int g[8];
-};
-__device__ __forceinline__ Groups groups_of(const NormArgs& a, int c) {
-    Groups r;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.g[e] = min(c + e, a.C - 1) / a.per;
+    Lane r;
+    r.vecs = min(kThreads, (a.C - block * kWide + 7) >> 3);
+    r.tall = kThreads / r.vecs;
+    r.l0 = static_cast<int>(threadIdx.x) / r.vecs;
+    r.c = r.l0 < r.tall ? block * kWide + 8 * (static_cast<int>(threadIdx.x) - r.l0 * r.vecs) : a.C;
     return r;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void norm_last_sums_kernel(NormArgs a) {
-    __shared__ double lds[kThreads][2];
-    const int unit = static_cast<int>(blockIdx.x) + a.first, n = div31(unit, a.by_pieces), piece = unit - n * a.pieces, block = static_cast<int>(blockIdx.y);
-    const int len = seq_length(a.lengths, n, a.L), from = piece * a.piece, to = min(len, from + a.piece);
-    const Lane k = lane_of(a, block);
-    double s[8] = {}, q[8] = {};
-    if (k.c < a.C && len > 0) {
-        const Groups of = groups_of(a, k.c);
-        float shift[8];
+struct LastUnit {
+    int unit, n, len, from, piece;
+};
+__device__ __forceinline__ LastUnit last_unit(const NormArgs& a, int unit) {
+    LastUnit r;
+    r.unit = unit;
+    r.n = div31(unit, a.by_pieces);
+    r.piece = unit - r.n * a.pieces;
+    r.len = seq_length(a.lengths, r.n, a.L);
+    r.from = r.piece * a.piece;
+    return r;
+}
+
+// Adds up s and q of the lanes that have the same channels; the sums of channel c go to part[2 c], part[2 c + 1].
+struct LastLds {
+    double v[kThreads][8 + 1];
+};
+__device__ __forceinline__ void channels_out(const NormArgs& a, const Lane& k, const double (&s)[8], const double (&q)[8], double* part, LastLds& lds) {
+    const int tid = static_cast<int>(threadIdx.x), first = k.c - 8 * (tid - k.l0 * k.vecs);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) shift[e] = load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, 0, 0), of.g[e] * a.per);
-        for (int l0 = from + k.l0; l0 < to; l0 += k.tall * kAhead) {
-            float v[kAhead][8];
+    for (int h = 0; h < 2; ++h) {
+        __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, min(l0 + j * k.tall, to - 1), a.x_sl), k.c, a.C, v[j]);
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                if (l0 + j * k.tall >= to) break;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const double d = static_cast<double>(v[j][e]) - static_cast<double>(shift[e]);
-                    s[e] += d;
-                    q[e] = fma(d, d, q[e]);
-                }
-            }
+        for (int e = 0; e < 8; ++e) lds.v[tid][e] = h ? q[e] : s[e];
+        __syncthreads();
+        // a channel of the workgroup's a lane
+        for (int i = tid; i < 8 * k.vecs; i += kThreads) {
+            double u = 0.0;
+            for (int t = 0; t < k.tall; ++t) u += lds.v[(i >> 3) + t * k.vecs][i & 7];
+            const int c = first + i;
+            if (c < a.C) part[2L * c + h] = u;
         }
     }
-    channels_out(a, k, block, s, q, a.part + 2L * unit * a.C, lds);
 }
 
-// One workgroup a sample and group.  Forward: mean and rstd.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void norm_last_stats_kernel(NormArgs a) {
-    __shared__ double lds[2 * kThreads / kSeqWave];
-    const int group = static_cast<int>(blockIdx.x) + a.first, n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per;
-    const int len = seq_length(a.lengths, n, a.L);
-    double s = 0.0, q = 0.0, mean, rstd;
-    const double* part = a.part + 2L * (static_cast<long>(n) * a.pieces * a.C + c0);
-    for (int i = static_cast<int>(threadIdx.x); i < a.per * a.pieces; i += kThreads) {
-        const int piece = i / a.per;
-        const long at = static_cast<long>(piece) * a.C + (i - piece * a.per);
-        s += part[2 * at];
-        q += part[2 * at + 1];
-    }
-    block_sums<kThreads>(s, q, lds);
-    const double shift = len > 0 ? load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, 0, 0), c0) : 0.f;
-    stats_of(s, q, static_cast<double>(len) * a.per, shift, a.eps, mean, rstd);
-    if (threadIdx.x == 0) {
-        a.stats[2L * group] = mean;
-        a.stats[2L * group + 1] = rstd;
-    }
-}
-
-// mean, rstd and parameters of a lane's channels
-struct Channels {
-    Channel of[8];
-    double mean[8], rstd[8];
+// the groups of a lane's channels
+struct Groups {
+    long g[8];   // among all samples'
 };
-__device__ __forceinline__ void channels_of(const NormArgs& a, int n, int c, Channels& r) {
-    const Groups g = groups_of(a, c);
+__device__ __forceinline__ Groups groups_of(const NormArgs& a, int n, int c) {
+    Groups r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const long group = static_cast<long>(n) * a.G + g.g[e];
-        r.mean[e] = a.stats[2 * group];
-        r.rstd[e] = a.stats[2 * group + 1];
-        r.of[e] = channel_of(mean_of(r.mean[e], r.rstd[e]), a.weight, a.bias, min(c + e, a.C - 1));
-    }
+    for (int e = 0; e < 8; ++e) r.g[e] = static_cast<long>(n) * a.G + div31(min(c + e, a.C - 1), a.by_per);
+    return r;
 }
 
-template <bool BF16, int ACT>
-__global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
-    const int unit = static_cast<int>(blockIdx.x) + a.first, n = div31(unit, a.by_pieces), piece = unit - n * a.pieces, block = static_cast<int>(blockIdx.y);
-    const int len = seq_length(a.lengths, n, a.L), from = piece * a.piece, to = min(a.L, from + a.piece);
-    const Lane k = lane_of(a, block);
-    if (k.c >= a.C) return;
-    Channels ch;
-    channels_of(a, n, k.c, ch);
-    for (int l0 = from + k.l0; l0 < to; l0 += k.tall * kAhead) {
-        float v[kAhead][8];
+// K positions' vectors of the lane's channels, from l0 on (those behind the last are the last)
+template <bool BF16, bool WHOLE, int K>
+__device__ __forceinline__ void load_last(const NormArgs& a, const void* base, int n, long sn, long sl, const Lane& k, int l0, int to, Raw8<BF16> (&r)[K]) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, min(l0 + j * k.tall, to - 1), a.x_sl), k.c, a.C, v[j]);
+    for (int j = 0; j < K; ++j) r[j] = raw8_row<BF16, WHOLE>(row_at<BF16>(base, n, sn, min(l0 + j * k.tall, to - 1), sl), k.c, a.C);
+}
+
+template <bool BF16, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_last_sums_kernel(NormArgs a) {
+    __shared__ LastLds lds;
+    const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
+    const int to = min(u.len, u.from + a.piece);
+    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    double s[8] = {}, q[8] = {};
+    if (k.c < a.C && u.from + k.l0 < to) {
+        double shift[8];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int l = l0 + j * k.tall;
-            if (l >= to) break;
+        for (int e = 0; e < 8; ++e) shift[e] = load_elem<BF16>(row_at<BF16>(a.x, u.n, a.x_sn, 0, 0), div31(min(k.c + e, a.C - 1), a.by_per) * a.per);
+        const auto add = [&](const Raw8<BF16>& raw) {
+            float v[8];
+            row_floats<BF16, WHOLE>(raw, k.c, a.C, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float y = act_of<ACT>(fmaf(h_of(v[j][e], ch.of[e]), ch.of[e].w, ch.of[e].b));
-                v[j][e] = l < len ? y : 0.f;
+                const double d = static_cast<double>(v[e]) - shift[e];
+                s[e] += d;
+                q[e] = fma(d, d, q[e]);
             }
-            row_store8<BF16>(row_at<BF16>(a.y, n, a.y_sn, l, a.y_sl), k.c, a.C, v[j]);
+        };
+        int l0 = u.from + k.l0;
+        for (int end = u.from + k.tall * kAhead; end <= to; end += k.tall * kAhead, l0 += k.tall * kAhead) {  // all lanes have all of them
+            Raw8<BF16> raw[kAhead];
+            load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, raw);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) add(raw[j]);
+        }
+#pragma unroll 1
+        for (; l0 < to; l0 += k.tall) {
+            Raw8<BF16> raw[1];
+            load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, raw);
+            add(raw[0]);
         }
     }
+    channels_out(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
 }
 
-template <int ACT>
-__device__ __forceinline__ void back_last(const float (&x)[8], const float (&dy)[8], const Channels& ch, float (&h)[8], float (&dp)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[e] = h_of(x[e], ch.of[e]);
-        float p = fmaf(h[e], ch.of[e].w, ch.of[e].b);
-        if (ACT == kRelu) p = relu_side(p, x[e], ch.of[e], ch.mean[e], ch.rstd[e]);
-        dp[e] = back_of<ACT>(dy[e], p);
-    }
-}
-
-template <bool BF16, int ACT>
-__global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs a) {
-    __shared__ double lds[kThreads][2];
-    const int unit = static_cast<int>(blockIdx.x) + a.first, n = div31(unit, a.by_pieces), piece = unit - n * a.pieces, block = static_cast<int>(blockIdx.y);
-    const int len = seq_length(a.lengths, n, a.L), from = piece * a.piece, to = min(len, from + a.piece);
-    const Lane k = lane_of(a, block);
-    double s[8] = {}, q[8] = {};
-    if (k.c < a.C) {
-        Channels ch;
-        channels_of(a, n, k.c, ch);
-        for (int l0 = from + k.l0; l0 < to; l0 += k.tall * 2) {
-            float v[2][8], g[2][8];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int l = min(l0 + j * k.tall, to - 1);
-                row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, l, a.x_sl), k.c, a.C, v[j]);
-                row_load8<BF16>(row_at<BF16>(a.dy, n, a.dy_sn, l, a.dy_sl), k.c, a.C, g[j]);
+// Sums of the pieces of a sample's channels, for one workgroup a sample and group: of its channels together, and (backward) of each.
+// A lane has one channel at a time and every share-th piece.
+__device__ __forceinline__ void join_pieces(const NormArgs& a, int n, int c0, double* channels, double& s, double& q, double (*lds)[2]) {
+    const int tid = static_cast<int>(threadIdx.x), wide = min(a.per, kJoinThreads), shares = kJoinThreads / wide, share = tid / wide;
+    s = q = 0.0;
+    for (int c1 = 0; c1 < a.per; c1 += wide) {
+        const int c = c1 + tid - share * wide;
+        double cs = 0.0, cq = 0.0;
+        if (share < shares && c < a.per) {
+            const double* part = a.part + 2L * (static_cast<long>(n) * a.pieces * a.C + c0 + c);
+#pragma unroll 4
+            for (int p = share; p < a.pieces; p += shares) {
+                cs += part[2L * p * a.C];
+                cq += part[2L * p * a.C + 1];
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (l0 + j * k.tall >= to) break;
-                float h[8], dp[8];
-                back_last<ACT>(v[j], g[j], ch, h, dp);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    s[e] += static_cast<double>(dp[e]);
-                    q[e] = fma(static_cast<double>(dp[e]), static_cast<double>(h[e]), q[e]);
+        }
+        if (channels) {
+            __syncthreads();
+            lds[tid][0] = cs;
+            lds[tid][1] = cq;
+            __syncthreads();
+            if (share == 0 && c < a.per) {
+                for (int i = 1; i < shares; ++i) {
+                    cs += lds[tid + i * wide][0];
+                    cq += lds[tid + i * wide][1];
                 }
+                channels[2L * (static_cast<long>(n) * a.C + c0 + c)] = cs;
+                channels[2L * (static_cast<long>(n) * a.C + c0 + c) + 1] = cq;
+                const double w = weight_of(a, c0 + c);
+                s = fma(w, cs, s);
+                q = fma(w, cq, q);
             }
+        } else {
+            s += cs;
+            q += cq;
         }
     }
-    channels_out(a, k, block, s, q, a.part + 2L * unit * a.C, lds);
 }
 
-// Backward: sums[n][c] of the pieces' sums, behind them; one wave a sample and channel.
-__global__ __launch_bounds__(kThreads) void norm_last_join_kernel(NormArgs a, double* sums) {
-    const long i = (static_cast<long>(blockIdx.x) * kThreads + threadIdx.x) / kSeqWave;
-    if (i >= static_cast<long>(a.N) * a.C) return;
-    const int n = div31(static_cast<int>(i), a.by_C), c = static_cast<int>(i) - n * a.C, lane = threadIdx.x & (kSeqWave - 1);
-    double s = 0.0, q = 0.0;
-    for (int p = lane; p < a.pieces; p += kSeqWave) {
-        const long at = (static_cast<long>(n) * a.pieces + p) * a.C + c;
-        s += a.part[2 * at];
-        q += a.part[2 * at + 1];
-    }
-    for (int m = 1; m < kSeqWave; m <<= 1) {
-        s += lane_xor(s, m);
-        q += lane_xor(q, m);
-    }
-    if (lane == 0) {
-        sums[2 * i] = s;
-        sums[2 * i + 1] = q;
-    }
+template <bool BF16>
+__global__ __launch_bounds__(kJoinThreads) void norm_last_stats_kernel(NormArgs a) {
+    __shared__ double lds[2 * kJoinThreads / kSeqWave];
+    const int group = static_cast<int>(blockIdx.x) + a.first, n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per;
+    const int len = seq_length(a.lengths, n, a.L);
+    const float first = load_elem<BF16>(row_at<BF16>(a.x, n, a.x_sn, 0, 0), c0);
+    double s, q, mean, rstd;
+    join_pieces(a, n, c0, nullptr, s, q, nullptr);
+    block_sums<kJoinThreads>(s, q, lds);
+    stats_of(s, q, static_cast<double>(len) * a.per, len > 0 ? first : 0.f, a.eps, mean, rstd);
+    keep_stats(a, group, mean, rstd);
 }
 
-// One workgroup a sample and group: the group's sums over m, in place of its channels' (they are read by norm_channels_kernel before).
-__global__ __launch_bounds__(kThreads) void norm_last_groups_kernel(NormArgs a, const double* sums, double* groups) {
-    __shared__ double lds[2 * kThreads / kSeqWave];
+// Backward: the channels' sums to sums[n][c], the group's over m to groups[n][g].
+__global__ __launch_bounds__(kJoinThreads) void norm_last_join_kernel(NormArgs a, double* sums, double* groups) {
+    __shared__ double lds[2 * kJoinThreads / kSeqWave], all[kJoinThreads][2];
     const int group = static_cast<int>(blockIdx.x) + a.first, n = div31(group, a.by_G), c0 = (group - n * a.G) * a.per;
     const int len = seq_length(a.lengths, n, a.L);
     double s, q;
-    join_channels(a, sums + 2L * (static_cast<long>(n) * a.C + c0), c0, 1, s, q, lds);
+    join_pieces(a, n, c0, sums, s, q, all);
+    block_sums<kJoinThreads>(s, q, lds);
     const double over = len > 0 ? 1.0 / (static_cast<double>(len) * a.per) : 0.0;
     if (threadIdx.x == 0) {
         groups[2L * group] = s * over;
@@ -537,56 +671,167 @@ __global__ __launch_bounds__(kThreads) void norm_last_groups_kernel(NormArgs a, 
     }
 }
 
-template <bool BF16, int ACT>
-__global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, const double* groups) {
-    const int unit = static_cast<int>(blockIdx.x) + a.first, n = div31(unit, a.by_pieces), piece = unit - n * a.pieces, block = static_cast<int>(blockIdx.y);
-    const int len = seq_length(a.lengths, n, a.L), from = piece * a.piece, to = min(a.L, from + a.piece);
-    const Lane k = lane_of(a, block);
-    if (k.c >= a.C) return;
-    Channels ch;
-    channels_of(a, n, k.c, ch);
-    const Groups of = groups_of(a, k.c);
-    float s1[8], q1[8];
+// statistics and parameters of a lane's channels
+__device__ __forceinline__ void channels_of(const NormArgs& a, int c, const Groups& g, Channel (&r)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const long group = static_cast<long>(n) * a.G + of.g[e];
-        s1[e] = static_cast<float>(groups[2 * group]);
-        q1[e] = static_cast<float>(groups[2 * group + 1]);
+        const int at = min(c + e, a.C - 1);
+        r[e] = channel_of(mean_of(a.stats[2 * g.g[e]], a.stats[2 * g.g[e] + 1]), weight_of(a, at), bias_of(a, at));
     }
-    for (int l0 = from + k.l0; l0 < to; l0 += k.tall * 2) {
-        float v[2][8], g[2][8];
+}
+
+template <bool BF16, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
+    const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
+    const int to = min(a.L, u.from + a.piece);
+    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    if (k.c >= a.C || u.from + k.l0 >= to) return;
+    Raw8<BF16> raw[kAhead];
+    load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, u.from + k.l0, to, raw);
+    Channel ch[8];
+    channels_of(a, k.c, groups_of(a, u.n, k.c), ch);
+    const auto put = [&](const Raw8<BF16>& r, int l) {
+        float v[8];
+        row_floats<BF16, WHOLE>(r, k.c, a.C, v);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int l = min(l0 + j * k.tall, to - 1);
-            row_load8<BF16>(row_at<BF16>(a.x, n, a.x_sn, l, a.x_sl), k.c, a.C, v[j]);
-            row_load8<BF16>(row_at<BF16>(a.dy, n, a.dy_sn, l, a.dy_sl), k.c, a.C, g[j]);
+        for (int e = 0; e < 8; ++e) {
+            const float y = act_of<ACT>(fmaf(v[e] - ch[e].hi, ch[e].a, ch[e].b));
+            v[e] = l < u.len ? y : 0.f;
+        }
+        vector_store8<BF16, WHOLE>(row_at<BF16>(a.y, u.n, a.y_sn, l, a.y_sl), k.c, a.C, v);
+    };
+    const int step = k.tall * kAhead;
+    for (int l0 = u.from + k.l0, end = u.from + step;; end += step) {
+        if (end <= to) {  // all lanes have all of them
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) put(raw[j], l0 + j * k.tall);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                if (l0 + j * k.tall < to) put(raw[j], l0 + j * k.tall);
+        }
+        l0 += step;
+        if (l0 >= to) break;
+        load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, raw);
+    }
+}
+
+template <bool BF16, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs a) {
+    __shared__ LastLds lds;
+    constexpr int K = kAheadBack<BF16>;
+    const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
+    const int to = min(u.len, u.from + a.piece);
+    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    double s[8] = {}, q[8] = {};
+    if (k.c < a.C && u.from + k.l0 < to) {
+        const Groups of = groups_of(a, u.n, k.c);
+        Channel ch[8];
+        channels_of(a, k.c, of, ch);
+        const auto add = [&](const Raw8<BF16>& xr, const Raw8<BF16>& gr, float (&s8)[8], float (&q8)[8]) {
+            float x[8], g[8], t[8];
+            row_floats<BF16, WHOLE>(xr, k.c, a.C, x);
+            row_floats<BF16, WHOLE>(gr, k.c, a.C, g);
+            back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s8[e] += g[e];
+                q8[e] = fmaf(g[e], t[e], q8[e]);
+            }
+        };
+        const auto flush = [&](const float (&s8)[8], const float (&q8)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                s[e] += static_cast<double>(s8[e]);
+                q[e] += static_cast<double>(q8[e]);
+            }
+        };
+        int l0 = u.from + k.l0;
+        for (int end = u.from + k.tall * K; end <= to; end += k.tall * K, l0 += k.tall * K) {  // all lanes have all of them
+            Raw8<BF16> xr[K], gr[K];
+            load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, xr);
+            load_last<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, k, l0, to, gr);
+            float s8[8] = {}, q8[8] = {};
+#pragma unroll
+            for (int j = 0; j < K; ++j) add(xr[j], gr[j], s8, q8);
+            flush(s8, q8);
+        }
+#pragma unroll 1
+        for (; l0 < to; l0 += k.tall) {
+            Raw8<BF16> xr[1], gr[1];
+            load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, xr);
+            load_last<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, k, l0, to, gr);
+            float s8[8] = {}, q8[8] = {};
+            add(xr[0], gr[0], s8, q8);
+            flush(s8, q8);
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int l = l0 + j * k.tall;
-            if (l >= to) break;
-            float h[8], dp[8];
-            back_last<ACT>(v[j], g[j], ch, h, dp);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[j][e] = l < len ? ch.of[e].rstd * (fmaf(dp[e], ch.of[e].w, -s1[e]) - h[e] * q1[e]) : 0.f;
-            row_store8<BF16>(row_at<BF16>(a.dx, n, a.dx_sn, l, a.dx_sl), k.c, a.C, v[j]);
+        for (int e = 0; e < 8; ++e) {
+            q[e] = with_h(q[e], s[e], a.stats[2 * of.g[e]], a.stats[2 * of.g[e] + 1]);
         }
+    }
+    channels_out(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
+}
+
+template <bool BF16, int ACT, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, const double* sums, const double* groups) {
+    constexpr int K = 2;
+    if (took_channels(a, sums, 1)) return;
+    const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) - a.extra + a.first);
+    const int to = min(a.L, u.from + a.piece);
+    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    if (k.c >= a.C || u.from + k.l0 >= to) return;
+    Raw8<BF16> xr[K], gr[K];
+    load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, u.from + k.l0, to, xr);
+    load_last<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, k, u.from + k.l0, to, gr);
+    const Groups of = groups_of(a, u.n, k.c);
+    Channel ch[8];
+    channels_of(a, k.c, of, ch);
+    Back back[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        back[e] = back_const(mean_of(a.stats[2 * of.g[e]], a.stats[2 * of.g[e] + 1]), groups[2 * of.g[e]], groups[2 * of.g[e] + 1]);
+    }
+    const auto put = [&](const Raw8<BF16>& xr1, const Raw8<BF16>& gr1, int l) {
+        float x[8], g[8], t[8];
+        row_floats<BF16, WHOLE>(xr1, k.c, a.C, x);
+        row_floats<BF16, WHOLE>(gr1, k.c, a.C, g);
+        back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(g[e], ch[e].a, fmaf(t[e], back[e].q, back[e].s)) : 0.f;
+        vector_store8<BF16, WHOLE>(row_at<BF16>(a.dx, u.n, a.dx_sn, l, a.dx_sl), k.c, a.C, x);
+    };
+    const int step = k.tall * K;
+    for (int l0 = u.from + k.l0, end = u.from + step;; end += step) {
+        if (end <= to) {  // all lanes have all of them
+#pragma unroll
+            for (int j = 0; j < K; ++j) put(xr[j], gr[j], l0 + j * k.tall);
+        } else {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (l0 + j * k.tall < to) put(xr[j], gr[j], l0 + j * k.tall);
+        }
+        l0 += step;
+        if (l0 >= to) break;
+        load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, l0, to, xr);
+        load_last<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, k, l0, to, gr);
     }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 constexpr long kFill = 2048;   // workgroups that keep the chip busy: 8 a compute unit
-constexpr int kMostPieces = 512;
+constexpr int kMostPieces = 512, kOne = 1024, kOneBack = 512;
 
 int ceil_to(long n, int to) { return static_cast<int>((n + to - 1) / to * to); }
 
 struct Plan {
     bool last;
+    int one;   // threads of a workgroup that has a whole group, or 0
     int vecs, items, pieces, piece, rows_pieces, rows_piece, lanes, blocks;
     size_t part, sums, groups, bytes;
 };
 // `last`: channels contiguous
-Plan plan_of(int N, int C, int L, int G, bool last, bool back) {
+Plan plan_of(int N, int C, int L, int G, int dtype, bool last, bool back) {
     Plan p{};
     p.last = last;
     const long groups = static_cast<long>(N) * G;
@@ -610,9 +855,21 @@ Plan plan_of(int N, int C, int L, int G, bool last, bool back) {
     } else {
         p.vecs = (L + 7) / 8;
         p.items = static_cast<int>(static_cast<long>(C / G) * p.vecs);
+        // what a workgroup's lanes hold: up to four vectors each, two of x and two of dy for floats backward
+        const int most = back && dtype == CONV1D_FP32 ? 2 : kAhead, wide = back ? kOneBack : kOne;
+        p.one = p.items <= most * kThreads ? kThreads : p.items <= most * wide ? wide : 0;
+        if (p.one) {
+            p.pieces = 1;
+            p.part = take(back ? static_cast<size_t>(N) * C : 0);
+            p.bytes = at;
+            return p;
+        }
         long pieces = kFill / groups;
         pieces = pieces < 1 ? 1 : pieces > kMostPieces ? kMostPieces : pieces;
+        // (in whole steps of a workgroup's loads where that leaves enough workgroups)
+        const int step = kThreads * (back && dtype == CONV1D_FP32 ? 2 : kAhead);
         p.piece = ceil_to((p.items + pieces - 1) / pieces, kThreads);
+        if (2 * p.piece > step) p.piece = ceil_to(p.piece, step);
         p.pieces = cdiv(p.items, p.piece);
         if (back) {
             const long rows = static_cast<long>(N) * C;
@@ -664,82 +921,98 @@ NormArgs args_of(const conv1d_norm_t* p, const Plan& plan, void* workspace) {
     a.by_pieces = make_div31(plan.pieces);
     a.by_G = make_div31(p->G);
     a.by_C = make_div31(p->C);
+    a.by_per = make_div31(a.per);
     a.by_rows_pieces = make_div31(plan.rows_pieces ? plan.rows_pieces : 1);
     return a;
 }
 
-// all units of a launch, in pieces that a grid may have
+// All units of a launch, in pieces that a grid may have; with `extra` workgroups before them in the first.
 template <typename... More>
-hipError_t launch_units(void (*kern)(NormArgs, More...), NormArgs& a, long units, int blocks, hipStream_t st, More... more) {
-    const long most = kSeqMostThreads / kThreads / blocks;
-    for (long u = 0; u < units; u += most) {
+hipError_t launch_units(void (*kern)(NormArgs, More...), NormArgs& a, int threads, long units, int blocks, int extra, hipStream_t st, More... more) {
+    const long most = kSeqMostThreads / threads / blocks - extra;
+    a.extra = extra;
+    for (long u = 0; u < units; u += most, a.extra = 0) {
         a.first = static_cast<int>(u);
-        const hipError_t e = launch_kernel(kern, dim3(static_cast<unsigned>(units - u < most ? units - u : most), static_cast<unsigned>(blocks)), dim3(kThreads), 0, st,
-                                           a, more...);
+        const long some = units - u < most ? units - u : most;
+        const hipError_t e = launch_kernel(kern, dim3(static_cast<unsigned>(some + a.extra), static_cast<unsigned>(blocks)), dim3(threads), 0, st, a, more...);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-template <bool BF16, int ACT>
+template <bool BF16, int ACT, bool WHOLE>
 hipError_t forward(NormArgs& a, const Plan& plan, hipStream_t st) {
     const long groups = static_cast<long>(a.N) * a.G;
+    if (plan.one == kThreads) return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kThreads>, a, kThreads, groups, 1, 0, st);
+    if (plan.one) return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kOne>, a, kOne, groups, 1, 0, st);
     if (!plan.last) {
-        const hipError_t e = launch_units(norm_sums_kernel<BF16>, a, groups * plan.pieces, 1, st);
-        return e == hipSuccess ? launch_units(norm_apply_kernel<BF16, ACT>, a, groups * plan.pieces, 1, st) : e;
+        const hipError_t e = launch_units(norm_sums_kernel<BF16, WHOLE>, a, kThreads, groups * plan.pieces, 1, 0, st);
+        return e == hipSuccess ? launch_units(norm_apply_kernel<BF16, ACT, WHOLE>, a, kThreads, groups * plan.pieces, 1, 0, st) : e;
     }
     const long units = static_cast<long>(a.N) * plan.pieces;
-    hipError_t e = launch_units(norm_last_sums_kernel<BF16>, a, units, plan.blocks, st);
-    if (e == hipSuccess) e = launch_units(norm_last_stats_kernel<BF16>, a, groups, 1, st);
-    if (e == hipSuccess) e = launch_units(norm_last_apply_kernel<BF16, ACT>, a, units, plan.blocks, st);
+    hipError_t e = launch_units(norm_last_sums_kernel<BF16, WHOLE>, a, kThreads, units, plan.blocks, 0, st);
+    if (e == hipSuccess) e = launch_units(norm_last_stats_kernel<BF16>, a, kJoinThreads, groups, 1, 0, st);
+    if (e == hipSuccess) e = launch_units(norm_last_apply_kernel<BF16, ACT, WHOLE>, a, kThreads, units, plan.blocks, 0, st);
     return e;
 }
 
-template <bool BF16, int ACT>
+template <bool BF16, int ACT, bool WHOLE>
 hipError_t backward(NormArgs& a, const Plan& plan, double* sums, double* groups, hipStream_t st) {
-    const long many = static_cast<long>(a.N) * a.G, waves = kThreads / kSeqWave;
-    const bool channels = a.dweight || a.dbias;
-    const dim3 wave_a_channel(static_cast<unsigned>(cdiv(a.C, waves)));
-    if (!plan.last) {
-        const long teams = kThreads / plan.lanes, rows = static_cast<long>(a.N) * a.C * plan.rows_pieces;
-        hipError_t e = launch_units(norm_back_sums_kernel<BF16, ACT>, a, cdiv(rows, teams), 1, st);
-        if (e == hipSuccess) e = launch_units(norm_back_kernel<BF16, ACT>, a, many * plan.pieces, 1, st);
-        if (e == hipSuccess && channels) e = launch_kernel(norm_channels_kernel, wave_a_channel, dim3(kThreads), 0, st, a);
+    const long many = static_cast<long>(a.N) * a.G;
+    const int channels = a.dweight || a.dbias ? cdiv(a.C, kThreads / kSeqWave) : 0;
+    if (plan.one) {
+        // (extra: the kernel's own, whether sums of channels are wanted)
+        hipError_t e = hipSuccess;
+        const long most = kSeqMostThreads / plan.one;
+        a.extra = channels;
+        for (long u = 0; u < many && e == hipSuccess; u += most) {
+            a.first = static_cast<int>(u);
+            e = launch_kernel(plan.one == kThreads ? norm_back_one_kernel<BF16, ACT, WHOLE, kThreads> : norm_back_one_kernel<BF16, ACT, WHOLE, kOneBack>,
+                              dim3(static_cast<unsigned>(many - u < most ? many - u : most)), dim3(plan.one), 0, st, a);
+        }
+        if (e == hipSuccess && channels) e = launch_kernel(norm_channels_kernel, dim3(channels), dim3(kThreads), 0, st, a);
         return e;
     }
-    const long units = static_cast<long>(a.N) * plan.pieces;
-    hipError_t e = launch_units(norm_last_back_sums_kernel<BF16, ACT>, a, units, plan.blocks, st);
-    if (e == hipSuccess)
-        e = launch_kernel(norm_last_join_kernel, dim3(static_cast<unsigned>(cdiv(static_cast<long>(a.N) * a.C, waves))), dim3(kThreads), 0, st, a, sums);
-    if (e == hipSuccess) e = launch_units(norm_last_groups_kernel, a, many, 1, st, static_cast<const double*>(sums), groups);
-    if (e == hipSuccess) e = launch_units(norm_last_back_kernel<BF16, ACT>, a, units, plan.blocks, st, static_cast<const double*>(groups));
-    if (e == hipSuccess && channels) {
-        NormArgs c = a;
-        c.part = sums;
-        c.rows_pieces = 1;
-        e = launch_kernel(norm_channels_kernel, wave_a_channel, dim3(kThreads), 0, st, c);
+    if (!plan.last) {
+        const long teams = kThreads / plan.lanes, rows = static_cast<long>(a.N) * a.C * plan.rows_pieces;
+        const hipError_t e = launch_units(norm_back_sums_kernel<BF16, ACT, WHOLE>, a, kThreads, cdiv(rows, teams), 1, 0, st);
+        return e == hipSuccess ? launch_units(norm_back_kernel<BF16, ACT, WHOLE>, a, kThreads, many * plan.pieces, 1, channels, st) : e;
     }
+    const long units = static_cast<long>(a.N) * plan.pieces;
+    hipError_t e = launch_units(norm_last_back_sums_kernel<BF16, ACT, WHOLE>, a, kThreads, units, plan.blocks, 0, st);
+    if (e == hipSuccess) e = launch_units(norm_last_join_kernel, a, kJoinThreads, many, 1, 0, st, sums, groups);
+    if (e == hipSuccess)
+        e = launch_units(norm_last_back_kernel<BF16, ACT, WHOLE>, a, kThreads, units, plan.blocks, channels, st, static_cast<const double*>(sums),
+                         static_cast<const double*>(groups));
     return e;
 }
 
-template <bool BF16>
+template <bool BF16, bool WHOLE>
 hipError_t forward(NormArgs& a, const Plan& plan, int act, hipStream_t st) {
-    return act == kRelu ? forward<BF16, kRelu>(a, plan, st) : act == kSilu ? forward<BF16, kSilu>(a, plan, st) : forward<BF16, kNone>(a, plan, st);
+    return act == kRelu   ? forward<BF16, kRelu, WHOLE>(a, plan, st)
+           : act == kSilu ? forward<BF16, kSilu, WHOLE>(a, plan, st)
+                          : forward<BF16, kNone, WHOLE>(a, plan, st);
 }
-template <bool BF16>
+template <bool BF16, bool WHOLE>
 hipError_t backward(NormArgs& a, const Plan& plan, int act, double* sums, double* groups, hipStream_t st) {
-    return act == kRelu   ? backward<BF16, kRelu>(a, plan, sums, groups, st)
-           : act == kSilu ? backward<BF16, kSilu>(a, plan, sums, groups, st)
-                          : backward<BF16, kNone>(a, plan, sums, groups, st);
+    return act == kRelu   ? backward<BF16, kRelu, WHOLE>(a, plan, sums, groups, st)
+           : act == kSilu ? backward<BF16, kSilu, WHOLE>(a, plan, sums, groups, st)
+                          : backward<BF16, kNone, WHOLE>(a, plan, sums, groups, st);
 }
 
 int act_flag(int flags) { return flags & CONV1D_NORM_RELU ? kRelu : flags & CONV1D_NORM_SILU ? kSilu : kNone; }
+// rows of whole vectors, all of which count (channels contiguous: positions that do not are passed over anyway)
+bool is_whole(const conv1d_norm_t* p, bool last) { return last ? p->C % 8 == 0 : p->L % 8 == 0 && !p->lengths; }
 int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; }
 
 size_t workspace_of(int N, int C, int L, int G, bool back) {
     if (N < 1 || C < 1 || L < 1 || G < 1 || C % G || !sizes_ok(N, C, L, G)) return 0;
-    const size_t rows = plan_of(N, C, L, G, false, back).bytes, last = plan_of(N, C, L, G, true, back).bytes;
-    return rows > last ? rows : last;
+    size_t most = 0;
+    for (int i = 0; i < 4; ++i) {
+        const size_t n = plan_of(N, C, L, G, i & 1 ? CONV1D_BF16 : CONV1D_FP32, i & 2, back).bytes;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 }  // namespace
@@ -758,14 +1031,16 @@ int conv1d_norm_fwd(const conv1d_norm_t* p, void* y, long y_sn, long y_sc, long 
     const int order = order_of(p);
     if (!seq_aligned(y, size) || !seq_aligned(stats, 8) || !seq_aligned(workspace, 256) || !order || !fits(p, order, y_sc, y_sl)) return CONV1D_EINVAL;
     if (!sizes_ok(p->N, p->C, p->L, p->G)) return CONV1D_EUNSUPPORTED;
-    const Plan plan = plan_of(p->N, p->C, p->L, p->G, order == 2, false);
-    if (!workspace || workspace_bytes < plan.bytes) return CONV1D_EWORKSPACE;
+    const Plan plan = plan_of(p->N, p->C, p->L, p->G, p->dtype, order == 2, false);
+    if (workspace_bytes < plan.bytes || (plan.bytes && !workspace)) return CONV1D_EWORKSPACE;
     NormArgs a = args_of(p, plan, workspace);
     a.y = y; a.y_sn = y_sn; a.y_sc = y_sc; a.y_sl = y_sl;
     a.stats = stats ? stats : plan.last ? reinterpret_cast<double*>(static_cast<char*>(workspace) + plan.groups) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int act = act_flag(p->flags);
-    return status_of(p->dtype == CONV1D_BF16 ? forward<true>(a, plan, act, st) : forward<false>(a, plan, act, st));
+    const bool whole = is_whole(p, plan.last);
+    if (p->dtype == CONV1D_BF16) return status_of(whole ? forward<true, true>(a, plan, act, st) : forward<true, false>(a, plan, act, st));
+    return status_of(whole ? forward<false, true>(a, plan, act, st) : forward<false, false>(a, plan, act, st));
 }
 
 int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_sc, long dy_sl, const double* stats, void* dx, long dx_sn, long dx_sc, long dx_sl,
@@ -777,8 +1052,8 @@ int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_
         !seq_aligned(workspace, 256) || !order || !fits(p, order, dy_sc, dy_sl) || !fits(p, order, dx_sc, dx_sl))
         return CONV1D_EINVAL;
     if (!sizes_ok(p->N, p->C, p->L, p->G)) return CONV1D_EUNSUPPORTED;
-    const Plan plan = plan_of(p->N, p->C, p->L, p->G, order == 2, true);
-    if (!workspace || workspace_bytes < plan.bytes) return CONV1D_EWORKSPACE;
+    const Plan plan = plan_of(p->N, p->C, p->L, p->G, p->dtype, order == 2, true);
+    if (workspace_bytes < plan.bytes || (plan.bytes && !workspace)) return CONV1D_EWORKSPACE;
     NormArgs a = args_of(p, plan, workspace);
     a.dy = dy; a.dy_sn = dy_sn; a.dy_sc = dy_sc; a.dy_sl = dy_sl;
     a.dx = dx; a.dx_sn = dx_sn; a.dx_sc = dx_sc; a.dx_sl = dx_sl;
@@ -788,7 +1063,9 @@ int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int act = act_flag(p->flags);
     double *sums = reinterpret_cast<double*>(ws + plan.sums), *groups = reinterpret_cast<double*>(ws + plan.groups);
-    return status_of(p->dtype == CONV1D_BF16 ? backward<true>(a, plan, act, sums, groups, st) : backward<false>(a, plan, act, sums, groups, st));
+    const bool whole = is_whole(p, plan.last);
+    if (p->dtype == CONV1D_BF16) return status_of(whole ? backward<true, true>(a, plan, act, sums, groups, st) : backward<true, false>(a, plan, act, sums, groups, st));
+    return status_of(whole ? backward<false, true>(a, plan, act, sums, groups, st) : backward<false, false>(a, plan, act, sums, groups, st));
 }
 
 }  // extern "C"
