@@ -348,18 +348,20 @@ __global__ __launch_bounds__(kThreads) void embed_few_sums_kernel(FewArgs a) {
     }
 }
 
-// 16 neighbouring numbers a workgroup, each the sum of 64 lanes' shares of the chunks
+// 16 neighbouring numbers a workgroup, each the sum of THREADS / 16 lanes' shares of the chunks
 constexpr int kFewJoin = 1024;
-__global__ __launch_bounds__(kFewJoin) void embed_few_join_kernel(FewArgs a) {
-    __shared__ double lds[kFewJoin / 16][17];
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void embed_few_join_kernel(FewArgs a) {
+    __shared__ double lds[THREADS / 16][17];
     const int tid = static_cast<int>(threadIdx.x), o = tid & 15, slice = tid >> 4;
     const long at = 16L * blockIdx.x + o;  // of part
     double s = 0.0;
 #pragma unroll 4
-    for (int c = slice; c < a.chunks; c += kFewJoin / 16) s += a.part[static_cast<long>(c) * a.Vp * a.Dp + at];
+    for (int c = slice; c < a.chunks; c += THREADS / 16) s += a.part[static_cast<long>(c) * a.Vp * a.Dp + at];
     lds[slice][o] = s;
     __syncthreads();
-    for (int half = kFewJoin / 32; half > 0; half >>= 1) {
+#pragma unroll
+    for (int half = THREADS / 32; half > 0; half >>= 1) {
         if (slice < half) lds[slice][o] += lds[slice + half][o];
         __syncthreads();
     }
@@ -912,7 +914,7 @@ struct FewPlan {
     int VB, DB, Vp, Dp, vgroups, dgroups, chunk, samples, per_sample, chunks;
     size_t bytes;
 };
-FewPlan few_plan(int N, int D, int L, int V) {
+FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     FewPlan p{};
     p.Vp = static_cast<int>(round_up(V, 16));
     p.Dp = static_cast<int>(round_up(D, 16));
@@ -920,8 +922,10 @@ FewPlan few_plan(int N, int D, int L, int V) {
     p.DB = p.Dp <= 16 ? 1 : 4;
     p.vgroups = cdiv(p.Vp, 16 * p.VB);
     p.dgroups = cdiv(p.Dp, 16 * p.DB);
-    // enough workgroups to fill the chip, but no more partial sums than dy has numbers
-    const long want = kFill / (static_cast<long>(p.vgroups) * p.dgroups), M = static_cast<long>(N) * L, step = 32 * kWaves;
+    // enough workgroups to fill the chip once (three of the largest tiles fit a compute unit), but no more partial sums than dy has
+    // numbers; in whole blocks
+    const long M = static_cast<long>(N) * L, step = 32 * kWaves * (dtype == CONV1D_BF16 ? kU<true> : kU<false>);
+    const long want = (p.VB * p.DB == 16 ? 3 * kFill / 8 : kFill) / (static_cast<long>(p.vgroups) * p.dgroups);
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
     if (chunk >= 2L * L) {
@@ -937,9 +941,9 @@ FewPlan few_plan(int N, int D, int L, int V) {
     return p;
 }
 // Whether the gradient is taken as a product
-bool is_few(int N, int D, int L, int V, bool turned) {
+bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
-    const FewPlan p = few_plan(N, D, L, V);
+    const FewPlan p = few_plan(N, D, L, V, dtype);
     return static_cast<long>(p.chunks) * p.vgroups * p.dgroups <= kMostBlocks && static_cast<long>(p.Vp) * p.Dp / 16 <= kMostBlocks;
 }
 
@@ -998,7 +1002,11 @@ hipError_t few_gradient(const conv1d_embed_t* p, const void* dy, long dy_sn, lon
     const unsigned units = static_cast<unsigned>(static_cast<long>(plan.chunks) * plan.vgroups * plan.dgroups);
     const hipError_t e = launch_kernel(kern, dim3(units), dim3(kThreads), 0, st, a);
     if (e != hipSuccess) return e;
-    return launch_kernel(embed_few_join_kernel, dim3(static_cast<unsigned>(static_cast<long>(plan.Vp) * plan.Dp / 16)), dim3(kFewJoin), 0, st, a);
+    // few numbers: large workgroups
+    const long joins = static_cast<long>(plan.Vp) * plan.Dp / 16;
+    const bool large = joins < kFill / 8;
+    return launch_kernel(large ? embed_few_join_kernel<kFewJoin> : embed_few_join_kernel<kThreads>, dim3(static_cast<unsigned>(joins)), dim3(large ? kFewJoin : kThreads), 0,
+                         st, a);
 }
 
 template <bool BF16>
@@ -1100,7 +1108,7 @@ int conv1d_embed_fwd(const conv1d_embed_t* p, const void* table, void* y, long y
 
 size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype) {
     if (N < 1 || D < 1 || L < 1 || V < 1 || !sizes_ok(N, D, L, V) || (dtype != CONV1D_FP32 && dtype != CONV1D_BF16)) return 0;
-    const size_t few = is_few(N, D, L, V, true) ? few_plan(N, D, L, V).bytes : plan_of(N, D, L, V, dtype, true).bytes, rest = plan_of(N, D, L, V, dtype, false).bytes;
+    const size_t few = is_few(N, D, L, V, dtype, true) ? few_plan(N, D, L, V, dtype).bytes : plan_of(N, D, L, V, dtype, true).bytes, rest = plan_of(N, D, L, V, dtype, false).bytes;
     return few > rest ? few : rest;  // for dy in either order
 }
 
@@ -1114,8 +1122,8 @@ int conv1d_embed_bwd(const conv1d_embed_t* p, const void* dy, long dy_sn, long d
     char* ws = static_cast<char*>(workspace);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf16 = p->dtype == CONV1D_BF16;
-    if (is_few(p->N, p->D, p->L, p->V, turned)) {
-        const FewPlan plan = few_plan(p->N, p->D, p->L, p->V);
+    if (is_few(p->N, p->D, p->L, p->V, p->dtype, turned)) {
+        const FewPlan plan = few_plan(p->N, p->D, p->L, p->V, p->dtype);
         if (!workspace || workspace_bytes < plan.bytes) return CONV1D_EWORKSPACE;
         float* part = reinterpret_cast<float*>(ws);
         return status_of(bf16 ? few_gradient<true>(p, dy, dy_sn, dy_sd, dtable, plan, part, st) : few_gradient<false>(p, dy, dy_sn, dy_sd, dtable, plan, part, st));
