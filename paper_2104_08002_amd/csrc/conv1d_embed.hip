@@ -223,68 +223,97 @@ __device__ __forceinline__ Chunk chunk_of(const FewArgs& a, int chunk) {
     r.to = min(a.L, r.from + a.chunk);
     return r;
 }
-template <bool BF16>
-constexpr int kU = BF16 ? 4 : 2;   // steps whose loads a wave has in flight
+// steps whose loads a wave has in flight, beside as many that it multiplies
+template <bool BF16, int DB>
+constexpr int kU = BF16 && DB == 1 ? 4 : 2;
 constexpr int kMostBlock = 32 * kWaves * 4;
+
+// A block of the chunk: positions l0 ... of sample n, of which len count.
+struct Block {
+    int n, l0, len;
+};
+// the chunk's first block that holds any position, from the given one on; n behind the last sample: none
+__device__ __forceinline__ Block settle(const FewArgs& a, const Chunk& t, Block b) {
+    while (b.n < t.n0 + t.samples) {
+        b.len = min(t.to, seq_length(a.lengths, b.n, a.L));
+        if (b.l0 < b.len) break;
+        ++b.n;
+        b.l0 = t.from;
+    }
+    return b;
+}
+
+template <bool BF16, int U, int DB>
+struct FewLoads {
+    Raw8<BF16> raw[U][DB];
+    int toks[U * 32 * kWaves / kThreads ? U * 32 * kWaves / kThreads : 1];
+};
+template <bool BF16, int U, int DB>
+__device__ __forceinline__ void load_block(const FewArgs& a, const Block& b, int d0, FewLoads<BF16, U, DB>& r) {
+    using T = typename RowElem<BF16>::type;
+    constexpr int BLOCK = 32 * kWaves * U;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), l = b.l0 + 32 * U * (tid / kSeqWave) + 8 * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < BLOCK / kThreads; ++i) r.toks[i] = token_at(a.tokens, a.wide, b.n, a.tok_sn, b.l0 + i * kThreads + tid, b.len, a.V);
+    const T* base = static_cast<const T*>(a.dy) + b.n * a.dy_sn;
+    const bool inside = b.l0 + BLOCK <= b.len;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        const T* row = base + min(d0 + 16 * d + (lane & 15), a.D - 1) * a.dy_sd;
+        if (inside) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) r.raw[u][d] = raw8_inside<BF16>(row, l + 32 * u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) r.raw[u][d] = raw8<BF16>(row, l + 32 * u, b.len);
+        }
+    }
+}
 
 template <bool BF16, bool FINITE, int VB, int DB>
 __device__ __forceinline__ void few_sums(const FewArgs& a, const Chunk& t, int v0, int d0, f32x4 (&acc)[VB][DB], unsigned short (*toks)[kMostBlock]) {
-    using T = typename RowElem<BF16>::type;
-    constexpr int U = kU<BF16>, BLOCK = 32 * kWaves * U;
-    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), wave = tid / kSeqWave;
+    constexpr int U = kU<BF16, DB>, BLOCK = 32 * kWaves * U;
+    const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), mine = 32 * U * (tid / kSeqWave);
 #pragma unroll
     for (int v = 0; v < VB; ++v)
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[v][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    int turn = 0;
-    for (int n = t.n0; n < t.n0 + t.samples; ++n) {
-        const int len = min(t.to, seq_length(a.lengths, n, a.L));
-        const T* rows[DB];
+    Block b = settle(a, t, Block{t.n0, t.from, 0});
+    if (b.n >= t.n0 + t.samples) return;
+    FewLoads<BF16, U, DB> now, next;
+    load_block(a, b, d0, now);
+    for (int turn = 0;; turn ^= 1) {
 #pragma unroll
-        for (int d = 0; d < DB; ++d) rows[d] = static_cast<const T*>(a.dy) + n * a.dy_sn + min(d0 + 16 * d + (lane & 15), a.D - 1) * a.dy_sd;
-        for (int l0 = t.from; l0 < len; l0 += BLOCK, turn ^= 1) {
-            const int mine = 32 * U * wave, l = l0 + mine + 8 * (lane >> 4);
-            Raw8<BF16> raw[U][DB];
-            if (l0 + BLOCK <= len) {
+        for (int i = 0; i < BLOCK / kThreads; ++i) toks[turn][i * kThreads + tid] = static_cast<unsigned short>(now.toks[i]);
+        __syncthreads();  // (the next block writes the other half, the one after that waits behind the next)
+        const Block after = settle(a, t, Block{b.n, b.l0 + BLOCK, 0});
+        const bool more = after.n < t.n0 + t.samples;
+        if (more) load_block(a, after, d0, next);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (b.l0 + mine + 32 * u >= b.len) break;
+            const Tokens8 k = *reinterpret_cast<const Tokens8*>(&toks[turn][mine + 32 * u + 8 * (lane >> 4)]);
+            Parts<BF16> x[DB];
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) raw[u][d] = raw8_inside<BF16>(rows[d], l + 32 * u);
-            } else {
+            for (int d = 0; d < DB; ++d) x[d] = parts_of<BF16, FINITE>(now.raw[u][d]);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+            for (int v = 0; v < VB; ++v) {
+                const u32x4 one = truth8(k, v0 + 16 * v + (lane & 15));
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) raw[u][d] = raw8<BF16>(rows[d], l + 32 * u, len);
-            }
-#pragma unroll
-            for (int p = tid; p < BLOCK; p += kThreads) {
-                const int tok = token_at(a.tokens, a.wide, n, a.tok_sn, l0 + p, len, a.V);
-                toks[turn][p] = static_cast<unsigned short>(tok);
-            }
-            __syncthreads();  // (the next block writes the other half, the one after that waits behind the next)
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (l0 + mine + 32 * u >= len) break;
-                const Tokens8 k = *reinterpret_cast<const Tokens8*>(&toks[turn][mine + 32 * u + 8 * (lane >> 4)]);
-                Parts<BF16> x[DB];
-#pragma unroll
-                for (int d = 0; d < DB; ++d) x[d] = parts_of<BF16, FINITE>(raw[u][d]);
-#pragma unroll
-                for (int v = 0; v < VB; ++v) {
-                    const u32x4 one = truth8(k, v0 + 16 * v + (lane & 15));
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        f32x4 s = sp::mfma(x[d].p[0], one, f32x4{0.f, 0.f, 0.f, 0.f});
-                        if constexpr (!BF16) {
-                            s = sp::mfma(x[d].p[1], one, s);
-                            s = sp::mfma(x[d].p[2], one, s);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[v][d][e] += s[e];
+                for (int d = 0; d < DB; ++d) {
+                    f32x4 s = sp::mfma(x[d].p[0], one, f32x4{0.f, 0.f, 0.f, 0.f});
+                    if constexpr (!BF16) {
+                        s = sp::mfma(x[d].p[1], one, s);
+                        s = sp::mfma(x[d].p[2], one, s);
                     }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[v][d][e] += s[e];
                 }
             }
         }
+        if (!more) break;
+        now = next;
+        b = after;
     }
 }
 
@@ -924,7 +953,7 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.dgroups = cdiv(p.Dp, 16 * p.DB);
     // enough workgroups to fill the chip once (three of the largest tiles fit a compute unit), but no more partial sums than dy has
     // numbers; in whole blocks
-    const long M = static_cast<long>(N) * L, step = 32 * kWaves * (dtype == CONV1D_BF16 ? kU<true> : kU<false>);
+    const long M = static_cast<long>(N) * L, step = 32L * kWaves * (dtype == CONV1D_BF16 && p.DB == 1 ? kU<true, 1> : kU<false, 1>);
     const long want = (p.VB * p.DB == 16 ? 3 * kFill / 8 : kFill) / (static_cast<long>(p.vgroups) * p.dgroups);
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
@@ -940,10 +969,15 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.bytes = sizeof(float) * static_cast<size_t>(p.chunks) * p.Vp * p.Dp;
     return p;
 }
-// Whether the gradient is taken as a product
+// Whether the gradient is taken as a product: its time grows with tokens x channels x positions (in tiles of 16: 1e-8 us each, 1.7e-8 for
+// floats, and 12 us), that of the sort with the positions (40 us and 6.5e-5 us each).  Product and sort, us: 8 x 512 x 8192 bfloat16 16 tokens
+// 21 and 53, 64 tokens 35 and 51, 128 tokens 54 and 51; 8 x 128 x 20000 128 tokens 41 and 47, 512 tokens 100 and 58; 12 x 49 x 4999
+// float 256 tokens 29 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 77 and 103, 1024 tokens 126 and 105.
 bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
     const FewPlan p = few_plan(N, D, L, V, dtype);
+    const double M = static_cast<double>(N) * L, work = M * p.Vp * p.Dp * (dtype == CONV1D_BF16 ? 1.0 : 1.7);
+    if (work > 3e9 + 6500.0 * M) return false;
     return static_cast<long>(p.chunks) * p.vgroups * p.dgroups <= kMostBlocks && static_cast<long>(p.Vp) * p.Dp / 16 <= kMostBlocks;
 }
 
