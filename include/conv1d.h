@@ -377,7 +377,7 @@ int conv1d_embed_fwd(const conv1d_embed_t* p, const void* table, void* y, long y
 
 /* dtable: [V][D] float, all of it: scale * the sum of dy over the positions of each token (0 for a token that is not there), in an
  * order that depends on the tokens, the sizes and dy's strides alone.  dy: dtype, strides as for y. */
-size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype);
+size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype, long dy_sd, long dy_sl);
 int conv1d_embed_bwd(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy_sd, long dy_sl, float* dtable, void* workspace,
                      size_t workspace_bytes, void* stream);
 
@@ -398,14 +398,14 @@ typedef struct {
     int N, C, L, G, dtype, flags;
 } conv1d_norm_t;
 
-/* stats: [N][G][2] double, mean and rstd, for the backward pass; or NULL. */
-size_t conv1d_norm_fwd_workspace_bytes(int N, int C, int L, int G);
+/* stats: [N][G][2] double, mean and rstd, for the backward pass; or NULL.  A workspace of 0 bytes may be NULL. */
+size_t conv1d_norm_fwd_workspace_bytes(int N, int C, int L, int G, int dtype, long x_sc, long x_sl);
 int conv1d_norm_fwd(const conv1d_norm_t* p, void* y, long y_sn, long y_sc, long y_sl, double* stats, void* workspace, size_t workspace_bytes,
                     void* stream);
 
 /* Gradients for dy of the call that p describes and that wrote stats: dx [N][C][L] dtype;  dweight, dbias [C] float, or NULL if not
  * wanted.  The ReLU's gradient is 0 where p is 0 or less, found in 64 bits where p is next to 0. */
-size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G);
+size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G, int dtype, long x_sc, long x_sl);
 int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_sc, long dy_sl, const double* stats, void* dx, long dx_sn,
                     long dx_sc, long dx_sl, float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 

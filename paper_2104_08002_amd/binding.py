@@ -104,11 +104,11 @@ def load() -> ctypes.CDLL:
         ("conv1d_grad_norm", i, [vp, vp, vp, i, i, vp, vp, sz, vp]),
         ("conv1d_grad_clip", i, [vp, vp, vp, i, vp, f, vp]),
         ("conv1d_embed_fwd", i, [vp, vp, vp, l, l, l, vp]),
-        ("conv1d_embed_bwd_workspace_bytes", sz, [i] * 5),
+        ("conv1d_embed_bwd_workspace_bytes", sz, [i] * 5 + [l] * 2),
         ("conv1d_embed_bwd", i, [vp, vp, l, l, l, vp, vp, sz, vp]),
-        ("conv1d_norm_fwd_workspace_bytes", sz, [i] * 4),
+        ("conv1d_norm_fwd_workspace_bytes", sz, [i] * 5 + [l] * 2),
         ("conv1d_norm_fwd", i, [vp, vp, l, l, l, vp, vp, sz, vp]),
-        ("conv1d_norm_bwd_workspace_bytes", sz, [i] * 4),
+        ("conv1d_norm_bwd_workspace_bytes", sz, [i] * 5 + [l] * 2),
         ("conv1d_norm_bwd", i, [vp, vp, l, l, l, vp, vp, l, l, l, vp, vp, vp, sz, vp]),
         ("conv1d_dropout", i, [vp, vp, l, l, vp]),
     ):

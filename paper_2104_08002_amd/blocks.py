@@ -62,13 +62,17 @@ def _ordered_output(out, shape, last, like, ins):
 
 
 # ---- embedding -----------------------------------------------------------------------------------------------------------
-def _embed(tokens, lengths, V, D, dtype, scale, device):
-    if tokens.dim() != 2 or 0 in tokens.shape:
-        raise ValueError("tokens must have the shape [N, L], none of it 0")
-    if tokens.dtype not in (torch.int32, torch.int64):
+def _embed(tokens, lengths, V, D, dtype, scale, device, step=False):
+    if tokens.dim() != (1 if step else 2) or 0 in tokens.shape:
+        raise ValueError(f"tokens must have the shape {'[N]' if step else '[N, L]'}, none of it 0")
+    if tokens.dtype != torch.int64 and tokens.dtype != torch.int32:
         raise TypeError(f"tokens must be int32 or int64: got {tokens.dtype}")
-    N, L = tokens.shape
-    _rows(tokens, "tokens", tokens.shape, tokens.dtype, device)
+    N, L = (tokens.shape[0], 1) if step else tokens.shape
+    if step:
+        if tokens.device != device:
+            raise ValueError("tokens must be on the device of the table")
+    else:
+        _rows(tokens, "tokens", tokens.shape, tokens.dtype, device)
     if lengths is not None:
         _whole(lengths, "lengths", (N,), torch.int32, device)
     return _EMBED.pack(tokens.data_ptr(), _ptr(lengths), tokens.stride(0), N, D, L, V, dtype, EMBED_TOKENS64 if tokens.dtype == torch.int64 else 0, scale)
@@ -100,9 +104,7 @@ def conv1d_embed_fwd(table, tokens, scale: float = 1.0, lengths=None, channels_l
 def conv1d_embed_step(table, tokens, scale: float = 1.0, out=None):
     """y[N, D] = scale * table[tokens] for one token of every sequence, tokens[N]."""
     V, D, code = _table(table)
-    if tokens.dim() != 1:
-        raise ValueError("tokens must have the shape [N]")
-    p = _embed(tokens[:, None], None, V, D, code, scale, table.device)
+    p = _embed(tokens, None, V, D, code, scale, table.device, step=True)
     if out is None:
         y = table.new_empty((tokens.shape[0], D))
     else:
@@ -124,7 +126,7 @@ def conv1d_embed_bwd(dy, tokens, V: int, scale: float = 1.0, lengths=None, works
         raise ValueError(f"tokens must have the shape {[N, L]}")
     sn, sd, sl = _ordered(dy, "dy", dy.shape, dy.dtype, dev)
     lib = binding.load()
-    workspace = _room(workspace, lib.conv1d_embed_bwd_workspace_bytes(N, D, L, V, code), dev)
+    workspace = _room(workspace, lib.conv1d_embed_bwd_workspace_bytes(N, D, L, V, code, sd, sl), dev)
     dtable = torch.empty((V, D), dtype=torch.float32, device=dev)
     binding._check(lib.conv1d_embed_bwd(p, dy.data_ptr(), sn, sd, sl, dtable.data_ptr(), _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return dtable
@@ -148,7 +150,7 @@ def _norm(x, groups, weight, bias, relu, silu, eps, lengths):
     if lengths is not None:
         _whole(lengths, "lengths", (N,), torch.int32, dev)
     return _NORM.pack(x.data_ptr(), _ptr(weight), _ptr(bias), _ptr(lengths), *strides, eps, N, C, L, groups, code,
-                      (NORM_RELU if relu else 0) | (NORM_SILU if silu else 0)), N, C, L
+                      (NORM_RELU if relu else 0) | (NORM_SILU if silu else 0)), (N, C, L, groups, code, *strides[1:])
 
 
 @_on_device
@@ -160,11 +162,11 @@ def conv1d_norm_fwd(x, groups: int, weight=None, bias=None, relu: bool = False, 
 
     lengths int32 [N]: positions from there on are not part of the sequence, y is 0 there.
     """
-    p, N, C, L = _norm(x, groups, weight, bias, relu, silu, eps, lengths)
+    p, sizes = _norm(x, groups, weight, bias, relu, silu, eps, lengths)
     lib = binding.load()
     y = _ordered_output(out, x.shape, _channels_last(x), x, (x, weight, bias, lengths))
-    stats = torch.empty((N, groups, 2), dtype=torch.float64, device=x.device) if want_stats else None
-    workspace = _room(workspace, lib.conv1d_norm_fwd_workspace_bytes(N, C, L, groups), x.device)
+    stats = torch.empty((x.shape[0], groups, 2), dtype=torch.float64, device=x.device) if want_stats else None
+    workspace = _room(workspace, lib.conv1d_norm_fwd_workspace_bytes(*sizes), x.device)
     binding._check(lib.conv1d_norm_fwd(p, y.data_ptr(), *y.stride(), _ptr(stats), _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return (y, stats) if want_stats else y
 
@@ -174,7 +176,7 @@ def conv1d_norm_bwd(dy, stats, x, groups: int, weight=None, bias=None, relu: boo
                     workspace=None):
     """(dx, dweight, dbias) of the call of conv1d_norm_fwd that had the same arguments and left `stats`: dx in x's type and order, which
     is dy's too, dweight and dbias [C] float32, None for a parameter that was not there."""
-    p, N, C, L = _norm(x, groups, weight, bias, relu, silu, eps, lengths)
+    (p, sizes), (N, C, L) = _norm(x, groups, weight, bias, relu, silu, eps, lengths), x.shape
     lib, dev, last = binding.load(), x.device, _channels_last(x)
     strides = _ordered(dy, "dy", x.shape, x.dtype, dev)
     if (strides[1] != 1 and C > 1) if last else (strides[2] != 1 and L > 1):
@@ -182,7 +184,7 @@ def conv1d_norm_bwd(dy, stats, x, groups: int, weight=None, bias=None, relu: boo
     _whole(stats, "stats", (N, groups, 2), torch.float64, dev)
     dx = _new(x.shape, last, x)
     dweight, dbias = (None if t is None else torch.empty_like(t) for t in (weight, bias))
-    workspace = _room(workspace, lib.conv1d_norm_bwd_workspace_bytes(N, C, L, groups), dev)
+    workspace = _room(workspace, lib.conv1d_norm_bwd_workspace_bytes(*sizes), dev)
     binding._check(lib.conv1d_norm_bwd(p, dy.data_ptr(), *strides, stats.data_ptr(), dx.data_ptr(), *dx.stride(), _ptr(dweight), _ptr(dbias),
                                        _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return dx, dweight, dbias

@@ -490,7 +490,7 @@ __device__ __forceinline__ void put_keys(const SortArgs& a, SortLds& s) {
             total = a.totals[digit_of];
         }
     } else {
-#pragma unroll 8
+#pragma unroll 16
         for (int t = slice; t < a.tiles; t += kSort / kBins) {
             const int n = counts[t * kBins + digit_of];
             total += n;
@@ -775,11 +775,6 @@ struct JoinArgs {
     int cols, teams;  // vectors of a row that a lane group takes at a time, lane groups of a workgroup
 };
 constexpr int kJoin = 256, kShort = 16;
-// whether the run at the end of `chunk` goes on in the first rows of chunk + i
-__device__ __forceinline__ bool goes_on(const JoinArgs& a, int key, long chunk, int i) {
-    const long at = (chunk + i) * a.chunk;
-    return at < a.M && a.keys[at] == key;
-}
 // 8 columns of a chunk's share
 __device__ __forceinline__ void share(const JoinArgs& a, int c, bool first, int d, float (&v)[8]) {
     row_load8_inside<false>((first ? a.tail : a.head) + static_cast<long>(c) * (8 * a.per_row), d, v);
@@ -793,12 +788,19 @@ __global__ __launch_bounds__(kJoin) void embed_join_kernel(JoinArgs a) {
     const int chunk = first + team;
     if (team < a.teams && chunk < a.chunks - 1) {
         const long behind = (static_cast<long>(chunk) + 1) * a.chunk, from = behind - a.chunk;
-        const int key = a.keys[behind - 1];
-        const bool earlier = a.keys[from] == key && from > 0 && a.keys[from - 1] == key;
-        if (key >= 0 && key < a.V && a.keys[behind] == key && !earlier) {
+        // (all that may be needed is on its way at once)
+        const int key = a.keys[behind - 1], next = a.keys[behind], begin = a.keys[from], before = a.keys[max(from, 1L) - 1];
+        int on_key[kShort];
+#pragma unroll
+        for (int i = 0; i < kShort; ++i) on_key[i] = a.keys[min((chunk + i + 2L) * a.chunk, a.M - 1L)];
+        float ahead[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) share(a, min(chunk + i, a.chunks - 1), i == 0, 8 * lane, ahead[i]);
+        const bool earlier = begin == key && from > 0 && before == key;
+        if (key >= 0 && key < a.V && next == key && !earlier) {
             bool on[kShort];
 #pragma unroll
-            for (int i = 0; i < kShort; ++i) on[i] = goes_on(a, key, chunk, i + 2);
+            for (int i = 0; i < kShort; ++i) on[i] = (chunk + i + 2L) * a.chunk < a.M && on_key[i] == key;
             int many = 1;  // chunks that it goes on in; kShort + 1: that many or more
 #pragma unroll
             for (int i = 0; i < kShort; ++i) many += many == i + 1 && on[i];
@@ -808,13 +810,14 @@ __global__ __launch_bounds__(kJoin) void embed_join_kernel(JoinArgs a) {
                 for (int c0 = lane; c0 < a.per_row; c0 += a.cols) {
                     double sum[8] = {};
                     for (int c = 0; c <= many; c += 4) {  // four shares on their way at a time
-                        float v[4][8];
+                        if (c > 0 || c0 != lane) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) share(a, min(chunk + min(c + i, many), a.chunks - 1), c + i == 0, 8 * c0, v[i]);
+                            for (int i = 0; i < 4; ++i) share(a, min(chunk + min(c + i, many), a.chunks - 1), c + i == 0, 8 * c0, ahead[i]);
+                        }
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) sum[e] += c + i <= many ? static_cast<double>(v[i][e]) : 0.0;
+                            for (int e = 0; e < 8; ++e) sum[e] += c + i <= many ? static_cast<double>(ahead[i][e]) : 0.0;
                     }
                     float v[8];
 #pragma unroll
@@ -992,7 +995,7 @@ Plan plan_of(int N, int D, int L, int V, int dtype, bool turned) {
     while (bits < 31 && (1L << bits) <= V) ++bits;  // the keys 0 ... V
     p.passes = cdiv(bits, 8);
     p.bits = cdiv(bits, p.passes);
-    p.per_lane = p.M <= 64 * kSort ? 1 : kKeys;  // up to 64 tiles, or larger ones
+    p.per_lane = p.M <= kFewTiles * kSort ? 1 : kKeys;
     p.tiles = cdiv(p.M, p.per_lane * kSort);
     p.per_row = (D + 7) / 8;
     // chunks of 32 rows, of 16 where that leaves the chip idle
@@ -1140,10 +1143,10 @@ int conv1d_embed_fwd(const conv1d_embed_t* p, const void* table, void* y, long y
     return status_of(p->dtype == CONV1D_BF16 ? look_up<true>(p, a, st) : look_up<false>(p, a, st));
 }
 
-size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype) {
+size_t conv1d_embed_bwd_workspace_bytes(int N, int D, int L, int V, int dtype, long dy_sd, long dy_sl) {
     if (N < 1 || D < 1 || L < 1 || V < 1 || !sizes_ok(N, D, L, V) || (dtype != CONV1D_FP32 && dtype != CONV1D_BF16)) return 0;
-    const size_t few = is_few(N, D, L, V, dtype, true) ? few_plan(N, D, L, V, dtype).bytes : plan_of(N, D, L, V, dtype, true).bytes, rest = plan_of(N, D, L, V, dtype, false).bytes;
-    return few > rest ? few : rest;  // for dy in either order
+    const bool turned = is_turned(D, L, dy_sd, dy_sl);
+    return is_few(N, D, L, V, dtype, turned) ? few_plan(N, D, L, V, dtype).bytes : plan_of(N, D, L, V, dtype, turned).bytes;
 }
 
 int conv1d_embed_bwd(const conv1d_embed_t* p, const void* dy, long dy_sn, long dy_sd, long dy_sl, float* dtable, void* workspace, size_t workspace_bytes,

@@ -1005,14 +1005,9 @@ int act_flag(int flags) { return flags & CONV1D_NORM_RELU ? kRelu : flags & CONV
 bool is_whole(const conv1d_norm_t* p, bool last) { return last ? p->C % 8 == 0 : p->L % 8 == 0 && !p->lengths; }
 int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; }
 
-size_t workspace_of(int N, int C, int L, int G, bool back) {
-    if (N < 1 || C < 1 || L < 1 || G < 1 || C % G || !sizes_ok(N, C, L, G)) return 0;
-    size_t most = 0;
-    for (int i = 0; i < 4; ++i) {
-        const size_t n = plan_of(N, C, L, G, i & 1 ? CONV1D_BF16 : CONV1D_FP32, i & 2, back).bytes;
-        most = n > most ? n : most;
-    }
-    return most;
+size_t workspace_of(int N, int C, int L, int G, int dtype, long x_sc, long x_sl, bool back) {
+    if (N < 1 || C < 1 || L < 1 || G < 1 || C % G || !sizes_ok(N, C, L, G) || (dtype != CONV1D_FP32 && dtype != CONV1D_BF16)) return 0;
+    return plan_of(N, C, L, G, dtype, order_of(C, L, x_sc, x_sl) == 2, back).bytes;
 }
 
 }  // namespace
@@ -1022,8 +1017,12 @@ using namespace conv1d;
 
 extern "C" {
 
-size_t conv1d_norm_fwd_workspace_bytes(int N, int C, int L, int G) { return workspace_of(N, C, L, G, false); }
-size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G) { return workspace_of(N, C, L, G, true); }
+size_t conv1d_norm_fwd_workspace_bytes(int N, int C, int L, int G, int dtype, long x_sc, long x_sl) {
+    return workspace_of(N, C, L, G, dtype, x_sc, x_sl, false);
+}
+size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G, int dtype, long x_sc, long x_sl) {
+    return workspace_of(N, C, L, G, dtype, x_sc, x_sl, true);
+}
 
 int conv1d_norm_fwd(const conv1d_norm_t* p, void* y, long y_sn, long y_sc, long y_sl, double* stats, void* workspace, size_t workspace_bytes, void* stream) {
     if (!shape_ok(p) || !y) return CONV1D_EINVAL;

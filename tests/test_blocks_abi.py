@@ -46,12 +46,11 @@ def test_embedding_refusals_of_tensors(lib):
     assert bwd(_embed(), FAKE, 600, 200, 2, FAKE, FAKE, 1 << 40, None) == EINVAL
     assert bwd(_embed(), FAKE, 600, 100, 1, FAKE, FAKE + 128, 1 << 40, None) == EINVAL
     for V in (50, 5000):
-        need = lib.conv1d_embed_bwd_workspace_bytes(2, 6, 100, V, 0)
-        assert need > 0
-        # either order has to fit in it; one of them needs all of it
-        st = [bwd(_embed(V=V), FAKE, *s, FAKE, None, 0, None) for s in ((600, 100, 1), (600, 1, 6))]
-        assert st == [EWORKSPACE, EWORKSPACE]
-    assert lib.conv1d_embed_bwd_workspace_bytes(0, 6, 100, 50, 0) == 0 and lib.conv1d_embed_bwd_workspace_bytes(2, 6, 100, 50, 3) == 0
+        for s in ((600, 100, 1), (600, 1, 6)):
+            need = lib.conv1d_embed_bwd_workspace_bytes(2, 6, 100, V, 0, *s[1:])
+            assert need > 0
+            assert bwd(_embed(V=V), FAKE, *s, FAKE, None, need, None) == EWORKSPACE and bwd(_embed(V=V), FAKE, *s, FAKE, FAKE, need - 1, None) == EWORKSPACE
+    assert lib.conv1d_embed_bwd_workspace_bytes(0, 6, 100, 50, 0, 100, 1) == 0 and lib.conv1d_embed_bwd_workspace_bytes(2, 6, 100, 50, 3, 100, 1) == 0
 
 
 def _norm(**kw):
@@ -77,7 +76,8 @@ def test_norm_refusals_of_tensors(lib):
     assert fwd(_norm(), FAKE, 600, 1, 6, None, FAKE, 1 << 40, None) == EINVAL             # y in the other order
     assert fwd(_norm(), FAKE, 600, 100, 1, FAKE + 4, FAKE, 1 << 40, None) == EINVAL
     assert fwd(_norm(), FAKE, 600, 100, 1, None, FAKE + 8, 1 << 40, None) == EINVAL
-    need = lib.conv1d_norm_fwd_workspace_bytes(2, 6, 100000, 1)
+    need = lib.conv1d_norm_fwd_workspace_bytes(2, 6, 100000, 1, 0, 100000, 1)
+    assert need > 0 and lib.conv1d_norm_fwd_workspace_bytes(2, 6, 100, 3, 0, 100, 1) == 0   # small groups: one launch
     assert fwd(_norm(**big), FAKE, 600000, 100000, 1, None, FAKE, 0, None) == EWORKSPACE
     assert fwd(_norm(**big), FAKE, 600000, 100000, 1, None, None, need, None) == EWORKSPACE
     rest = (FAKE, FAKE, FAKE, 1 << 40, None)
@@ -87,7 +87,7 @@ def test_norm_refusals_of_tensors(lib):
     assert bwd(_norm(), FAKE, 600, 100, 1, FAKE, None, 600, 100, 1, *rest) == EINVAL
     assert bwd(_norm(), FAKE, 600, 100, 1, FAKE, FAKE, 600, 1, 6, *rest) == EINVAL
     assert bwd(_norm(), FAKE, 600, 100, 1, FAKE, FAKE, 600, 100, 1, FAKE, FAKE, FAKE, 8, None) == EWORKSPACE
-    assert lib.conv1d_norm_bwd_workspace_bytes(2, 6, 100, 4) == 0
+    assert lib.conv1d_norm_bwd_workspace_bytes(2, 6, 100, 4, 0, 100, 1) == 0 and lib.conv1d_norm_bwd_workspace_bytes(2, 6, 100, 3, 2, 100, 1) == 0
 
 
 def _dropout(**kw):

@@ -39,7 +39,7 @@ def _embed_case(lib, c):
     strides = (2 * D * L, 1, 2 * D) if last else (2 * D * L, L, 1)
     y += (D if last else D * L) * e
     st = lib.conv1d_embed_fwd(ctypes.byref(p), mem.tensor(V * D * e, e), y, *strides, None)
-    n = lib.conv1d_embed_bwd_workspace_bytes(N, D, L, V, dtype)
+    n = lib.conv1d_embed_bwd_workspace_bytes(N, D, L, V, dtype, *strides[1:])
     return st or lib.conv1d_embed_bwd(ctypes.byref(p), y, *strides, mem.tensor(4 * V * D, 4), mem.tensor(n, 256), n, None)
 
 
@@ -62,10 +62,10 @@ def _norm_case(lib, c):
     at = (C if last else C * L) * e
     x, y, dy, dx = mem.tensor(2 * rows, e) + at, mem.tensor(rows, e), mem.tensor(2 * rows, e) + at, mem.tensor(rows, e)
     p = Norm(x, mem.tensor(4 * C, 4) if opt else None, mem.tensor(4 * C, 4) if opt else None, _lengths(mem, N, L, kind), *wide, 1e-5, N, C, L, G, dtype, act)
-    n = lib.conv1d_norm_fwd_workspace_bytes(N, C, L, G)
+    n = lib.conv1d_norm_fwd_workspace_bytes(N, C, L, G, dtype, *wide[1:])
     stats = mem.tensor(16 * N * G, 8)
     st = lib.conv1d_norm_fwd(ctypes.byref(p), y, *dense, stats if opt else None, mem.tensor(n, 256), n, None)
-    n = lib.conv1d_norm_bwd_workspace_bytes(N, C, L, G)
+    n = lib.conv1d_norm_bwd_workspace_bytes(N, C, L, G, dtype, *wide[1:])
     return st or lib.conv1d_norm_bwd(ctypes.byref(p), dy, *wide, stats, dx, *dense, mem.tensor(4 * C, 4) if opt else None, mem.tensor(4 * C, 4) if opt else None,
                                      mem.tensor(n, 256), n, None)
 
