@@ -9,6 +9,7 @@ Devices, streams, outputs and workspaces as in ``sequence``.
 """
 from __future__ import annotations
 
+import functools
 import struct
 from typing import Optional
 
@@ -24,6 +25,12 @@ NORM_RELU, NORM_SILU = 1, 2
 _EMBED = struct.Struct("2Pl6if4x")
 _NORM = struct.Struct("4P3ld6i")
 _DROPOUT = struct.Struct("4P4l2Ld4i")
+
+
+# how much room a call of these sizes needs (a call into the library, each time, is 1 us)
+@functools.lru_cache(maxsize=256)
+def _room_for(what, *sizes):
+    return getattr(binding.load(), what + "_workspace_bytes")(*sizes)
 
 
 def _ordered(t, name, shape, dtype, device):
@@ -126,7 +133,7 @@ def conv1d_embed_bwd(dy, tokens, V: int, scale: float = 1.0, lengths=None, works
         raise ValueError(f"tokens must have the shape {[N, L]}")
     sn, sd, sl = _ordered(dy, "dy", dy.shape, dy.dtype, dev)
     lib = binding.load()
-    workspace = _room(workspace, lib.conv1d_embed_bwd_workspace_bytes(N, D, L, V, code, sd, sl), dev)
+    workspace = _room(workspace, _room_for("conv1d_embed_bwd", N, D, L, V, code, sd, sl), dev)
     dtable = torch.empty((V, D), dtype=torch.float32, device=dev)
     binding._check(lib.conv1d_embed_bwd(p, dy.data_ptr(), sn, sd, sl, dtable.data_ptr(), _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return dtable
@@ -166,7 +173,7 @@ def conv1d_norm_fwd(x, groups: int, weight=None, bias=None, relu: bool = False, 
     lib = binding.load()
     y = _ordered_output(out, x.shape, _channels_last(x), x, (x, weight, bias, lengths))
     stats = torch.empty((x.shape[0], groups, 2), dtype=torch.float64, device=x.device) if want_stats else None
-    workspace = _room(workspace, lib.conv1d_norm_fwd_workspace_bytes(*sizes), x.device)
+    workspace = _room(workspace, _room_for("conv1d_norm_fwd", *sizes), x.device)
     binding._check(lib.conv1d_norm_fwd(p, y.data_ptr(), *y.stride(), _ptr(stats), _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return (y, stats) if want_stats else y
 
@@ -184,7 +191,7 @@ def conv1d_norm_bwd(dy, stats, x, groups: int, weight=None, bias=None, relu: boo
     _whole(stats, "stats", (N, groups, 2), torch.float64, dev)
     dx = _new(x.shape, last, x)
     dweight, dbias = (None if t is None else torch.empty_like(t) for t in (weight, bias))
-    workspace = _room(workspace, lib.conv1d_norm_bwd_workspace_bytes(*sizes), dev)
+    workspace = _room(workspace, _room_for("conv1d_norm_bwd", *sizes), dev)
     binding._check(lib.conv1d_norm_bwd(p, dy.data_ptr(), *strides, stats.data_ptr(), dx.data_ptr(), *dx.stride(), _ptr(dweight), _ptr(dbias),
                                        _ptr(workspace), _bytes(workspace), binding._current_stream()))
     return dx, dweight, dbias

@@ -462,8 +462,9 @@ __global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
         s = fma(static_cast<double>(w), static_cast<double>(s8), s);
         q = fma(static_cast<double>(w), static_cast<double>(q8), q);
     }
-    block_sums<THREADS>(s, q, lds);  // (with barriers, behind which every vector's sums are there)
+    block_sums<THREADS>(s, q, lds);
     if (a.extra) {
+        __syncthreads();  // every vector's sums are there
         // lanes of a channel: as many as there are for all of them, up to a wave
         int lanes = 1;
         while (lanes < kSeqWave && 2 * lanes * a.per <= THREADS) lanes *= 2;
@@ -820,7 +821,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
 
 // ---- host -----------------------------------------------------------------------------------------------------------
 constexpr long kFill = 2048;   // workgroups that keep the chip busy: 8 a compute unit
-constexpr int kMostPieces = 512, kOne = 1024, kOneBack = 512;
+constexpr int kMostPieces = 512;
 
 int ceil_to(long n, int to) { return static_cast<int>((n + to - 1) / to * to); }
 
@@ -855,9 +856,15 @@ Plan plan_of(int N, int C, int L, int G, int dtype, bool last, bool back) {
     } else {
         p.vecs = (L + 7) / 8;
         p.items = static_cast<int>(static_cast<long>(C / G) * p.vecs);
-        // what a workgroup's lanes hold: up to four vectors each, two of x and two of dy for floats backward
-        const int most = back && dtype == CONV1D_FP32 ? 2 : kAhead, wide = back ? kOneBack : kOne;
-        p.one = p.items <= most * kThreads ? kThreads : p.items <= most * wide ? wide : 0;
+        // A workgroup for each group: four vectors a lane (two of x and two of dy for floats backward), one wave where groups are small and
+        // many.  Two launches, which share a group out, take over where few groups leave the chip idle: 16 groups of 4096 vectors forward
+        // 8.4 and 6.4 us, of 2048 backward 10.5 and 7.0 (256 groups: 11.7 and 15.2; 1024 groups of 512: 10.9 and 13.6).
+        const int most = back && dtype == CONV1D_FP32 ? 2 : kAhead;
+        const bool few = groups < (back ? 128 : 32);
+        if (p.items <= most * kSeqWave && groups >= kFill / 2) p.one = kSeqWave;
+        else if (p.items <= most * kThreads && (!back || !few || p.items <= 512)) p.one = kThreads;
+        else if (p.items <= most * 2 * kThreads && !(back && few)) p.one = 2 * kThreads;
+        else if (p.items <= most * 4 * kThreads && !back && !few) p.one = 4 * kThreads;
         if (p.one) {
             p.pieces = 1;
             p.part = take(back ? static_cast<size_t>(N) * C : 0);
@@ -943,8 +950,13 @@ hipError_t launch_units(void (*kern)(NormArgs, More...), NormArgs& a, int thread
 template <bool BF16, int ACT, bool WHOLE>
 hipError_t forward(NormArgs& a, const Plan& plan, hipStream_t st) {
     const long groups = static_cast<long>(a.N) * a.G;
-    if (plan.one == kThreads) return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kThreads>, a, kThreads, groups, 1, 0, st);
-    if (plan.one) return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kOne>, a, kOne, groups, 1, 0, st);
+    switch (plan.one) {
+        case kSeqWave: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kSeqWave>, a, kSeqWave, groups, 1, 0, st);
+        case kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kThreads>, a, kThreads, groups, 1, 0, st);
+        case 2 * kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>, a, 2 * kThreads, groups, 1, 0, st);
+        case 4 * kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, 4 * kThreads>, a, 4 * kThreads, groups, 1, 0, st);
+        default: break;
+    }
     if (!plan.last) {
         const hipError_t e = launch_units(norm_sums_kernel<BF16, WHOLE>, a, kThreads, groups * plan.pieces, 1, 0, st);
         return e == hipSuccess ? launch_units(norm_apply_kernel<BF16, ACT, WHOLE>, a, kThreads, groups * plan.pieces, 1, 0, st) : e;
@@ -967,7 +979,9 @@ hipError_t backward(NormArgs& a, const Plan& plan, double* sums, double* groups,
         a.extra = channels;
         for (long u = 0; u < many && e == hipSuccess; u += most) {
             a.first = static_cast<int>(u);
-            e = launch_kernel(plan.one == kThreads ? norm_back_one_kernel<BF16, ACT, WHOLE, kThreads> : norm_back_one_kernel<BF16, ACT, WHOLE, kOneBack>,
+            e = launch_kernel(plan.one == kSeqWave   ? norm_back_one_kernel<BF16, ACT, WHOLE, kSeqWave>
+                              : plan.one == kThreads ? norm_back_one_kernel<BF16, ACT, WHOLE, kThreads>
+                                                     : norm_back_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>,
                               dim3(static_cast<unsigned>(many - u < most ? many - u : most)), dim3(plan.one), 0, st, a);
         }
         if (e == hipSuccess && channels) e = launch_kernel(norm_channels_kernel, dim3(channels), dim3(kThreads), 0, st, a);
