@@ -819,6 +819,152 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
     }
 }
 
+// ---- channels contiguous, a workgroup a group ---------------------------------------------------------------------------------
+// A lane has 8 neighbouring channels of the group at K positions, tall apart, in registers.
+__device__ __forceinline__ Lane group_lane(const NormArgs& a, int c0, int threads) {
+    Lane r;
+    r.vecs = (a.per + 7) >> 3;
+    r.tall = threads / r.vecs;
+    r.l0 = static_cast<int>(threadIdx.x) / r.vecs;
+    r.c = r.l0 < r.tall ? 8 * (static_cast<int>(threadIdx.x) - r.l0 * r.vecs) : a.per;  // within the group
+    return r;
+}
+// K positions' vectors, of a row that is the group's channels at one position
+template <bool BF16, bool WHOLE, int K>
+__device__ __forceinline__ void load_group(const NormArgs& a, const void* base, int n, long sn, long sl, int c0, const Lane& k, Raw8<BF16> (&r)[K]) {
+    using T = typename RowElem<BF16>::type;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const T* row = static_cast<const T*>(base) + n * sn + min(k.l0 + j * k.tall, a.L - 1) * sl + c0;
+        r[j] = raw8_row<BF16, WHOLE>(row, min(k.c, 8 * (k.vecs - 1)), a.per);  // (a lane that has no channels reads the last)
+    }
+}
+
+template <bool BF16, int ACT, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_last_one_kernel(NormArgs a) {
+    using T = typename RowElem<BF16>::type;
+    __shared__ double lds[2 * THREADS / kSeqWave];
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
+    const Lane k = group_lane(a, u.c0, THREADS);
+    Raw8<BF16> raw[kAhead];
+    load_group<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, u.c0, k, raw);
+    const float first = load_elem<BF16>(row_at<BF16>(a.x, u.n, a.x_sn, 0, 0), u.c0);
+    const double shift = u.len > 0 ? first : 0.f;
+    float w[8], b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = u.c0 + min(k.c + e, a.per - 1);
+        w[e] = weight_of(a, c);
+        b[e] = bias_of(a, c);
+    }
+    double s = 0.0, q = 0.0, mean, rstd;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        if (k.l0 + j * k.tall >= u.len || k.c >= a.per) break;
+        float v[8];
+        row_floats<BF16, WHOLE>(raw[j], k.c, a.per, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double d = WHOLE || k.c + e < a.per ? static_cast<double>(v[e]) - shift : 0.0;
+            s += d;
+            q = fma(d, d, q);
+        }
+    }
+    block_sums<THREADS>(s, q, lds);
+    stats_of(s, q, static_cast<double>(u.len) * a.per, shift, a.eps, mean, rstd);
+    keep_stats(a, u.group, mean, rstd);
+    const Mean m = mean_of(mean, rstd);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        const int l = k.l0 + j * k.tall;
+        if (l >= a.L || k.c >= a.per) break;
+        float v[8];
+        row_floats<BF16, WHOLE>(raw[j], k.c, a.per, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const Channel ch = channel_of(m, w[e], b[e]);
+            const float y = act_of<ACT>(fmaf(v[e] - ch.hi, ch.a, ch.b));
+            v[e] = l < u.len ? y : 0.f;
+        }
+        vector_store8<BF16, WHOLE>(static_cast<T*>(a.y) + u.n * a.y_sn + l * a.y_sl + u.c0, k.c, a.per, v);
+    }
+}
+
+template <bool BF16, int ACT, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a) {
+    using T = typename RowElem<BF16>::type;
+    constexpr int K = kAheadBack<BF16>;
+    __shared__ double lds[2 * THREADS / kSeqWave];
+    __shared__ double all[THREADS][8 + 1];
+    const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
+    const int tid = static_cast<int>(threadIdx.x);
+    const Lane k = group_lane(a, u.c0, THREADS);
+    Raw8<BF16> xr[K], gr[K];
+    load_group<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, u.c0, k, xr);
+    load_group<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, u.c0, k, gr);
+    const double mean = a.stats[2L * u.group], rstd = a.stats[2L * u.group + 1];
+    const Mean m = mean_of(mean, rstd);
+    Channel ch[8];
+    float w[8], s8[8] = {}, q8[8] = {};
+    long g[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = u.c0 + min(k.c + e, a.per - 1);
+        w[e] = weight_of(a, c);
+        ch[e] = channel_of(m, w[e], bias_of(a, c));
+        g[e] = u.group;
+    }
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        if (k.l0 + j * k.tall >= u.len || k.c >= a.per) break;
+        float x[8], dy[8], t[8];
+        row_floats<BF16, WHOLE>(xr[j], k.c, a.per, x);
+        row_floats<BF16, WHOLE>(gr[j], k.c, a.per, dy);
+        back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s8[e] += WHOLE || k.c + e < a.per ? dy[e] : 0.f;
+            q8[e] = WHOLE || k.c + e < a.per ? fmaf(dy[e], t[e], q8[e]) : 0.f;
+        }
+    }
+    double s = 0.0, q = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        s = fma(static_cast<double>(w[e]), static_cast<double>(s8[e]), s);
+        q = fma(static_cast<double>(w[e]), static_cast<double>(q8[e]), q);
+    }
+    block_sums<THREADS>(s, q, lds);
+    if (a.extra) {
+        double* part = a.part + 2 * (static_cast<long>(u.n) * a.C + u.c0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) all[tid][e] = h ? with_h(static_cast<double>(q8[e]), static_cast<double>(s8[e]), mean, rstd) : static_cast<double>(s8[e]);
+            __syncthreads();
+            for (int c = tid; c < a.per; c += THREADS) {
+                double sum = 0.0;
+                for (int t = 0; t < k.tall; ++t) sum += all[(c >> 3) + t * k.vecs][c & 7];
+                part[2L * c + h] = u.len > 0 ? sum : 0.0;
+            }
+        }
+    }
+    const double over = u.len > 0 ? 1.0 / (static_cast<double>(u.len) * a.per) : 0.0;
+    const Back back = back_const(m, s * over, with_h(q, s, mean, rstd) * over);
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int l = k.l0 + j * k.tall;
+        if (l >= a.L || k.c >= a.per) break;
+        float x[8], dy[8], t[8];
+        row_floats<BF16, WHOLE>(xr[j], k.c, a.per, x);
+        row_floats<BF16, WHOLE>(gr[j], k.c, a.per, dy);
+        back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(dy[e], ch[e].a, fmaf(t[e], back.q, back.s)) : 0.f;
+        vector_store8<BF16, WHOLE>(static_cast<T*>(a.dx) + u.n * a.dx_sn + l * a.dx_sl + u.c0, k.c, a.per, x);
+    }
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------
 constexpr long kFill = 2048;   // workgroups that keep the chip busy: 8 a compute unit
 constexpr int kMostPieces = 512;
@@ -843,6 +989,20 @@ Plan plan_of(int N, int C, int L, int G, int dtype, bool last, bool back) {
         return here;
     };
     if (last) {
+        // A workgroup for each group, where its lanes hold it, as below (a lane has four positions, two for floats backward).
+        const int K = back && dtype == CONV1D_FP32 ? 2 : kAhead, per = (C / G + 7) / 8;
+        for (int threads : {kSeqWave, kThreads, 2 * kThreads, 4 * kThreads}) {
+            if (threads == 4 * kThreads && back) continue;
+            if (threads == kSeqWave && groups < kFill / 2) continue;
+            if (!p.one && per <= threads && L <= static_cast<long>(K) * (threads / per)) p.one = threads;
+        }
+        if (p.one > kThreads && groups < (back ? 128 : 32)) p.one = 0;
+        if (p.one) {
+            p.pieces = 1;
+            p.part = take(back ? static_cast<size_t>(N) * C : 0);
+            p.bytes = at;
+            return p;
+        }
         p.blocks = cdiv(C, kWide);
         const int vecs = C >= kWide ? kThreads : (C + 7) / 8, tall = kThreads / vecs;
         long pieces = kFill / 2 / (static_cast<long>(N) * p.blocks);
@@ -950,11 +1110,12 @@ hipError_t launch_units(void (*kern)(NormArgs, More...), NormArgs& a, int thread
 template <bool BF16, int ACT, bool WHOLE>
 hipError_t forward(NormArgs& a, const Plan& plan, hipStream_t st) {
     const long groups = static_cast<long>(a.N) * a.G;
+    const auto one = [&](void (*rows)(NormArgs), void (*last)(NormArgs)) { return launch_units(plan.last ? last : rows, a, plan.one, groups, 1, 0, st); };
     switch (plan.one) {
-        case kSeqWave: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kSeqWave>, a, kSeqWave, groups, 1, 0, st);
-        case kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, kThreads>, a, kThreads, groups, 1, 0, st);
-        case 2 * kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>, a, 2 * kThreads, groups, 1, 0, st);
-        case 4 * kThreads: return launch_units(norm_one_kernel<BF16, ACT, WHOLE, 4 * kThreads>, a, 4 * kThreads, groups, 1, 0, st);
+        case kSeqWave: return one(norm_one_kernel<BF16, ACT, WHOLE, kSeqWave>, norm_last_one_kernel<BF16, ACT, WHOLE, kSeqWave>);
+        case kThreads: return one(norm_one_kernel<BF16, ACT, WHOLE, kThreads>, norm_last_one_kernel<BF16, ACT, WHOLE, kThreads>);
+        case 2 * kThreads: return one(norm_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>, norm_last_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>);
+        case 4 * kThreads: return one(norm_one_kernel<BF16, ACT, WHOLE, 4 * kThreads>, norm_last_one_kernel<BF16, ACT, WHOLE, 4 * kThreads>);
         default: break;
     }
     if (!plan.last) {
@@ -979,10 +1140,11 @@ hipError_t backward(NormArgs& a, const Plan& plan, double* sums, double* groups,
         a.extra = channels;
         for (long u = 0; u < many && e == hipSuccess; u += most) {
             a.first = static_cast<int>(u);
-            e = launch_kernel(plan.one == kSeqWave   ? norm_back_one_kernel<BF16, ACT, WHOLE, kSeqWave>
-                              : plan.one == kThreads ? norm_back_one_kernel<BF16, ACT, WHOLE, kThreads>
-                                                     : norm_back_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>,
-                              dim3(static_cast<unsigned>(many - u < most ? many - u : most)), dim3(plan.one), 0, st, a);
+            void (*kern)(NormArgs) = plan.one == kSeqWave   ? (plan.last ? norm_last_back_one_kernel<BF16, ACT, WHOLE, kSeqWave> : norm_back_one_kernel<BF16, ACT, WHOLE, kSeqWave>)
+                                     : plan.one == kThreads ? (plan.last ? norm_last_back_one_kernel<BF16, ACT, WHOLE, kThreads> : norm_back_one_kernel<BF16, ACT, WHOLE, kThreads>)
+                                     : plan.last            ? norm_last_back_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>
+                                                            : norm_back_one_kernel<BF16, ACT, WHOLE, 2 * kThreads>;
+            e = launch_kernel(kern, dim3(static_cast<unsigned>(many - u < most ? many - u : most)), dim3(plan.one), 0, st, a);
         }
         if (e == hipSuccess && channels) e = launch_kernel(norm_channels_kernel, dim3(channels), dim3(kThreads), 0, st, a);
         return e;
@@ -1016,7 +1178,10 @@ hipError_t backward(NormArgs& a, const Plan& plan, int act, double* sums, double
 
 int act_flag(int flags) { return flags & CONV1D_NORM_RELU ? kRelu : flags & CONV1D_NORM_SILU ? kSilu : kNone; }
 // rows of whole vectors, all of which count (channels contiguous: positions that do not are passed over anyway)
-bool is_whole(const conv1d_norm_t* p, bool last) { return last ? p->C % 8 == 0 : p->L % 8 == 0 && !p->lengths; }
+bool is_whole(const conv1d_norm_t* p, const Plan& plan) {
+    if (plan.last) return (plan.one ? p->C / p->G : p->C) % 8 == 0;
+    return p->L % 8 == 0 && !p->lengths;
+}
 int status_of(hipError_t e) { return e == hipSuccess ? CONV1D_OK : CONV1D_EHIP; }
 
 size_t workspace_of(int N, int C, int L, int G, int dtype, long x_sc, long x_sl, bool back) {
@@ -1048,10 +1213,10 @@ int conv1d_norm_fwd(const conv1d_norm_t* p, void* y, long y_sn, long y_sc, long 
     if (workspace_bytes < plan.bytes || (plan.bytes && !workspace)) return CONV1D_EWORKSPACE;
     NormArgs a = args_of(p, plan, workspace);
     a.y = y; a.y_sn = y_sn; a.y_sc = y_sc; a.y_sl = y_sl;
-    a.stats = stats ? stats : plan.last ? reinterpret_cast<double*>(static_cast<char*>(workspace) + plan.groups) : nullptr;
+    a.stats = stats ? stats : plan.last && !plan.one ? reinterpret_cast<double*>(static_cast<char*>(workspace) + plan.groups) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int act = act_flag(p->flags);
-    const bool whole = is_whole(p, plan.last);
+    const bool whole = is_whole(p, plan);
     if (p->dtype == CONV1D_BF16) return status_of(whole ? forward<true, true>(a, plan, act, st) : forward<true, false>(a, plan, act, st));
     return status_of(whole ? forward<false, true>(a, plan, act, st) : forward<false, false>(a, plan, act, st));
 }
@@ -1076,7 +1241,7 @@ int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int act = act_flag(p->flags);
     double *sums = reinterpret_cast<double*>(ws + plan.sums), *groups = reinterpret_cast<double*>(ws + plan.groups);
-    const bool whole = is_whole(p, plan.last);
+    const bool whole = is_whole(p, plan);
     if (p->dtype == CONV1D_BF16) return status_of(whole ? backward<true, true>(a, plan, act, sums, groups, st) : backward<true, false>(a, plan, act, sums, groups, st));
     return status_of(whole ? backward<false, true>(a, plan, act, sums, groups, st) : backward<false, false>(a, plan, act, sums, groups, st));
 }

@@ -73,7 +73,7 @@ def _norm_case(lib, c):
 def test_norm_stays_in_bounds(model):
     rnd = random.Random(6)
     cases = [(N, C, L, G, dt, last, act, kind, 1, at_end)
-             for N, C, L, G in ((1, 1, 1, 1), (2, 6, 1, 3), (1, 15, 2100, 3), (3, 8, 7, 2), (2, 70, 65, 1), (1, 2100, 3, 4), (1, 3, 20001, 1), (600, 4, 9, 4), (2, 2050, 17, 2))
+             for N, C, L, G in ((1, 1, 1, 1), (2, 6, 1, 3), (1, 15, 2100, 3), (3, 8, 7, 2), (2, 70, 65, 1), (1, 2100, 3, 4), (1, 3, 20001, 1), (600, 4, 9, 4), (2, 2050, 17, 2), (1, 24, 5, 1), (2, 48, 40, 2), (1030, 24, 3, 1), (1, 120, 1, 5))
              for dt, act in ((0, 1), (1, 2)) for last in (False, True) for kind in (0, 2) for at_end in (True, False)]
     for _ in range(150):
         G = rnd.choice((1, 2, 3, 4))

@@ -153,7 +153,7 @@ def test_embedding_step(blocks, dtype, N, D, V):
 
 # ---- group norm ------------------------------------------------------------------------------------------------------------------
 NORM = [(1, 1, 1, 1), (2, 6, 1, 3), (3, 12, 7, 4), (2, 15, 2051, 3), (1, 8, 40001, 2), (2, 64, 300, 8), (3, 45, 129, 5), (2, 96, 33, 1), (1, 2100, 5, 7), (40, 32, 16, 32),
-        (2, 3, 5000, 3), (1, 512, 70, 16), (300, 10, 3, 2)]
+        (2, 3, 5000, 3), (1, 512, 70, 16), (300, 10, 3, 2), (1100, 12, 9, 1), (2, 1000, 3, 1), (40, 64, 200, 8), (3, 27, 60, 3), (130, 40, 100, 1)]
 
 
 def _norm_inputs(gen, N, C, L, dtype, at=1.0):
