@@ -720,7 +720,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
 template <bool BF16, int ACT, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs a) {
     __shared__ LastLds lds;
-    constexpr int K = kAheadBack<BF16>;
+    constexpr int K = 2;
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
     const int to = min(u.len, u.from + a.piece);
     const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
