@@ -195,6 +195,25 @@ def test_norm(blocks, dtype, last, act, affine, lengths, N, C, L, G):
 
 
 @ORDER
+@pytest.mark.parametrize("L", [40, 5000])
+def test_norm_of_one_parameter(blocks, last, L):
+    x, dy, weight, bias = _norm_inputs(_gen(L), 3, 24, L, torch.bfloat16)
+    _check_norm(blocks, x, dy, 3, weight, None, "relu", None, last)
+    _check_norm(blocks, x, dy, 3, None, bias, "silu", _lengths("ragged", 3, L), last)
+
+
+@ORDER
+def test_relu_of_values_next_to_zero(blocks, last):
+    """A bias that brings many values of p to within some roundings of 0: which side they lie on is the definition's."""
+    gen = _gen(31)
+    x = torch.randn(2, 16, 3000, generator=gen, device="cuda")
+    x[:, 8:] = x[:, 8:].round()              # few values, so that
+    h = ref.norm(x, x, 2, None, None, "none", 1e-5, None)["y"][0]
+    bias = -h[0, :, 7].float()               # one value a channel lies next to 0
+    _check_norm(blocks, x, torch.randn(2, 16, 3000, generator=gen, device="cuda"), 2, None, bias, "relu", None, last)
+
+
+@ORDER
 @pytest.mark.parametrize("at", [1e3, 1e6])
 def test_norm_of_values_far_from_zero(blocks, last, at):
     """A mean of thousands and millions of spreads; a first value far from the others."""

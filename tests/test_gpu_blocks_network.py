@@ -136,6 +136,45 @@ def test_training_step_captured(ops):
 
 
 @pytest.mark.parametrize("last", [False, True], ids=["positions", "channels"])
+def test_calls_captured(ops, last):
+    """Every way that a call can take, in a graph, replayed on new inputs with eager calls between: sorted and few tokens, groups of one
+    workgroup and of many."""
+    _, blocks = ops
+    gen = _gen(21)
+    order = (lambda v: v.transpose(1, 2).contiguous().transpose(1, 2)) if last else (lambda v: v)
+    sizes = ((3, 16, 4000, 2), (2, 64, 50, 8), (40, 32, 64, 32))
+    xs = [order(torch.randn(N, C, L, generator=gen, device="cuda")) for N, C, L, _ in sizes]
+    tokens = [torch.randint(0, 5000, (N, L), generator=gen, device="cuda") for N, _, L, _ in sizes]
+    table = torch.randn(5000, 16, generator=gen, device="cuda")
+
+    def calls():
+        out = []
+        for x, t, (_, C, _, G) in zip(xs, tokens, sizes):
+            y, stats = blocks.conv1d_norm_fwd(x, G, silu=True, want_stats=True)
+            out += [y, blocks.conv1d_norm_bwd(y, stats, x, G, silu=True)[0], blocks.conv1d_embed_bwd(x, t, 5000), blocks.conv1d_embed_bwd(x, t % 40, 40),
+                    blocks.conv1d_embed_fwd(table, t, channels_last=last), blocks.conv1d_embed_fwd(table, t % 40, channels_last=last)]
+        return out
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = calls()
+    for turn in range(3):
+        for x, t in zip(xs, tokens):
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+            t.copy_(torch.randint(0, 5000, t.shape, generator=gen, device="cuda") ** (turn + 1) % 5000)
+        graph.replay()
+        got = [o.clone() for o in outs]
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, calls())):
+            assert torch.equal(a, b), (turn, i)
+
+
+@pytest.mark.parametrize("last", [False, True], ids=["positions", "channels"])
 @pytest.mark.parametrize("act", ["none", "silu"])
 def test_norm_gradients_against_differences(ops, act, last):
     """(f(v + s d) - f(v - s d)) / 2 s against <gradient, d>, f the sum of y dy, taken in 64 bits, s = 1/64 and d of about 1 an element.
