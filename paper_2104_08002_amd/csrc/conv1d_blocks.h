@@ -108,26 +108,17 @@ __device__ __forceinline__ void floats_of(const Raw8<false>& x, float (&v)[8]) {
     for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x.v[e >> 2][e & 3]);
 }
 
-// A vector of a row of `all` elements from any l < all on.  WHOLE: the row is made of whole vectors.  Else it is loaded without a branch
-// from a place where all 8 are there, which may be up to 7 elements before l, and put right when it is turned into floats (what lies
-// behind the row's end is then some number of the row); rows of fewer than 8 elements are loaded one by one.
-template <bool BF16, bool WHOLE>
-__device__ __forceinline__ Raw8<BF16> raw8_row(const void* row, int l, int all) {
-    if constexpr (WHOLE) return raw8_inside<BF16>(row, l);
-    return all >= 8 ? raw8_inside<BF16>(row, min(l, all - 8)) : raw8<BF16>(row, l, all);
+// A row of `all` elements in vectors of 8.  WHOLE: it is made of whole ones.  Else the last is the row's last 8 elements, of which some are
+// the vector's before as well: they are written twice with one value, and sums leave them out of the last (`first_new` elements).  So every
+// load is of 8 elements that are there, without a branch or a shift.  A row of fewer than 8 elements is one vector, loaded one by one.
+template <bool WHOLE>
+__device__ __forceinline__ int vector_at(int vec, int all) {
+    return WHOLE || all < 8 ? 8 * vec : min(8 * vec, all - 8);
 }
 template <bool BF16, bool WHOLE>
-__device__ __forceinline__ void row_floats(const Raw8<BF16>& r, int l, int all, float (&v)[8]) {
-    floats_of(r, v);
-    if constexpr (!WHOLE) {
-        const int by = all >= 8 ? l - (all - 8) : 0;
-        if (wave_any(by > 0)) {
-#pragma unroll
-            for (int step = 4; step > 0; step >>= 1)
-#pragma unroll
-                for (int e = 0; e + step < 8; ++e) v[e] = by > 0 && (by & step) ? v[e + step] : v[e];
-        }
-    }
+__device__ __forceinline__ Raw8<BF16> raw8_row(const void* row, int at, int all) {
+    if constexpr (WHOLE) return raw8_inside<BF16>(row, at);
+    return all >= 8 ? raw8_inside<BF16>(row, at) : raw8<BF16>(row, at, all);
 }
 // the elements of at .. at + 7 that lie before end
 template <bool BF16, bool WHOLE>

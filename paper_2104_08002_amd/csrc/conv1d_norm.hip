@@ -136,15 +136,16 @@ constexpr int kAheadBack = BF16 ? 4 : 2;  // of x and of dy
 template <bool BF16, int K>
 struct Batch {
     Raw8<BF16> x[K];
-    int c[K], at[K];
+    int c[K], at[K], fresh[K];  // fresh: the first element that no vector before has
 };
-template <bool BF16, int K>
+template <bool BF16, bool WHOLE, int K>
 __device__ __forceinline__ void places_of(const NormArgs& a, int c0, int i0, int step, Batch<BF16, K>& r) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int i = min(i0 + k * step, a.items - 1), of = div31(i, a.by_vecs);
         r.c[k] = c0 + of;
-        r.at[k] = 8 * (i - of * a.vecs);
+        r.at[k] = vector_at<WHOLE>(i - of * a.vecs, a.L);
+        r.fresh[k] = 8 * (i - of * a.vecs) - r.at[k];
     }
 }
 template <bool BF16, bool WHOLE, int K>
@@ -156,12 +157,12 @@ __device__ __forceinline__ void load_rows(const NormArgs& a, const void* base, i
 
 // sums of x - shift and of its squares over one vector's values before len
 template <bool BF16, bool WHOLE>
-__device__ __forceinline__ void add_values(const NormArgs& a, const Raw8<BF16>& raw, int at, int len, double shift, double& s, double& q) {
+__device__ __forceinline__ void add_values(const Raw8<BF16>& raw, int at, int fresh, int len, double shift, double& s, double& q) {
     float v[8];
-    row_floats<BF16, WHOLE>(raw, at, a.L, v);
+    floats_of(raw, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const double d = WHOLE || at + e < len ? static_cast<double>(v[e]) - shift : 0.0;
+        const double d = WHOLE || (e >= fresh && at + e < len) ? static_cast<double>(v[e]) - shift : 0.0;
         s += d;
         q = fma(d, d, q);
     }
@@ -177,7 +178,7 @@ __device__ __forceinline__ double shift_of(const NormArgs& a, int n, int c0, int
 template <bool BF16, int ACT, bool WHOLE>
 __device__ __forceinline__ void apply_vector(const NormArgs& a, const Raw8<BF16>& raw, const Channel& k, int n, int c, int at, int len) {
     float v[8];
-    row_floats<BF16, WHOLE>(raw, at, a.L, v);
+    floats_of(raw, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float y = act_of<ACT>(fmaf(v[e] - k.hi, k.a, k.b));
@@ -209,11 +210,11 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormArgs a) {
     double s = 0.0, q = 0.0;
     for (int i0 = from + static_cast<int>(threadIdx.x); i0 < to; i0 += kThreads * kAhead) {
         Batch<BF16, kAhead> b;
-        places_of(a, u.c0, i0, kThreads, b);
+        places_of<BF16, WHOLE>(a, u.c0, i0, kThreads, b);
         load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (i0 + k * kThreads < to) add_values<BF16, WHOLE>(a, b.x[k], b.at[k], u.len, shift, s, q);
+            if (i0 + k * kThreads < to) add_values<BF16, WHOLE>(b.x[k], b.at[k], b.fresh[k], u.len, shift, s, q);
     }
     block_sums<kThreads>(s, q, lds);
     if (threadIdx.x == 0) {
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a) {
     const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
     const int from = u.piece * a.piece + static_cast<int>(threadIdx.x), to = min(a.items, (u.piece + 1) * a.piece);
     Batch<BF16, kAhead> b;
-    places_of(a, u.c0, from, kThreads, b);
+    places_of<BF16, WHOLE>(a, u.c0, from, kThreads, b);
     load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     const double shift = shift_of<BF16>(a, u.n, u.c0, u.len);
     double s = 0.0, q = 0.0, mean, rstd;
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormArgs a) {
                 apply_vector<BF16, ACT, WHOLE>(a, b.x[k], channel_of(m, weight_of(a, b.c[k]), bias_of(a, b.c[k])), u.n, b.c[k], b.at[k], u.len);
         i0 += kThreads * kAhead;
         if (i0 >= to) break;
-        places_of(a, u.c0, i0, kThreads, b);
+        places_of<BF16, WHOLE>(a, u.c0, i0, kThreads, b);
         load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     }
 }
@@ -268,13 +269,13 @@ __global__ __launch_bounds__(THREADS) void norm_one_kernel(NormArgs a) {
     const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
     const int tid = static_cast<int>(threadIdx.x);
     Batch<BF16, kAhead> b;
-    places_of(a, u.c0, tid, THREADS, b);
+    places_of<BF16, WHOLE>(a, u.c0, tid, THREADS, b);
     load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     const double shift = shift_of<BF16>(a, u.n, u.c0, u.len);
     double s = 0.0, q = 0.0, mean, rstd;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-        if (tid + k * THREADS < a.items) add_values<BF16, WHOLE>(a, b.x[k], b.at[k], u.len, shift, s, q);
+        if (tid + k * THREADS < a.items) add_values<BF16, WHOLE>(b.x[k], b.at[k], b.fresh[k], u.len, shift, s, q);
     block_sums<THREADS>(s, q, lds);
     stats_of(s, q, static_cast<double>(u.len) * a.per, shift, a.eps, mean, rstd);
     keep_stats(a, u.group, mean, rstd);
@@ -287,17 +288,17 @@ __global__ __launch_bounds__(THREADS) void norm_one_kernel(NormArgs a) {
 
 // sums of dp and dp t over a vector's positions before len
 template <bool BF16, int ACT, bool WHOLE>
-__device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, long group, int c, int at, int len,
-                                          float& s, float& q) {
+__device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, long group, int c, int at, int fresh,
+                                          int len, float& s, float& q) {
     float x[8], g[8], t[8];
-    row_floats<BF16, WHOLE>(xr, at, a.L, x);
-    row_floats<BF16, WHOLE>(gr, at, a.L, g);
+    floats_of(xr, x);
+    floats_of(gr, g);
     back8<ACT, 0>(a, x, &k, &group, c, t, g);
     s = q = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        s += WHOLE || at + e < len ? g[e] : 0.f;
-        q = WHOLE || at + e < len ? fmaf(g[e], t[e], q) : q;
+        s += WHOLE || (e >= fresh && at + e < len) ? g[e] : 0.f;
+        q = WHOLE || (e >= fresh && at + e < len) ? fmaf(g[e], t[e], q) : q;
     }
 }
 // dx of a vector
@@ -305,8 +306,8 @@ template <bool BF16, int ACT, bool WHOLE>
 __device__ __forceinline__ void back_vector(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, const Back& back, int n, long group, int c,
                                             int at, int len) {
     float x[8], g[8], t[8];
-    row_floats<BF16, WHOLE>(xr, at, a.L, x);
-    row_floats<BF16, WHOLE>(gr, at, a.L, g);
+    floats_of(xr, x);
+    floats_of(gr, g);
     back8<ACT, 0>(a, x, &k, &group, c, t, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = WHOLE || at + e < len ? fmaf(g[e], k.a, fmaf(t[e], back.q, back.s)) : 0.f;
@@ -333,10 +334,12 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
     double s = 0.0, q = 0.0;
     for (int i0 = from; i0 < to; i0 += a.lanes * K) {
         Raw8<BF16> v[K], g[K];
-        int at[K];
+        int at[K], fresh[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            at[k] = 8 * min(i0 + k * a.lanes, to - 1);
+            const int vec = min(i0 + k * a.lanes, to - 1);
+            at[k] = vector_at<WHOLE>(vec, a.L);
+            fresh[k] = 8 * vec - at[k];
             v[k] = raw8_row<BF16, WHOLE>(x, at[k], a.L);
             g[k] = raw8_row<BF16, WHOLE>(dy, at[k], a.L);
         }
@@ -346,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
         for (int k = 0; k < K; ++k) {
             if (i0 + k * a.lanes >= to) break;
             float s8, q8;
-            back_sums<BF16, ACT, WHOLE>(a, v[k], g[k], ch, group, c, at[k], len, s8, q8);
+            back_sums<BF16, ACT, WHOLE>(a, v[k], g[k], ch, group, c, at[k], fresh[k], len, s8, q8);
             s += static_cast<double>(s8);
             q += static_cast<double>(q8);
         }
@@ -404,7 +407,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_kernel(NormArgs a) {
     const int from = u.piece * a.piece + static_cast<int>(threadIdx.x), to = min(a.items, (u.piece + 1) * a.piece);
     Batch<BF16, K> b;
     Raw8<BF16> g[K];
-    places_of(a, u.c0, from, kThreads, b);
+    places_of<BF16, WHOLE>(a, u.c0, from, kThreads, b);
     load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
     const double mean = a.stats[2L * u.group], rstd = a.stats[2L * u.group + 1];
@@ -428,7 +431,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_kernel(NormArgs a) {
             }
         i0 += kThreads * K;
         if (i0 >= to) break;
-        places_of(a, u.c0, i0, kThreads, b);
+        places_of<BF16, WHOLE>(a, u.c0, i0, kThreads, b);
         load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
         load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
     }
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
     const int tid = static_cast<int>(threadIdx.x);
     Batch<BF16, K> b;
     Raw8<BF16> g[K];
-    places_of(a, u.c0, tid, THREADS, b);
+    places_of<BF16, WHOLE>(a, u.c0, tid, THREADS, b);
     load_rows<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sc, u.len, b, b.x);
     load_rows<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sc, u.len, b, g);
     const double mean = a.stats[2L * u.group], rstd = a.stats[2L * u.group + 1];
@@ -456,7 +459,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
         if (i >= a.items) break;
         const float w = weight_of(a, b.c[k]);
         float s8, q8;
-        back_sums<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), u.group, b.c[k], b.at[k], u.len, s8, q8);
+        back_sums<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), u.group, b.c[k], b.at[k], b.fresh[k], u.len, s8, q8);
         vector[i][0] = s8;
         vector[i][1] = q8;
         s = fma(static_cast<double>(w), static_cast<double>(s8), s);
@@ -504,13 +507,15 @@ constexpr int kWide = 8 * kThreads;
 
 struct Lane {
     int c, l0, tall, vecs;   // first channel (C or more: none), first position and step, lanes of a position
+    int fresh;               // (a group's) the first of its 8 channels that no lane before has
 };
+template <bool WHOLE>
 __device__ __forceinline__ Lane lane_of(const NormArgs& a, int block) {
     Lane r;
     r.vecs = min(kThreads, (a.C - block * kWide + 7) >> 3);
     r.tall = kThreads / r.vecs;
     r.l0 = static_cast<int>(threadIdx.x) / r.vecs;
-    r.c = r.l0 < r.tall ? block * kWide + 8 * (static_cast<int>(threadIdx.x) - r.l0 * r.vecs) : a.C;
+    r.c = r.l0 < r.tall ? vector_at<WHOLE>(block * (kWide / 8) + static_cast<int>(threadIdx.x) - r.l0 * r.vecs, a.C) : a.C;
     return r;
 }
 
@@ -531,8 +536,9 @@ __device__ __forceinline__ LastUnit last_unit(const NormArgs& a, int unit) {
 struct LastLds {
     double v[kThreads][8 + 1];
 };
+template <bool WHOLE>
 __device__ __forceinline__ void channels_out(const NormArgs& a, const Lane& k, const double (&s)[8], const double (&q)[8], double* part, LastLds& lds) {
-    const int tid = static_cast<int>(threadIdx.x), first = k.c - 8 * (tid - k.l0 * k.vecs);
+    const int tid = static_cast<int>(threadIdx.x), block = static_cast<int>(blockIdx.y);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         __syncthreads();
@@ -541,10 +547,11 @@ __device__ __forceinline__ void channels_out(const NormArgs& a, const Lane& k, c
         __syncthreads();
         // a channel of the workgroup's a lane
         for (int i = tid; i < 8 * k.vecs; i += kThreads) {
+            const int c = block * kWide + i, e = c - vector_at<WHOLE>(c >> 3, a.C);
+            if (c >= a.C) break;
             double u = 0.0;
-            for (int t = 0; t < k.tall; ++t) u += lds.v[(i >> 3) + t * k.vecs][i & 7];
-            const int c = first + i;
-            if (c < a.C) part[2L * c + h] = u;
+            for (int t = 0; t < k.tall; ++t) u += lds.v[(i >> 3) + t * k.vecs][e];
+            part[2L * c + h] = u;
         }
     }
 }
@@ -572,7 +579,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_sums_kernel(NormArgs a) {
     __shared__ LastLds lds;
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
     const int to = min(u.len, u.from + a.piece);
-    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    const Lane k = lane_of<WHOLE>(a, static_cast<int>(blockIdx.y));
     double s[8] = {}, q[8] = {};
     if (k.c < a.C && u.from + k.l0 < to) {
         double shift[8];
@@ -580,7 +587,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_sums_kernel(NormArgs a) {
         for (int e = 0; e < 8; ++e) shift[e] = load_elem<BF16>(row_at<BF16>(a.x, u.n, a.x_sn, 0, 0), div31(min(k.c + e, a.C - 1), a.by_per) * a.per);
         const auto add = [&](const Raw8<BF16>& raw) {
             float v[8];
-            row_floats<BF16, WHOLE>(raw, k.c, a.C, v);
+            floats_of(raw, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const double d = static_cast<double>(v[e]) - shift[e];
@@ -602,7 +609,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_sums_kernel(NormArgs a) {
             add(raw[0]);
         }
     }
-    channels_out(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
+    channels_out<WHOLE>(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
 }
 
 // Sums of the pieces of a sample's channels, for one workgroup a sample and group: of its channels together, and (backward) of each.
@@ -685,7 +692,7 @@ template <bool BF16, int ACT, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
     const int to = min(a.L, u.from + a.piece);
-    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    const Lane k = lane_of<WHOLE>(a, static_cast<int>(blockIdx.y));
     if (k.c >= a.C || u.from + k.l0 >= to) return;
     Raw8<BF16> raw[kAhead];
     load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, u.from + k.l0, to, raw);
@@ -693,7 +700,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
     channels_of(a, k.c, groups_of(a, u.n, k.c), ch);
     const auto put = [&](const Raw8<BF16>& r, int l) {
         float v[8];
-        row_floats<BF16, WHOLE>(r, k.c, a.C, v);
+        floats_of(r, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float y = act_of<ACT>(fmaf(v[e] - ch[e].hi, ch[e].a, ch[e].b));
@@ -723,7 +730,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs 
     constexpr int K = 2;
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
     const int to = min(u.len, u.from + a.piece);
-    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    const Lane k = lane_of<WHOLE>(a, static_cast<int>(blockIdx.y));
     double s[8] = {}, q[8] = {};
     if (k.c < a.C && u.from + k.l0 < to) {
         const Groups of = groups_of(a, u.n, k.c);
@@ -731,8 +738,8 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs 
         channels_of(a, k.c, of, ch);
         const auto add = [&](const Raw8<BF16>& xr, const Raw8<BF16>& gr, float (&s8)[8], float (&q8)[8]) {
             float x[8], g[8], t[8];
-            row_floats<BF16, WHOLE>(xr, k.c, a.C, x);
-            row_floats<BF16, WHOLE>(gr, k.c, a.C, g);
+            floats_of(xr, x);
+            floats_of(gr, g);
             back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -771,7 +778,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs 
             q[e] = with_h(q[e], s[e], a.stats[2 * of.g[e]], a.stats[2 * of.g[e] + 1]);
         }
     }
-    channels_out(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
+    channels_out<WHOLE>(a, k, s, q, a.part + 2L * u.unit * a.C, lds);
 }
 
 template <bool BF16, int ACT, bool WHOLE>
@@ -780,7 +787,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
     if (took_channels(a, sums, 1)) return;
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) - a.extra + a.first);
     const int to = min(a.L, u.from + a.piece);
-    const Lane k = lane_of(a, static_cast<int>(blockIdx.y));
+    const Lane k = lane_of<WHOLE>(a, static_cast<int>(blockIdx.y));
     if (k.c >= a.C || u.from + k.l0 >= to) return;
     Raw8<BF16> xr[K], gr[K];
     load_last<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, k, u.from + k.l0, to, xr);
@@ -795,8 +802,8 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
     }
     const auto put = [&](const Raw8<BF16>& xr1, const Raw8<BF16>& gr1, int l) {
         float x[8], g[8], t[8];
-        row_floats<BF16, WHOLE>(xr1, k.c, a.C, x);
-        row_floats<BF16, WHOLE>(gr1, k.c, a.C, g);
+        floats_of(xr1, x);
+        floats_of(gr1, g);
         back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(g[e], ch[e].a, fmaf(t[e], back[e].q, back[e].s)) : 0.f;
@@ -821,12 +828,14 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
 
 // ---- channels contiguous, a workgroup a group ---------------------------------------------------------------------------------
 // A lane has 8 neighbouring channels of the group at K positions, tall apart, in registers.
-__device__ __forceinline__ Lane group_lane(const NormArgs& a, int c0, int threads) {
+template <bool WHOLE>
+__device__ __forceinline__ Lane group_lane(const NormArgs& a, int threads) {
     Lane r;
     r.vecs = (a.per + 7) >> 3;
     r.tall = threads / r.vecs;
     r.l0 = static_cast<int>(threadIdx.x) / r.vecs;
-    r.c = r.l0 < r.tall ? 8 * (static_cast<int>(threadIdx.x) - r.l0 * r.vecs) : a.per;  // within the group
+    r.c = r.l0 < r.tall ? vector_at<WHOLE>(static_cast<int>(threadIdx.x) - r.l0 * r.vecs, a.per) : a.per;  // within the group
+    r.fresh = r.l0 < r.tall ? 8 * (static_cast<int>(threadIdx.x) - r.l0 * r.vecs) - r.c : 8;
     return r;
 }
 // K positions' vectors, of a row that is the group's channels at one position
@@ -836,7 +845,7 @@ __device__ __forceinline__ void load_group(const NormArgs& a, const void* base, 
 #pragma unroll
     for (int j = 0; j < K; ++j) {
         const T* row = static_cast<const T*>(base) + n * sn + min(k.l0 + j * k.tall, a.L - 1) * sl + c0;
-        r[j] = raw8_row<BF16, WHOLE>(row, min(k.c, 8 * (k.vecs - 1)), a.per);  // (a lane that has no channels reads the last)
+        r[j] = raw8_row<BF16, WHOLE>(row, min(k.c, vector_at<WHOLE>(k.vecs - 1, a.per)), a.per);  // (a lane that has no channels reads the last)
     }
 }
 
@@ -845,7 +854,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_one_kernel(NormArgs a) {
     using T = typename RowElem<BF16>::type;
     __shared__ double lds[2 * THREADS / kSeqWave];
     const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
-    const Lane k = group_lane(a, u.c0, THREADS);
+    const Lane k = group_lane<WHOLE>(a, THREADS);
     Raw8<BF16> raw[kAhead];
     load_group<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, u.c0, k, raw);
     const float first = load_elem<BF16>(row_at<BF16>(a.x, u.n, a.x_sn, 0, 0), u.c0);
@@ -862,10 +871,10 @@ __global__ __launch_bounds__(THREADS) void norm_last_one_kernel(NormArgs a) {
     for (int j = 0; j < kAhead; ++j) {
         if (k.l0 + j * k.tall >= u.len || k.c >= a.per) break;
         float v[8];
-        row_floats<BF16, WHOLE>(raw[j], k.c, a.per, v);
+        floats_of(raw[j], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const double d = WHOLE || k.c + e < a.per ? static_cast<double>(v[e]) - shift : 0.0;
+            const double d = WHOLE || (e >= k.fresh && k.c + e < a.per) ? static_cast<double>(v[e]) - shift : 0.0;
             s += d;
             q = fma(d, d, q);
         }
@@ -879,7 +888,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_one_kernel(NormArgs a) {
         const int l = k.l0 + j * k.tall;
         if (l >= a.L || k.c >= a.per) break;
         float v[8];
-        row_floats<BF16, WHOLE>(raw[j], k.c, a.per, v);
+        floats_of(raw[j], v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const Channel ch = channel_of(m, w[e], b[e]);
@@ -898,7 +907,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
     __shared__ double all[THREADS][8 + 1];
     const Unit u = unit_of(a, static_cast<int>(blockIdx.x) + a.first);
     const int tid = static_cast<int>(threadIdx.x);
-    const Lane k = group_lane(a, u.c0, THREADS);
+    const Lane k = group_lane<WHOLE>(a, THREADS);
     Raw8<BF16> xr[K], gr[K];
     load_group<BF16, WHOLE>(a, a.x, u.n, a.x_sn, a.x_sl, u.c0, k, xr);
     load_group<BF16, WHOLE>(a, a.dy, u.n, a.dy_sn, a.dy_sl, u.c0, k, gr);
@@ -918,13 +927,14 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
     for (int j = 0; j < K; ++j) {
         if (k.l0 + j * k.tall >= u.len || k.c >= a.per) break;
         float x[8], dy[8], t[8];
-        row_floats<BF16, WHOLE>(xr[j], k.c, a.per, x);
-        row_floats<BF16, WHOLE>(gr[j], k.c, a.per, dy);
+        floats_of(xr[j], x);
+        floats_of(gr[j], dy);
         back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s8[e] += WHOLE || k.c + e < a.per ? dy[e] : 0.f;
-            q8[e] = WHOLE || k.c + e < a.per ? fmaf(dy[e], t[e], q8[e]) : 0.f;
+            const bool counts = WHOLE || (e >= k.fresh && k.c + e < a.per);
+            s8[e] += counts ? dy[e] : 0.f;
+            q8[e] = counts ? fmaf(dy[e], t[e], q8[e]) : 0.f;
         }
     }
     double s = 0.0, q = 0.0;
@@ -944,7 +954,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
             __syncthreads();
             for (int c = tid; c < a.per; c += THREADS) {
                 double sum = 0.0;
-                for (int t = 0; t < k.tall; ++t) sum += all[(c >> 3) + t * k.vecs][c & 7];
+                for (int t = 0; t < k.tall; ++t) sum += all[(c >> 3) + t * k.vecs][c - vector_at<WHOLE>(c >> 3, a.per)];
                 part[2L * c + h] = u.len > 0 ? sum : 0.0;
             }
         }
@@ -956,8 +966,8 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
         const int l = k.l0 + j * k.tall;
         if (l >= a.L || k.c >= a.per) break;
         float x[8], dy[8], t[8];
-        row_floats<BF16, WHOLE>(xr[j], k.c, a.per, x);
-        row_floats<BF16, WHOLE>(gr[j], k.c, a.per, dy);
+        floats_of(xr[j], x);
+        floats_of(gr[j], dy);
         back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(dy[e], ch[e].a, fmaf(t[e], back.q, back.s)) : 0.f;
