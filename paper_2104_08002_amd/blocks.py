@@ -125,8 +125,8 @@ def conv1d_embed_step(table, tokens, scale: float = 1.0, out=None):
 def conv1d_embed_bwd(dy, tokens, V: int, scale: float = 1.0, lengths=None, workspace=None):
     """dtable [V, D] float32 for dy[N, D, L], positions or channels contiguous: scale times the sum of dy over the positions of each
     token, in an order that depends on the tokens, the sizes and dy's strides alone."""
-    if dy.dim() != 3 or 0 in dy.shape or V < 1:
-        raise ValueError("dy must have the shape [N, D, L], none of it 0, and V be at least 1")
+    if dy.dim() != 3 or 0 in dy.shape or not 1 <= V < 1 << 31:
+        raise ValueError("dy must have the shape [N, D, L], none of it 0, and V be at least 1 and below 2^31")
     (N, D, L), code, dev = dy.shape, binding._dtype_code(dy), dy.device
     p = _embed(tokens, lengths, V, D, code, scale, dev)
     if tokens.shape != (N, L):

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 // they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
 // running sum by an ordinary addition.  A value that is not finite would reach every token (0 * NaN): where a sum is not finite, the
 // wave workgroup goes through its positions again without such values, which are then added where they belong.
-constexpr int kFewTokens = 1024;
+constexpr int kFewTokens = 65520;  // (16 bits each, 0xffff is no token)
 
 struct FewArgs {
     const void *dy, *tokens;
@@ -976,15 +976,18 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.bytes = sizeof(float) * static_cast<size_t>(p.chunks) * p.Vp * p.Dp;
     return p;
 }
-// Whether the gradient is taken as a product: its time grows with tokens x channels x positions (in tiles of 16: 1e-8 us each, 1.7e-8 for
-// floats, and 12 us), that of the sort with the positions (40 us and 6.5e-5 us each).  Product and sort, us: 8 x 512 x 8192 bfloat16 16 tokens
-// 21 and 53, 64 tokens 35 and 51, 128 tokens 54 and 51; 8 x 128 x 20000 128 tokens 41 and 47, 512 tokens 100 and 58; 12 x 49 x 4999
-// float 256 tokens 29 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 77 and 103, 1024 tokens 126 and 105.
+// Whether the gradient is taken as a product, by what the two take, in us: the product 12, 1e-8 for each token x channel x position (in tiles
+// of 16; floats 1.7e-8), and its partial sums' way to memory and back; the sort 30, 10 a pass, 6.5e-5 a position, and clearing the gradient.
+// Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 53, 64 tokens 35 and 51, 128 tokens 54 and 51; 8 x 128 x 20000 128 tokens
+// 41 and 47, 512 tokens 100 and 58; 12 x 49 x 4999 float 256 tokens 29 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 77 and 103, 1024
+// tokens 126 and 105.
 bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
     const FewPlan p = few_plan(N, D, L, V, dtype);
-    const double M = static_cast<double>(N) * L, work = M * p.Vp * p.Dp * (dtype == CONV1D_BF16 ? 1.0 : 1.7);
-    if (work > 3e9 + 6500.0 * M) return false;
+    const double M = static_cast<double>(N) * L, tile = static_cast<double>(p.Vp) * p.Dp, us_a_byte = 1 / 5.2e6;
+    const double product = 12 + M * tile * (dtype == CONV1D_BF16 ? 1e-8 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte;
+    const double sort = 30 + (V < 256 ? 10 : V < 65536 ? 20 : 30) + 6.5e-5 * M + 4.0 * V * D * us_a_byte;
+    if (product > sort) return false;
     return static_cast<long>(p.chunks) * p.vgroups * p.dgroups <= kMostBlocks && static_cast<long>(p.Vp) * p.Dp / 16 <= kMostBlocks;
 }
 

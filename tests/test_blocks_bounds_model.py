@@ -46,7 +46,7 @@ def _embed_case(lib, c):
 def test_embedding_stays_in_bounds(model):
     rnd = random.Random(5)
     cases = [(N, D, L, V, dt, wide, last, kind, at_end)
-             for N, D, L, V in ((1, 1, 1, 1), (2, 3, 1, 5), (3, 64, 1, 300), (1, 15, 515, 5), (2, 17, 130, 256), (1, 65, 129, 70000), (1, 2100, 9, 3), (2, 8, 1100, 2))
+             for N, D, L, V in ((1, 1, 1, 1), (2, 3, 1, 5), (3, 64, 1, 300), (1, 15, 515, 5), (2, 17, 130, 256), (1, 65, 129, 70000), (1, 2100, 9, 3), (2, 8, 1100, 2), (2, 9, 30, 20000))
              for dt, wide in ((0, True), (1, False)) for last in (False, True) for kind in (0, 2) for at_end in (True, False)]
     for _ in range(150):
         cases.append((rnd.randint(1, 5), rnd.choice((1, 2, 7, 8, 15, 16, 17, 40, 64, 70, 130)), rnd.choice((1, 2, 7, 8, 33, 127, 128, 300, 513, 700)),

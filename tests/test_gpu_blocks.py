@@ -67,7 +67,7 @@ GRAD = 75 * ref.U
 
 EMBED = [(1, 1, 1, 1), (2, 3, 7, 5), (3, 15, 1000, 5), (2, 64, 129, 255), (2, 65, 128, 256), (4, 16, 513, 257), (1, 17, 2049, 4000), (2, 130, 300, 70000), (5, 8, 64, 2),
          (2, 2100, 40, 30), (1, 1, 40000, 3), (2, 512, 200, 1000), (70, 20, 9, 300), (9, 40, 1000, 1024),
-         (3, 33, 700, 1025)]
+         (3, 33, 700, 1025), (2, 5, 40, 30000), (1, 48, 100, 65520)]
 
 
 @TYPES
