@@ -118,7 +118,15 @@ __device__ __forceinline__ int vector_at(int vec, int all) {
 template <bool BF16, bool WHOLE>
 __device__ __forceinline__ Raw8<BF16> raw8_row(const void* row, int at, int all) {
     if constexpr (WHOLE) return raw8_inside<BF16>(row, at);
-    return all >= 8 ? raw8_inside<BF16>(row, at) : raw8<BF16>(row, at, all);
+    if (all >= 8) return raw8_inside<BF16>(row, at);
+    Raw8<BF16> r{};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < all) {
+            if constexpr (BF16) r.v[0][e >> 1] |= static_cast<unsigned>(static_cast<const unsigned short*>(row)[e]) << (16 * (e & 1));
+            else r.v[e >> 2][e & 3] = static_cast<const unsigned*>(row)[e];
+        }
+    return r;
 }
 // the elements of at .. at + 7 that lie before end
 template <bool BF16, bool WHOLE>

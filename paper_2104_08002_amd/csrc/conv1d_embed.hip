@@ -965,7 +965,10 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
     if (chunk >= 2L * L) {
+        // (a workgroup goes through its samples one behind the other: no more than a few for the partial sums' sake)
+        const long share = want > 1 ? (M / want + L - 1) / L : N, most = share > 4 ? share : 4;
         p.samples = static_cast<int>(chunk / L < N ? chunk / L : N);
+        if (p.samples > most) p.samples = static_cast<int>(most);
         p.chunk = L;
     } else {
         p.samples = 1;

@@ -81,14 +81,16 @@ __device__ __forceinline__ float weight_of(const NormArgs& a, int c) { return a.
 __device__ __forceinline__ float bias_of(const NormArgs& a, int c) { return a.bias ? a.bias[c] : 0.f; }
 
 // a number with the sign that p has in 64 bits
-__device__ __forceinline__ float side_of(const NormArgs& a, float x, long group, int c) {
+__device__ __forceinline__ float side_of(const NormArgs& a, float x, int n, int c) {
+    const long group = static_cast<long>(n) * a.G + div31(c, a.by_per);
     const double p = (static_cast<double>(x) - a.stats[2 * group]) * a.stats[2 * group + 1] * static_cast<double>(weight_of(a, c)) + static_cast<double>(bias_of(a, c));
     return p > 0.0 ? 1.f : p <= 0.0 ? -1.f : __builtin_nanf("");
 }
 
-// t = x - hi of 8 values, and dp in place of dy; channel e is k[STEP e], c + STEP e in group g[STEP e]
+// t = x - hi of 8 values, and dp in place of dy; channel e is k[STEP e], number c + STEP e.  (What lies next to 0 is rare: it goes through
+// one value at a time, so that it costs the other path no registers.)
 template <int ACT, int STEP>
-__device__ __forceinline__ void back8(const NormArgs& a, const float (&x)[8], const Channel* k, const long* g, int c, float (&t)[8], float (&dy)[8]) {
+__device__ __forceinline__ void back8(const NormArgs& a, const float (&x)[8], const Channel* k, int n, int c, float (&t)[8], float (&dy)[8]) {
     float p[8];
     bool near = false;
 #pragma unroll
@@ -99,8 +101,15 @@ __device__ __forceinline__ void back8(const NormArgs& a, const float (&x)[8], co
     }
     if (ACT == kRelu) {
         if (wave_any(near)) {
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) {
+                float v = x[0];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = side_of(a, x[e], g[STEP * e], min(c + STEP * e, a.C - 1));
+                for (int e = 1; e < 8; ++e) v = i == e ? x[e] : v;
+                const float side = side_of(a, v, n, min(c + STEP * i, a.C - 1));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[e] = i == e ? side : p[e];
+            }
         }
     }
 #pragma unroll
@@ -290,12 +299,12 @@ __global__ __launch_bounds__(THREADS) void norm_one_kernel(NormArgs a) {
 
 // sums of dp and dp t over a vector's positions before len
 template <bool BF16, int ACT, bool WHOLE>
-__device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, long group, int c, int at, int fresh,
+__device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, int n, int c, int at, int fresh,
                                           int len, float& s, float& q) {
     float x[8], g[8], t[8];
     floats_of(xr, x);
     floats_of(gr, g);
-    back8<ACT, 0>(a, x, &k, &group, c, t, g);
+    back8<ACT, 0>(a, x, &k, n, c, t, g);
     s = q = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -305,12 +314,12 @@ __device__ __forceinline__ void back_sums(const NormArgs& a, const Raw8<BF16>& x
 }
 // dx of a vector
 template <bool BF16, int ACT, bool WHOLE>
-__device__ __forceinline__ void back_vector(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, const Back& back, int n, long group, int c,
+__device__ __forceinline__ void back_vector(const NormArgs& a, const Raw8<BF16>& xr, const Raw8<BF16>& gr, const Channel& k, const Back& back, int n, int c,
                                             int at, int len) {
     float x[8], g[8], t[8];
     floats_of(xr, x);
     floats_of(gr, g);
-    back8<ACT, 0>(a, x, &k, &group, c, t, g);
+    back8<ACT, 0>(a, x, &k, n, c, t, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = WHOLE || at + e < len ? fmaf(g[e], k.a, fmaf(t[e], back.q, back.s)) : 0.f;
     vector_store8<BF16, WHOLE>(row_at<BF16>(a.dx, n, a.dx_sn, c, a.dx_sc), at, a.L, x);
@@ -351,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormArgs a) {
         for (int k = 0; k < K; ++k) {
             if (i0 + k * a.lanes >= to) break;
             float s8, q8;
-            back_sums<BF16, ACT, WHOLE>(a, v[k], g[k], ch, group, c, at[k], fresh[k], len, s8, q8);
+            back_sums<BF16, ACT, WHOLE>(a, v[k], g[k], ch, n, c, at[k], fresh[k], len, s8, q8);
             s += static_cast<double>(s8);
             q += static_cast<double>(q8);
         }
@@ -429,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_kernel(NormArgs a) {
         for (int k = 0; k < K; ++k)
             if (i0 + k * kThreads < to) {
                 const float w = weight_of(a, b.c[k]);
-                back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, u.group, b.c[k], b.at[k], u.len);
+                back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, b.c[k], b.at[k], u.len);
             }
         i0 += kThreads * K;
         if (i0 >= to) break;
@@ -461,7 +470,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
         if (i >= a.items) break;
         const float w = weight_of(a, b.c[k]);
         float s8, q8;
-        back_sums<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), u.group, b.c[k], b.at[k], b.fresh[k], u.len, s8, q8);
+        back_sums<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), u.n, b.c[k], b.at[k], b.fresh[k], u.len, s8, q8);
         vector[i][0] = s8;
         vector[i][1] = q8;
         s = fma(static_cast<double>(w), static_cast<double>(s8), s);
@@ -498,7 +507,7 @@ __global__ __launch_bounds__(THREADS) void norm_back_one_kernel(NormArgs a) {
     for (int k = 0; k < K; ++k) {
         if (tid + k * THREADS >= a.items) break;
         const float w = weight_of(a, b.c[k]);
-        back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, u.group, b.c[k], b.at[k], u.len);
+        back_vector<BF16, ACT, WHOLE>(a, b.x[k], g[k], channel_of(m, w, bias_of(a, b.c[k])), back, u.n, b.c[k], b.at[k], u.len);
     }
 }
 
@@ -727,7 +736,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_apply_kernel(NormArgs a) {
 }
 
 template <bool BF16, int ACT, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void norm_last_back_sums_kernel(NormArgs a) {
     __shared__ LastLds lds;
     constexpr int K = 2;
     const LastUnit u = last_unit(a, static_cast<int>(blockIdx.x) + a.first);
@@ -742,7 +751,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_sums_kernel(NormArgs 
             float x[8], g[8], t[8];
             floats_of(xr, x);
             floats_of(gr, g);
-            back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
+            back8<ACT, 1>(a, x, ch, u.n, k.c, t, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 s8[e] += g[e];
@@ -806,7 +815,7 @@ __global__ __launch_bounds__(kThreads) void norm_last_back_kernel(NormArgs a, co
         float x[8], g[8], t[8];
         floats_of(xr1, x);
         floats_of(gr1, g);
-        back8<ACT, 1>(a, x, ch, of.g, k.c, t, g);
+        back8<ACT, 1>(a, x, ch, u.n, k.c, t, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(g[e], ch[e].a, fmaf(t[e], back[e].q, back[e].s)) : 0.f;
         vector_store8<BF16, WHOLE>(row_at<BF16>(a.dx, u.n, a.dx_sn, l, a.dx_sl), k.c, a.C, x);
@@ -917,13 +926,11 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
     const Mean m = mean_of(mean, rstd);
     Channel ch[8];
     float w[8], s8[8] = {}, q8[8] = {};
-    long g[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int c = u.c0 + min(k.c + e, a.per - 1);
         w[e] = weight_of(a, c);
         ch[e] = channel_of(m, w[e], bias_of(a, c));
-        g[e] = u.group;
     }
 #pragma unroll
     for (int j = 0; j < K; ++j) {
@@ -931,7 +938,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
         float x[8], dy[8], t[8];
         floats_of(xr[j], x);
         floats_of(gr[j], dy);
-        back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
+        back8<ACT, 1>(a, x, ch, u.n, u.c0 + k.c, t, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool counts = WHOLE || (e >= k.fresh && k.c + e < a.per);
@@ -970,7 +977,7 @@ __global__ __launch_bounds__(THREADS) void norm_last_back_one_kernel(NormArgs a)
         float x[8], dy[8], t[8];
         floats_of(xr[j], x);
         floats_of(gr[j], dy);
-        back8<ACT, 1>(a, x, ch, g, u.c0 + k.c, t, dy);
+        back8<ACT, 1>(a, x, ch, u.n, u.c0 + k.c, t, dy);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = l < u.len ? fmaf(dy[e], ch[e].a, fmaf(t[e], back.q, back.s)) : 0.f;
         vector_store8<BF16, WHOLE>(static_cast<T*>(a.dx) + u.n * a.dx_sn + l * a.dx_sl + u.c0, k.c, a.per, x);
@@ -1011,6 +1018,7 @@ Plan plan_of(int N, int C, int L, int G, int dtype, bool last, bool back) {
             if (threads == kSeqWave && !many) continue;
             if (threads == 2 * kThreads && many && (back || C / G * (dtype == CONV1D_BF16 ? 2 : 4) < 64)) continue;
             if (threads == 4 * kThreads && (many || back)) continue;
+            if (C / G < 8 && static_cast<long>(N) * C * L > 1 << 16) continue;  // (less than a vector: the general way shares lines better)
             if (!p.one && per <= threads && L <= static_cast<long>(K) * (threads / per)) p.one = threads;
         }
         if (p.one > kThreads && groups < (back ? 128 : 32)) p.one = 0;
