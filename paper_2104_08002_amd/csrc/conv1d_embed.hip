@@ -919,7 +919,9 @@ hipError_t look_up(const conv1d_embed_t* p, LookArgs& a, hipStream_t st) {
     }
     void (*kern)(LookArgs) = nullptr;
     size_t lds = 0;
-    if (p->V < kFewRows) {
+    // A few channels leave most lanes of a tile's loads idle (16 x 15 x 60000 bfloat16, 5 tokens 11.7 us for 17.8 by tiles, 1000 tokens 19 for 24; 12 x
+    // 49 x 4999 float, 256 tokens 8.2 for 8.3); tiles are faster for more (8 x 128 x 20000 bfloat16, 4 tokens 11.5 for 14.6, 1000 tokens 11 for 22).
+    if (p->V < kFewRows && (p->D <= 16 || (p->D <= 48 && p->V <= 256))) {
         // as many channels a workgroup as leave enough workgroups, and room for several beside each other
         a.tiles = cdiv(p->L, 8 * kThreads);
         a.per_row = 16;

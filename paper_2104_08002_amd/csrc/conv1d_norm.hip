@@ -633,7 +633,7 @@ __device__ __forceinline__ void join_pieces(const NormArgs& a, int n, int c0, do
         double cs = 0.0, cq = 0.0;
         if (share < shares && c < a.per) {
             const double* part = a.part + 2L * (static_cast<long>(n) * a.pieces * a.C + c0 + c);
-#pragma unroll 4
+#pragma unroll 12
             for (int p = share; p < a.pieces; p += shares) {
                 cs += part[2L * p * a.C];
                 cq += part[2L * p * a.C + 1];
