@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kThreads) void embed_turn_kernel(LookArgs a) {
     }
 }
 
-// Few tokens (16 x 15 x 60000 bfloat16, five of them, in 64 bits: 11.7 us, 18.3 by tiles): the workgroup's channels of the whole table, scaled and rounded, lie in LDS (and a row of zeros for no token); a lane has
+// Few tokens and channels (16 x 15 x 60000 bfloat16, five tokens: 11.7 us, 17.8 by tiles): the workgroup's channels of the whole table, scaled and rounded, lie in LDS (and a row of zeros for no token); a lane has
 // 8 positions, whose tokens (read side by side, and handed over in LDS) it keeps.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void embed_few_kernel(LookArgs a) {
@@ -141,10 +141,11 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 
 // ---- backward, few tokens: a product with truth values ----------------------------------------------------------------------
 // Bound by memory for tens of tokens (16 x 15 x 60000 bfloat16, five: 12.8 us, 36 MB), by the vector units for hundreds (12 x 49 x 4999 float, 257:
-// 22 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
+// 24 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
 // B operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum
 // they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
-// running sum by an ordinary addition.  A value that is not finite would reach every token (0 * NaN): where a sum is not finite, the
+// running sum by ordinary additions; of a float, the upper 8 bits by themselves: 32 of them add up to 24 bits and lose nothing as long as their
+// exponents are less than 11 apart (all three parts in one sum, 12 x 49 x 4999, 257 tokens: error against 64 bits 1.3e-7 of the norm).  A value that is not finite would reach every token (0 * NaN): where a sum is not finite, the
 // wave workgroup goes through its positions again without such values, which are then added where they belong.
 constexpr int kFewTokens = 65520;  // (16 bits each, 0xffff is no token)
 
@@ -302,10 +303,13 @@ __device__ __forceinline__ void few_sums(const FewArgs& a, const Chunk& t, int v
                 const u32x4 one = truth8(k, v0 + 16 * v + (lane & 15));
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    f32x4 s = sp::mfma(x[d].p[0], one, f32x4{0.f, 0.f, 0.f, 0.f});
+                    const f32x4 none = f32x4{0.f, 0.f, 0.f, 0.f};
+                    f32x4 s = sp::mfma(x[d].p[0], one, none);
                     if constexpr (!BF16) {
                         s = sp::mfma(x[d].p[1], one, s);
-                        s = sp::mfma(x[d].p[2], one, s);
+                        const f32x4 h = sp::mfma(x[d].p[2], one, none);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[e] += h[e];
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[v][d][e] += s[e];

@@ -6,7 +6,7 @@
 // pieces to fill the chip: one launch adds up each piece, the next joins a group's pieces (every workgroup for itself, in one order)
 // and writes.  Values are summed as differences from the group's first one, in 64 bits, so that neither a mean far from 0 nor a
 // long group costs digits; mean and rstd are kept in 64 bits, and (x - mean) is taken with the mean as two floats.
-// 8 x 64 x 20000 bfloat16 in 8 groups: 7 + 9 us forward, 11 + 15 backward (20, 41, 41 and 61 MB: 2.9 to 4.6 TB/s in one turn of the chip);
+// 8 x 64 x 20000 bfloat16 in 8 groups: 7 + 9 us forward, 11 + 14 backward (20, 41, 41 and 61 MB: 2.9 to 4.4 TB/s in one turn of the chip);
 // 8 x 512 x 8192 with channels next to each other: 15 + 5 + 28 forward, 32 + 5 + 39 backward (67, 134, 134 and 201 MB: 4.2 to 5.1 TB/s).
 #include "conv1d_blocks.h"
 
