@@ -288,12 +288,19 @@ def conv1d_dropout(x, p: float, key: int, call: int = 0, counter=None, residual=
 
 
 class Dropout(torch.nn.Module):
-    """Dropout of a share `p`, with a residual: each call in training takes the next `call` of its key.  Layers have a key each.  A
-    captured step brings a `counter` that it moves on, since the calls' numbers are fixed in the graph."""
+    """Dropout of a share `p`, with a residual: each call in training takes the next `call` of its key, both of which a state dict
+    holds.  Layers have a key each.  A captured step brings a `counter` that it moves on, since the calls' numbers are fixed in
+    the graph."""
 
     def __init__(self, p: float, key: int, call: int = 0):
         super().__init__()
         self.p, self.key, self.call = p, key, call
+
+    def get_extra_state(self):
+        return {"key": self.key, "call": self.call}
+
+    def set_extra_state(self, state):
+        self.key, self.call = state["key"], state["call"]
 
     def forward(self, x, residual=None, lengths=None, counter=None):
         if not self.training:

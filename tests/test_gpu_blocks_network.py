@@ -331,6 +331,9 @@ def test_autograd_of_broadcast_and_unusual_inputs(ops):
     layer = autograd.Dropout(0.5, key=3)
     a, b = layer(x.detach()), layer(x.detach())
     assert not torch.equal(a, b) and torch.equal(b, blocks.conv1d_dropout(x.detach(), 0.5, 3, 1))
+    again = autograd.Dropout(0.5, key=9)
+    again.load_state_dict(layer.state_dict())
+    assert torch.equal(again(x.detach()), layer(x.detach()))
     layer.eval()
     assert torch.equal(layer(x.detach(), residual=r.detach()), x.detach() + r.detach())
     norm, embed = autograd.GroupNorm(2, C, relu=True), autograd.Embedding(5, C, scale=2.0, dtype=torch.bfloat16)
