@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 
 // ---- backward, few tokens: a product with truth values ----------------------------------------------------------------------
 // Bound by memory for tens of tokens (16 x 15 x 60000 bfloat16, five: 12.8 us, 36 MB), by the vector units for hundreds (12 x 49 x 4999 float, 257:
-// 24 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
+// 22 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
 // B operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum
 // they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
 // running sum by ordinary additions; of a float, the upper 8 bits by themselves: 32 of them add up to 24 bits and lose nothing as long as their
@@ -227,7 +227,7 @@ __device__ __forceinline__ Chunk chunk_of(const FewArgs& a, int chunk) {
 }
 // steps whose loads a wave has in flight, beside as many that it multiplies
 template <bool BF16, int DB>
-constexpr int kU = BF16 && DB == 1 ? 4 : 2;
+constexpr int kU = BF16 ? (DB == 1 ? 4 : 2) : (DB == 1 ? 2 : 1);
 constexpr int kMostBlock = 32 * kWaves * 4;
 
 // A block of the chunk: positions l0 ... of sample n, of which len count.
@@ -248,7 +248,7 @@ __device__ __forceinline__ Block settle(const FewArgs& a, const Chunk& t, Block 
 template <bool BF16, int U, int DB>
 struct FewLoads {
     Raw8<BF16> raw[U][DB];
-    int toks[U * 32 * kWaves / kThreads ? U * 32 * kWaves / kThreads : 1];
+    int toks[(U * 32 * kWaves + kThreads - 1) / kThreads];
 };
 template <bool BF16, int U, int DB>
 __device__ __forceinline__ void load_block(const FewArgs& a, const Block& b, int d0, FewLoads<BF16, U, DB>& r) {
@@ -256,7 +256,7 @@ __device__ __forceinline__ void load_block(const FewArgs& a, const Block& b, int
     constexpr int BLOCK = 32 * kWaves * U;
     const int tid = static_cast<int>(threadIdx.x), lane = tid & (kSeqWave - 1), l = b.l0 + 32 * U * (tid / kSeqWave) + 8 * (lane >> 4);
 #pragma unroll
-    for (int i = 0; i < BLOCK / kThreads; ++i) r.toks[i] = token_at(a.tokens, a.wide, b.n, a.tok_sn, b.l0 + i * kThreads + tid, b.len, a.V);
+    for (int i = 0; i * kThreads < BLOCK; ++i) r.toks[i] = token_at(a.tokens, a.wide, b.n, a.tok_sn, b.l0 + i * kThreads + tid, b.len, a.V);
     const T* base = static_cast<const T*>(a.dy) + b.n * a.dy_sn;
     const bool inside = b.l0 + BLOCK <= b.len;
 #pragma unroll
@@ -286,7 +286,7 @@ __device__ __forceinline__ void few_sums(const FewArgs& a, const Chunk& t, int v
     load_block(a, b, d0, now);
     for (int turn = 0;; turn ^= 1) {
 #pragma unroll
-        for (int i = 0; i < BLOCK / kThreads; ++i) toks[turn][i * kThreads + tid] = static_cast<unsigned short>(now.toks[i]);
+        for (int i = 0; i * kThreads < BLOCK; ++i) toks[turn][i * kThreads + tid] = static_cast<unsigned short>(now.toks[i]);
         __syncthreads();  // (the next block writes the other half, the one after that waits behind the next)
         const Block after = settle(a, t, Block{b.n, b.l0 + BLOCK, 0});
         const bool more = after.n < t.n0 + t.samples;
@@ -322,8 +322,9 @@ __device__ __forceinline__ void few_sums(const FewArgs& a, const Chunk& t, int v
     }
 }
 
+// (three workgroups a compute unit for bfloat16: 8 x 128 x 20000, 64 tokens 25 us for 31 with two; for floats they would spill)
 template <bool BF16, int VB, int DB>
-__global__ __launch_bounds__(kThreads) void embed_few_sums_kernel(FewArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 ? 3 : 2) void embed_few_sums_kernel(FewArgs a) {
     using T = typename RowElem<BF16>::type;
     __shared__ float lds[VB * 16][DB * 16 + 4];
     const int unit = static_cast<int>(blockIdx.x), cd = div31(unit, a.by_vgroups), v0 = (unit - cd * a.vgroups) * (16 * VB);
@@ -966,7 +967,7 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.dgroups = cdiv(p.Dp, 16 * p.DB);
     // enough workgroups to fill the chip once (three of the largest tiles fit a compute unit), but no more partial sums than dy has
     // numbers; in whole blocks
-    const long M = static_cast<long>(N) * L, step = 32L * kWaves * (dtype == CONV1D_BF16 && p.DB == 1 ? kU<true, 1> : kU<false, 1>);
+    const long M = static_cast<long>(N) * L, step = 32L * kWaves * (dtype == CONV1D_BF16 ? (p.DB == 1 ? kU<true, 1> : kU<true, 4>) : (p.DB == 1 ? kU<false, 1> : kU<false, 4>));
     const long want = (p.VB * p.DB == 16 ? 3 * kFill / 8 : kFill) / (static_cast<long>(p.vgroups) * p.dgroups);
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
@@ -985,16 +986,16 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.bytes = sizeof(float) * static_cast<size_t>(p.chunks) * p.Vp * p.Dp;
     return p;
 }
-// Whether the gradient is taken as a product, by what the two take, in us: the product 12, 1e-8 for each token x channel x position (in tiles
+// Whether the gradient is taken as a product, by what the two take, in us: the product 12, 6.5e-9 for each token x channel x position (in tiles
 // of 16; floats 1.7e-8), and its partial sums' way to memory and back; the sort 30, 10 a pass, 6.5e-5 a position, and clearing the gradient.
-// Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 53, 64 tokens 35 and 51, 128 tokens 54 and 51; 8 x 128 x 20000 128 tokens
-// 41 and 47, 512 tokens 100 and 58; 12 x 49 x 4999 float 256 tokens 29 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 77 and 103, 1024
-// tokens 126 and 105.
+// Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 49, 128 tokens 40 and 48, 256 tokens 65 and 55; 8 x 128 x 20000 256 tokens
+// 43 and 53, 512 tokens 70 and 53; 12 x 49 x 4999 float 256 tokens 32 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 73 and 104, 1024
+// tokens 121 and 106.
 bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
     const FewPlan p = few_plan(N, D, L, V, dtype);
     const double M = static_cast<double>(N) * L, tile = static_cast<double>(p.Vp) * p.Dp, us_a_byte = 1 / 5.2e6;
-    const double product = 12 + M * tile * (dtype == CONV1D_BF16 ? 1e-8 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte;
+    const double product = 12 + M * tile * (dtype == CONV1D_BF16 ? 6.5e-9 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte;
     const double sort = 30 + (V < 256 ? 10 : V < 65536 ? 20 : 30) + 6.5e-5 * M + 4.0 * V * D * us_a_byte;
     if (product > sort) return false;
     return static_cast<long>(p.chunks) * p.vgroups * p.dgroups <= kMostBlocks && static_cast<long>(p.Vp) * p.Dp / 16 <= kMostBlocks;
