@@ -290,7 +290,11 @@ def conv1d_dropout(x, p: float, key: int, call: int = 0, counter=None, residual=
 class Dropout(torch.nn.Module):
     """Dropout of a share `p`, with a residual: each call in training takes the next `call` of its key, both of which a state dict
     holds.  Layers have a key each.  A captured step brings a `counter` that it moves on, since the calls' numbers are fixed in
-    the graph."""
+    the graph.
+
+    A pass that is run again for its gradient (activation checkpointing) has to drop what it dropped before: it is handed its `call`,
+    `checkpoint(block, x, layer.next_call())`, and leaves the module's own number alone.  Without one, a pass within a running backward pass is
+    refused."""
 
     def __init__(self, p: float, key: int, call: int = 0):
         super().__init__()
@@ -302,8 +306,16 @@ class Dropout(torch.nn.Module):
     def set_extra_state(self, state):
         self.key, self.call = state["key"], state["call"]
 
-    def forward(self, x, residual=None, lengths=None, counter=None):
+    def next_call(self) -> int:
+        """Takes a call's number, for a pass that is handed it."""
+        self.call += 1
+        return self.call - 1
+
+    def forward(self, x, residual=None, lengths=None, counter=None, call=None):
         if not self.training:
             return conv1d_dropout(x, 0.0, 0, residual=residual, lengths=lengths)
-        self.call += 1
-        return conv1d_dropout(x, self.p, self.key, self.call - 1, counter, residual, lengths)
+        if call is None:
+            if torch._C._current_graph_task_id() != -1:
+                raise RuntimeError("dropout within a backward pass is a pass run again: it needs the call that it had (Dropout.next_call)")
+            call = self.next_call()
+        return conv1d_dropout(x, self.p, self.key, call, counter, residual, lengths)
