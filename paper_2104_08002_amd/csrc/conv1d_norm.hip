@@ -30,7 +30,7 @@ struct NormArgs {
     int vecs, items;        // vectors of 8 of a row, of a group
     int pieces, piece;      // of a group, and its vectors
     int rows_pieces, rows_piece, lanes;  // backward: pieces of a row, their vectors, lanes that a piece has
-    int first, extra;       // extra: workgroups of the launch that add up channels (of one workgroup a group: whether they are wanted)
+    int first, extra;       // extra: workgroups of each of the grid's rows that add up channels (of one workgroup a group: whether they are wanted)
     Div31 by_vecs, by_pieces, by_G, by_C, by_per, by_rows_pieces;
 };
 
@@ -400,11 +400,11 @@ __device__ __forceinline__ void channel_sums(const NormArgs& a, int c, const dou
         if (a.dweight) a.dweight[c] = static_cast<float>(q);
     }
 }
-// the first `a.extra` workgroups of a launch
+// the first `a.extra` workgroups of each of the grid's rows
 __device__ __forceinline__ bool took_channels(const NormArgs& a, const double* part, int each) {
     if (static_cast<int>(blockIdx.x) >= a.extra) return false;
-    const int c = (static_cast<int>(blockIdx.x) * kThreads + static_cast<int>(threadIdx.x)) / kSeqWave;
-    if (blockIdx.y == 0 && c < a.C) channel_sums(a, c, part, each);
+    const int c = (static_cast<int>(blockIdx.y) * a.extra + static_cast<int>(blockIdx.x)) * (kThreads / kSeqWave) + static_cast<int>(threadIdx.x) / kSeqWave;
+    if (c < a.C) channel_sums(a, c, part, each);
     return true;
 }
 __global__ __launch_bounds__(kThreads) void norm_channels_kernel(NormArgs a) { took_channels(a, a.part, 1); }
@@ -1118,11 +1118,12 @@ NormArgs args_of(const conv1d_norm_t* p, const Plan& plan, void* workspace) {
     return a;
 }
 
-// All units of a launch, in pieces that a grid may have; with `extra` workgroups before them in the first.
+// All units of a launch, in pieces that a grid of `blocks` rows may have; with `extra` workgroups, shared out over the rows, before them in the
+// first.  (At most 2^18 of them with one row, and with 2^20 channels 512 in each of 512 rows of 2^14: some are always left for the units.)
 template <typename... More>
 hipError_t launch_units(void (*kern)(NormArgs, More...), NormArgs& a, int threads, long units, int blocks, int extra, hipStream_t st, More... more) {
-    const long most = kSeqMostThreads / threads / blocks - extra;
-    a.extra = extra;
+    a.extra = cdiv(extra, blocks);
+    const long most = kSeqMostThreads / threads / blocks - a.extra;
     for (long u = 0; u < units; u += most, a.extra = 0) {
         a.first = static_cast<int>(u);
         const long some = units - u < most ? units - u : most;
