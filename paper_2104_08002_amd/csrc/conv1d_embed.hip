@@ -158,6 +158,7 @@ struct FewArgs {
     float scale;
     int wide, N, D, L, V, Vp, Dp, vgroups, dgroups;
     int chunk, samples, per_sample, chunks;  // a chunk: positions of a sample, or all of some samples; chunks of a sample (or of those)
+    int slice, slices;                       // chunks that a row of the joining grid has, its rows
     Div31 by_vgroups, by_dgroups, by_sample;
 };
 
@@ -229,6 +230,10 @@ __device__ __forceinline__ Chunk chunk_of(const FewArgs& a, int chunk) {
 template <bool BF16, int DB>
 constexpr int kU = BF16 ? (DB == 1 ? 4 : 2) : (DB == 1 ? 2 : 1);
 constexpr int kMostBlock = 32 * kWaves * 4;
+// Most steps of a wave in one chunk, which bounds the additions in float: chunks are added up in 64 bits.  (Without a bound 2^28 equal floats of one
+// token in 2048 chunks were off by 1e-5; chunks of 16 steps cost nothing up to some millions of positions, 160 x 16 x 2^20 bfloat16, 64 tokens
+// 1.66 ms for 1.76, 32 x 16 x 2^20, 200 tokens 1.21 for 1.05.)
+constexpr int kMostSteps = 16;
 
 // A block of the chunk: positions l0 ... of sample n, of which len count.
 struct Block {
@@ -383,25 +388,48 @@ __global__ __launch_bounds__(kThreads, BF16 ? 3 : 2) void embed_few_sums_kernel(
     }
 }
 
-// 16 neighbouring numbers a workgroup, each the sum of THREADS / 16 lanes' shares of the chunks
+// 16 neighbouring numbers a workgroup, each the sum of THREADS / 16 lanes' shares of the chunks; where few numbers have many chunks, of those
+// that one of a.slices rows of the grid has, left in two floats in the place of its first two.
 constexpr int kFewJoin = 1024;
+constexpr long kSliceChunks = 1024;  // chunks that are worth a slice (kFill / 4 slices and fewer: the last has more than 500)
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void embed_few_join_kernel(FewArgs a) {
     __shared__ double lds[THREADS / 16][17];
-    const int tid = static_cast<int>(threadIdx.x), o = tid & 15, slice = tid >> 4;
-    const long at = 16L * blockIdx.x + o;  // of part
+    const int tid = static_cast<int>(threadIdx.x), o = tid & 15, share = tid >> 4;
+    const int from = static_cast<int>(blockIdx.y) * a.slice, to = min(a.chunks, from + a.slice);
+    const long at = 16L * blockIdx.x + o, step = static_cast<long>(a.Vp) * a.Dp;  // of part
     double s = 0.0;
 #pragma unroll 4
-    for (int c = slice; c < a.chunks; c += THREADS / 16) s += a.part[static_cast<long>(c) * a.Vp * a.Dp + at];
-    lds[slice][o] = s;
+    for (int c = from + share; c < to; c += THREADS / 16) s += a.part[c * step + at];
+    lds[share][o] = s;
     __syncthreads();
 #pragma unroll
     for (int half = THREADS / 32; half > 0; half >>= 1) {
-        if (slice < half) lds[slice][o] += lds[slice + half][o];
+        if (share < half) lds[share][o] += lds[share + half][o];
         __syncthreads();
     }
+    if (share != 0) return;
+    s = lds[0][o];
+    const float high = static_cast<float>(s);
+    if (a.slices > 1) {
+        a.part[from * step + at] = high;
+        a.part[(from + 1) * step + at] = fabsf(high) < INFINITY ? static_cast<float>(s - static_cast<double>(high)) : 0.f;
+        return;
+    }
     const int v = static_cast<int>(at / a.Dp), d = static_cast<int>(at - static_cast<long>(v) * a.Dp);
-    if (slice == 0 && v < a.V && d < a.D) a.dtable[static_cast<long>(v) * a.D + d] = static_cast<float>(lds[0][o]) * a.scale;
+    if (v < a.V && d < a.D) a.dtable[static_cast<long>(v) * a.D + d] = high * a.scale;
+}
+// What the slices left, one number a lane.
+__global__ __launch_bounds__(kThreads) void embed_few_slices_kernel(FewArgs a) {
+    const long at = static_cast<long>(blockIdx.x) * kThreads + threadIdx.x, step = static_cast<long>(a.Vp) * a.Dp;
+    if (at >= step) return;
+    double s = 0.0;
+    for (int i = 0; i < a.slices; ++i) {
+        const float* part = a.part + static_cast<long>(i) * a.slice * step + at;
+        s += static_cast<double>(part[0]) + static_cast<double>(part[step]);
+    }
+    const int v = static_cast<int>(at / a.Dp), d = static_cast<int>(at - static_cast<long>(v) * a.Dp);
+    if (v < a.V && d < a.D) a.dtable[static_cast<long>(v) * a.D + d] = static_cast<float>(s) * a.scale;
 }
 
 // ---- backward, many tokens: the positions in the order of their tokens ---------------------------------------------------------
@@ -966,16 +994,21 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.vgroups = cdiv(p.Vp, 16 * p.VB);
     p.dgroups = cdiv(p.Dp, 16 * p.DB);
     // enough workgroups to fill the chip once (three of the largest tiles fit a compute unit), but no more partial sums than dy has
-    // numbers; in whole blocks
+    // numbers, as long as a wave's sums in float stay short; in whole blocks
     const long M = static_cast<long>(N) * L, step = 32L * kWaves * (dtype == CONV1D_BF16 ? (p.DB == 1 ? kU<true, 1> : kU<true, 4>) : (p.DB == 1 ? kU<false, 1> : kU<false, 4>));
     const long want = (p.VB * p.DB == 16 ? 3 * kFill / 8 : kFill) / (static_cast<long>(p.vgroups) * p.dgroups);
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
+    if (chunk > kMostSteps * 32L * kWaves) chunk = kMostSteps * 32L * kWaves;
     if (chunk >= 2L * L) {
-        // (a workgroup goes through its samples one behind the other: no more than a few for the partial sums' sake)
+        // (a workgroup goes through its samples one behind the other, in blocks of their own: no more than a few for the partial sums' sake)
         const long share = want > 1 ? (M / want + L - 1) / L : N, most = share > 4 ? share : 4;
         p.samples = static_cast<int>(chunk / L < N ? chunk / L : N);
         if (p.samples > most) p.samples = static_cast<int>(most);
+        // the steps of a sample that the first wave has
+        const int of = static_cast<int>(step / (32 * kWaves)), last = cdiv(static_cast<int>(L % step), 32);
+        const int steps = static_cast<int>(L / step) * of + (last < of ? last : of);
+        if (p.samples * steps > kMostSteps) p.samples = kMostSteps / steps;
         p.chunk = L;
     } else {
         p.samples = 1;
@@ -1056,11 +1089,17 @@ hipError_t few_gradient(const conv1d_embed_t* p, const void* dy, long dy_sn, lon
     const unsigned units = static_cast<unsigned>(static_cast<long>(plan.chunks) * plan.vgroups * plan.dgroups);
     const hipError_t e = launch_kernel(kern, dim3(units), dim3(kThreads), 0, st, a);
     if (e != hipSuccess) return e;
-    // few numbers: large workgroups
+    // few numbers: large workgroups, and of many chunks several rows of them (64 x 16 numbers of 131072: 2.61 ms in all for 2.86)
     const long joins = static_cast<long>(plan.Vp) * plan.Dp / 16;
     const bool large = joins < kFill / 8;
-    return launch_kernel(large ? embed_few_join_kernel<kFewJoin> : embed_few_join_kernel<kThreads>, dim3(static_cast<unsigned>(joins)), dim3(large ? kFewJoin : kThreads), 0,
-                         st, a);
+    const long rows = plan.chunks / kSliceChunks < kFill / 4 / joins ? plan.chunks / kSliceChunks : kFill / 4 / joins;
+    a.slices = rows > 1 ? static_cast<int>(rows) : 1;
+    a.slice = cdiv(plan.chunks, a.slices);
+    a.slices = cdiv(plan.chunks, a.slice);
+    const hipError_t j = launch_kernel(large ? embed_few_join_kernel<kFewJoin> : embed_few_join_kernel<kThreads>, dim3(static_cast<unsigned>(joins), static_cast<unsigned>(a.slices)),
+                                       dim3(large ? kFewJoin : kThreads), 0, st, a);
+    if (j != hipSuccess || a.slices == 1) return j;
+    return launch_kernel(embed_few_slices_kernel, dim3(static_cast<unsigned>(cdiv(16 * joins, kThreads))), dim3(kThreads), 0, st, a);
 }
 
 template <bool BF16>
