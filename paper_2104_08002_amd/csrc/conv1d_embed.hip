@@ -982,7 +982,7 @@ hipError_t look_up(const conv1d_embed_t* p, LookArgs& a, hipStream_t st) {
 
 // ---- the gradient's workspace -------------------------------------------------------------------------------------------
 struct FewPlan {
-    int VB, DB, Vp, Dp, vgroups, dgroups, chunk, samples, per_sample, chunks;
+    int VB, DB, Vp, Dp, vgroups, dgroups, block, chunk, samples, per_sample, chunks;  // block: positions that a workgroup takes at a time
     size_t bytes;
 };
 FewPlan few_plan(int N, int D, int L, int V, int dtype) {
@@ -996,6 +996,7 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     // enough workgroups to fill the chip once (three of the largest tiles fit a compute unit), but no more partial sums than dy has
     // numbers, as long as a wave's sums in float stay short; in whole blocks
     const long M = static_cast<long>(N) * L, step = 32L * kWaves * (dtype == CONV1D_BF16 ? (p.DB == 1 ? kU<true, 1> : kU<true, 4>) : (p.DB == 1 ? kU<false, 1> : kU<false, 4>));
+    p.block = static_cast<int>(step);
     const long want = (p.VB * p.DB == 16 ? 3 * kFill / 8 : kFill) / (static_cast<long>(p.vgroups) * p.dgroups);
     long chunk = want > 1 ? (M + want - 1) / want : M;
     if (chunk < p.Vp) chunk = p.Vp;
@@ -1019,17 +1020,28 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
     p.bytes = sizeof(float) * static_cast<size_t>(p.chunks) * p.Vp * p.Dp;
     return p;
 }
-// Whether the gradient is taken as a product, by what the two take, in us: the product 12, 6.5e-9 for each token x channel x position (in tiles
-// of 16; floats 1.7e-8), and its partial sums' way to memory and back; the sort 30, 10 a pass, 6.5e-5 a position, and clearing the gradient.
-// Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 49, 128 tokens 40 and 48, 256 tokens 65 and 55; 8 x 128 x 20000 256 tokens
+// Whether the gradient is taken as a product, by what the two take, in us.
+// Product: 12, 6.5e-9 for each token x channel x position of whole blocks (in tiles of 16; floats 1.7e-8), its partial sums' way to memory and
+// back, and the blocks that a sample's end cuts: their numbers are loaded one by one, and a workgroup goes through its samples in turn.
+// Sort: 11, 20 more up to 20000 positions, 10 a pass, clearing the gradient, and the larger of 6.5e-5 a position and 5e-3 a tile that is turned; what
+// does not stay in the caches goes to memory and back.
+// Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 49, 128 tokens 40 and 46, 256 tokens 65 and 55; 8 x 128 x 20000 256 tokens
 // 43 and 53, 512 tokens 70 and 53; 12 x 49 x 4999 float 256 tokens 32 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 73 and 104, 1024
-// tokens 121 and 106.
+// tokens 121 and 106.  Short samples: 20000 x 8 x 16, 600 tokens 1396 and 112; 20000 x 64 x 16, 64 tokens 580 and 114; 4000 x 64 x 4, 64 tokens
+// 64 and 42; 1000 x 64 x 200, 64 tokens 36 and 40; 16 x 64 x 100, 64 tokens 14 and 21; 20000 x 16 x 2 float, 16 tokens 53 and 169.  (Of 641 sizes the
+// slower way was taken at 182 for more than 1.2 times the time, up to 12.5, before cut blocks counted, now at 52, up to 2.7.)
 bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
     const FewPlan p = few_plan(N, D, L, V, dtype);
+    const bool bf16 = dtype == CONV1D_BF16;
     const double M = static_cast<double>(N) * L, tile = static_cast<double>(p.Vp) * p.Dp, us_a_byte = 1 / 5.2e6;
-    const double product = 12 + M * tile * (dtype == CONV1D_BF16 ? 6.5e-9 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte;
-    const double sort = 30 + (V < 256 ? 10 : V < 65536 ? 20 : 30) + 6.5e-5 * M + 4.0 * V * D * us_a_byte;
+    const double whole = M - static_cast<double>(N) * (L % p.block), cut = L % p.block ? static_cast<double>(N) * p.vgroups * p.dgroups : 0;
+    const double ends = cut * (p.DB == 1 ? (bf16 ? 8e-3 : 4e-3) : bf16 ? 28e-3 : 15e-3) * (L < 16 ? (L + 8) / 24.0 : 1.0), turns = 3.0 * (p.samples - 1);
+    const double product = 12 + whole * tile * (bf16 ? 6.5e-9 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte + (ends > turns ? ends : turns);
+    const double turned_tiles = static_cast<double>(N) * cdiv(L, kTurn / tile_channels(D)) * cdiv(D, tile_channels(D));
+    const double sorts = 6.5e-5 * M > 5e-3 * turned_tiles ? 6.5e-5 * M : 5e-3 * turned_tiles, beyond = M * D * (bf16 ? 2 : 4) - 32e6;
+    const double sort = 11 + (M < 20000 ? M / 1000 : 20) + (V < 256 ? 10 : V < 65536 ? 20 : 30) + sorts + 4.0 * V * D * us_a_byte +
+                        (beyond > 0 ? 2 * beyond * us_a_byte : 0);
     if (product > sort) return false;
     return static_cast<long>(p.chunks) * p.vgroups * p.dgroups <= kMostBlocks && static_cast<long>(p.Vp) * p.Dp / 16 <= kMostBlocks;
 }
