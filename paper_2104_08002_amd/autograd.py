@@ -237,7 +237,8 @@ class NormFunction(torch.autograd.Function):
     def backward(ctx, gy):
         x, weight, bias, lengths, stats = ctx.saved_tensors
         gy = _in_order(gy.resolve_neg().to(x.dtype), blocks._channels_last(x))
-        dx, dweight, dbias = blocks.conv1d_norm_bwd(gy, stats, x, weight=weight, bias=bias, lengths=lengths, **ctx.how)
+        dx, dweight, dbias = blocks.conv1d_norm_bwd(gy, stats, x, weight=weight, bias=bias, lengths=lengths, want_weight=ctx.needs_input_grad[1],
+                                                    want_bias=ctx.needs_input_grad[2], **ctx.how)
         dweight, dbias = (None if g is None else g.to(t) for g, t in zip((dweight, dbias), ctx.types))
         return dx, dweight, dbias, None, None, None, None, None
 

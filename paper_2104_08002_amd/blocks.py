@@ -180,9 +180,9 @@ def conv1d_norm_fwd(x, groups: int, weight=None, bias=None, relu: bool = False, 
 
 @_on_device
 def conv1d_norm_bwd(dy, stats, x, groups: int, weight=None, bias=None, relu: bool = False, silu: bool = False, eps: float = 1e-5, lengths=None,
-                    workspace=None):
+                    workspace=None, want_weight: bool = True, want_bias: bool = True):
     """(dx, dweight, dbias) of the call of conv1d_norm_fwd that had the same arguments and left `stats`: dx in x's type and order, which
-    is dy's too, dweight and dbias [C] float32, None for a parameter that was not there."""
+    is dy's too, dweight and dbias [C] float32, None for a parameter that was not there or whose gradient is not wanted."""
     (p, sizes), (N, C, L) = _norm(x, groups, weight, bias, relu, silu, eps, lengths), x.shape
     lib, dev, last = binding.load(), x.device, _channels_last(x)
     strides = _ordered(dy, "dy", x.shape, x.dtype, dev)
@@ -190,7 +190,7 @@ def conv1d_norm_bwd(dy, stats, x, groups: int, weight=None, bias=None, relu: boo
         raise ValueError("dy must be contiguous along its " + ("channels" if last else "positions") + ", as x is")
     _whole(stats, "stats", (N, groups, 2), torch.float64, dev)
     dx = _new(x.shape, last, x)
-    dweight, dbias = (None if t is None else torch.empty_like(t) for t in (weight, bias))
+    dweight, dbias = (torch.empty_like(t) if want and t is not None else None for t, want in ((weight, want_weight), (bias, want_bias)))
     workspace = _room(workspace, _room_for("conv1d_norm_bwd", *sizes), dev)
     binding._check(lib.conv1d_norm_bwd(p, dy.data_ptr(), *strides, stats.data_ptr(), dx.data_ptr(), *dx.stride(), _ptr(dweight), _ptr(dbias),
                                        _ptr(workspace), _bytes(workspace), binding._current_stream()))
