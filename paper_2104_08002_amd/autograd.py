@@ -290,8 +290,11 @@ def conv1d_dropout(x, p: float, key: int, call: int = 0, counter=None, residual=
 
 class Dropout(torch.nn.Module):
     """Dropout of a share `p`, with a residual: each call in training takes the next `call` of its key, both of which a state dict
-    holds.  Layers have a key each.  A captured step brings a `counter` that it moves on, since the calls' numbers are fixed in
-    the graph.
+    holds.  Layers have a key each, and so have the ranks that share a batch out; what several ranks compute alike takes one key on all of them.
+
+    A captured step brings a `counter`, since the calls' numbers are fixed in the graph: each replay drops what calls `call + counter` drop.  The step
+    moves it on behind its backward pass by as many as the calls that one module made in it (or more): by fewer, a replay's first calls drop what the
+    last ones of the replay before it did.
 
     A pass that is run again for its gradient (activation checkpointing) has to drop what it dropped before: it is handed its `call`,
     `checkpoint(block, x, layer.next_call())`, and leaves the module's own number alone.  Without one, a pass within a running backward pass is
