@@ -361,8 +361,8 @@ int conv1d_grad_clip(void* const* data, const size_t* counts, const int* dtypes,
  * embedding, group norm with an activation, dropout with the residual.  Rules as for
  * the sequence operators (lengths among them); workspaces are 256-byte aligned. */
 
-/* Embedding lookup: y[n][d][l] = scale * table[tokens[n][l]][d], rounded once; 0 behind a sequence's end and where a token is outside
- * [0, V), which has no gradient either.  D <= 2^20, V < 2^30, N * L <= 2^30 (more: CONV1D_EUNSUPPORTED). */
+/* Embedding lookup: y[n][d][l] = scale * table[tokens[n][l]][d], a product of floats rounded to dtype; 0 behind a sequence's end and
+ * where a token is outside [0, V), which has no gradient either.  D <= 2^20, V < 2^30, N * L <= 2^30 (more: CONV1D_EUNSUPPORTED). */
 #define CONV1D_EMBED_TOKENS64 1  /* tokens of 64 bits; else of 32 */
 typedef struct {
     const void* tokens;   /* [N][L], signed; tok_sn apart */
@@ -409,8 +409,8 @@ size_t conv1d_norm_bwd_workspace_bytes(int N, int C, int L, int G, int dtype, lo
 int conv1d_norm_bwd(const conv1d_norm_t* p, const void* dy, long dy_sn, long dy_sc, long dy_sl, const double* stats, void* dx, long dx_sn,
                     long dx_sc, long dx_sl, float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Dropout: y = residual + (kept ? x / (1 - p) : 0), rounded once.  Element (n, c, l) is kept where word l % 4 of block
- * (n * C + c) * ceil(L / 4) + l / 4 is at least floor(p * 2^32); a block is Philox4x32 in seven rounds, its counter the block's number
+/* Dropout: y = residual + (kept ? x / (1 - p) : 0), found in float (the factor, the product, the sum) and rounded to
+ * dtype.  Element (n, c, l) is kept where word l % 4 of block (n * C + c) * ceil(L / 4) + l / 4 is at least floor(p * 2^32); a block is Philox4x32 in seven rounds, its counter the block's number
  * (low words first) and call + *counter, its key `key`.  The same call with the gradient in place of x, and no residual, is its
  * backward pass.  What is dropped reaches nothing, an infinity or NaN neither.  0 <= p <= 1; N * C < 2^31, L <= 2^30. */
 typedef struct {

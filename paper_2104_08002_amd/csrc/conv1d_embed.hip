@@ -1,9 +1,11 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 //   y[n][d][l] = scale table[tokens[n][l]][d],   dtable[v][d] = scale sum over (n, l) with tokens[n][l] = v of dy[n][d][l]
-// Bound by memory.  Where positions are contiguous, tiles of positions and channels are turned in LDS: rows of the table are read
-// and written along the channels, y and dy along the positions.
+// Memory is what large calls wait for (4 to 5 of 5.2 TB/s at 8 x 512 x 8192); launches of one turn of the chip reach 3.  Where positions are
+// contiguous, tiles of positions and channels are turned in LDS: rows of the table are read and written along the channels, y and dy along
+// the positions.
 // The gradient adds the same positions in the same order in every run.  Few tokens: dy is multiplied with the truth values
-// "position l has token v" on the matrix cores, straight from memory.  Many: the positions are sorted by their token (a stable radix
+// "position l has token v" on the matrix cores, straight from memory, at most 16 sums of 32 products in float and four waves' together, the
+// rest in 64 bits.  Many: the positions are sorted by their token (a stable radix
 // sort, least digit first) while dy is turned into rows; each lane group adds a chunk of neighbouring rows in float and writes the
 // runs that lie in its chunk; what of a run lies in several chunks is joined in 64 bits.
 #include "conv1d_blocks.h"
@@ -40,8 +42,8 @@ __device__ __forceinline__ int token_at(const void* tokens, int wide, long n, lo
 
 constexpr int kTile = 8192;  // positions times channels of a tile: 16 or 32 KB
 
-// A tile of kTile / DT positions and DT channels: 8 x 512 x 8192 bfloat16 of 32000 tokens 20 to 23 us, 4.3 to 5 TB/s.  Two elements more than a row's positions: the eight channels that a lane writes, and
-// those of its neighbours, begin in different banks.
+// A tile of kTile / DT positions and DT channels: 8 x 512 x 8192 bfloat16 of 32000 tokens 20 to 23 us, 4.3 to 5 TB/s.  Two elements more than a
+// row's positions: the eight channels that a lane writes, and those of its neighbours, begin in different banks.
 template <bool BF16, int DT>
 __global__ __launch_bounds__(kThreads) void embed_turn_kernel(LookArgs a) {
     using T = typename RowElem<BF16>::type;
@@ -76,8 +78,9 @@ __global__ __launch_bounds__(kThreads) void embed_turn_kernel(LookArgs a) {
     }
 }
 
-// Few tokens and channels (16 x 15 x 60000 bfloat16, five tokens: 11.7 us, 17.8 by tiles): the workgroup's channels of the whole table, scaled and rounded, lie in LDS (and a row of zeros for no token); a lane has
-// 8 positions, whose tokens (read side by side, and handed over in LDS) it keeps.
+// Few tokens and channels (16 x 15 x 60000 bfloat16, five tokens: 11.7 us, 17.8 by tiles; 36 MB at 3.1 TB/s, 1920 workgroups that read and then
+// write once): the workgroup's channels of the whole table, scaled and rounded, lie in LDS (and a row of zeros for no token); a lane has 8
+// positions, whose tokens (read side by side, and handed over in LDS) it keeps.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void embed_few_kernel(LookArgs a) {
     using T = typename RowElem<BF16>::type;
@@ -140,13 +143,14 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 }
 
 // ---- backward, few tokens: a product with truth values ----------------------------------------------------------------------
-// Bound by memory for tens of tokens (16 x 15 x 60000 bfloat16, five: 12.8 us, 36 MB), by the vector units for hundreds (12 x 49 x 4999 float, 257:
-// 22 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
+// Tens of tokens: 16 x 15 x 60000 bfloat16, five, 12.8 us, 36 MB at 2.8 TB/s, since each of 1888 workgroups has one block, a chain of loads,
+// product and stores.  Hundreds: bound by the vector units (12 x 49 x 4999 float, 257: 22 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
 // B operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum
 // they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
 // running sum by ordinary additions; of a float, the upper 8 bits by themselves: 32 of them add up to 24 bits and lose nothing as long as their
-// exponents are less than 11 apart (all three parts in one sum, 12 x 49 x 4999, 257 tokens: error against 64 bits 1.3e-7 of the norm).  A value that is not finite would reach every token (0 * NaN): where a sum is not finite, the
-// wave workgroup goes through its positions again without such values, which are then added where they belong.
+// exponents are less than 11 apart (all three parts in one sum, 12 x 49 x 4999, 257 tokens: error against 64 bits 1.3e-7 of the norm).  A value that
+// is not finite would reach every token (0 * NaN): where a sum is not finite, the workgroup goes through its positions again without such
+// values, which are then added where they belong.
 constexpr int kFewTokens = 65520;  // (16 bits each, 0xffff is no token)
 
 struct FewArgs {
@@ -800,7 +804,8 @@ __global__ __launch_bounds__(kThreads) void embed_sums_kernel(SumArgs a) {
     put(behind ? a.tail + side : a.dtable + static_cast<long>(key) * a.D + d, behind ? 1.f : a.scale, behind, sum);
 }
 
-// Runs that cross the rows of one workgroup, its chunk here: what the chunks behind the one where a run begins have of it is added to that one's, by that chunk's lane group
+// Runs that cross the rows of one workgroup, its chunk here: what the chunks behind the one where a run begins have of it is added to that one's,
+// by that chunk's lane group
 // where those are few, by the whole workgroup where a run is long.  A chain of trips through memory (7 us), which is why all that may be
 // needed is loaded at once.
 struct JoinArgs {
@@ -1022,14 +1027,15 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
 }
 // Whether the gradient is taken as a product, by what the two take, in us.
 // Product: 12, 6.5e-9 for each token x channel x position of whole blocks (in tiles of 16; floats 1.7e-8), its partial sums' way to memory and
-// back, and the blocks that a sample's end cuts: their numbers are loaded one by one, and a workgroup goes through its samples in turn.
+// back, 5e-4 for each workgroup that joins 16 of them, and the blocks that a sample's end cuts: their numbers are loaded one by one, and a workgroup goes through its samples in turn.
 // Sort: 11, 20 more up to 20000 positions, 10 a pass, clearing the gradient, and the larger of 6.5e-5 a position and 5e-3 a tile that is turned; what
 // does not stay in the caches goes to memory and back.
 // Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 49, 128 tokens 40 and 46, 256 tokens 65 and 55; 8 x 128 x 20000 256 tokens
 // 43 and 53, 512 tokens 70 and 53; 12 x 49 x 4999 float 256 tokens 32 and 52, 1024 tokens 68 and 51; 16 x 15 x 60000 512 tokens 73 and 104, 1024
 // tokens 121 and 106.  Short samples: 20000 x 8 x 16, 600 tokens 1396 and 112; 20000 x 64 x 16, 64 tokens 580 and 114; 4000 x 64 x 4, 64 tokens
-// 64 and 42; 1000 x 64 x 200, 64 tokens 36 and 40; 16 x 64 x 100, 64 tokens 14 and 21; 20000 x 16 x 2 float, 16 tokens 53 and 169.  (Of 641 sizes the
-// slower way was taken at 182 for more than 1.2 times the time, up to 12.5, before cut blocks counted, now at 52, up to 2.7.)
+// 64 and 42; 1000 x 64 x 200, 64 tokens 36 and 40; 16 x 64 x 100, 64 tokens 14 and 21; 20000 x 16 x 2 float, 16 tokens 53 and 169.  Many tokens, few
+// positions: 2 x 110 x 2 float, 31203 tokens 132 and 20; 1 x 55 x 26 bfloat16, 23921 tokens 65 and 22.  (Of 641 sizes the slower way was taken at 182
+// for more than 1.2 times the time, up to 12.5, by positions alone, now at 47, up to 2.7.)
 bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     if (!turned || V > kFewTokens) return false;
     const FewPlan p = few_plan(N, D, L, V, dtype);
@@ -1037,7 +1043,7 @@ bool is_few(int N, int D, int L, int V, int dtype, bool turned) {
     const double M = static_cast<double>(N) * L, tile = static_cast<double>(p.Vp) * p.Dp, us_a_byte = 1 / 5.2e6;
     const double whole = M - static_cast<double>(N) * (L % p.block), cut = L % p.block ? static_cast<double>(N) * p.vgroups * p.dgroups : 0;
     const double ends = cut * (p.DB == 1 ? (bf16 ? 8e-3 : 4e-3) : bf16 ? 28e-3 : 15e-3) * (L < 16 ? (L + 8) / 24.0 : 1.0), turns = 3.0 * (p.samples - 1);
-    const double product = 12 + whole * tile * (bf16 ? 6.5e-9 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte + (ends > turns ? ends : turns);
+    const double product = 12 + whole * tile * (bf16 ? 6.5e-9 : 1.7e-8) + 8 * tile * p.chunks * us_a_byte + 5e-4 * tile / 16 + (ends > turns ? ends : turns);
     const double turned_tiles = static_cast<double>(N) * cdiv(L, kTurn / tile_channels(D)) * cdiv(D, tile_channels(D));
     const double sorts = 6.5e-5 * M > 5e-3 * turned_tiles ? 6.5e-5 * M : 5e-3 * turned_tiles, beyond = M * D * (bf16 ? 2 : 4) - 32e6;
     const double sort = 11 + (M < 20000 ? M / 1000 : 20) + (V < 256 ? 10 : V < 65536 ? 20 : 30) + sorts + 4.0 * V * D * us_a_byte +
