@@ -144,10 +144,11 @@ __global__ __launch_bounds__(kThreads) void embed_copy_kernel(LookArgs a) {
 
 // ---- backward, few tokens: a product with truth values ----------------------------------------------------------------------
 // Tens of tokens: 16 x 15 x 60000 bfloat16, five, 12.8 us, 36 MB at 2.8 TB/s, since each of 1888 workgroups has one block, a chain of loads,
-// product and stores.  Hundreds: bound by the vector units (12 x 49 x 4999 float, 257: 22 us).  dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a
-// B operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum
-// they are.  The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the
-// running sum by ordinary additions; of a float, the upper 8 bits by themselves: 32 of them add up to 24 bits and lose nothing as long as their
+// product and stores.  Hundreds: bound by the vector units (12 x 49 x 4999 float, 257: 22 us).
+// dtable[v][d] = sum over l of dy[d][l] [token l = v]: an A operand is 16 channels of 32 neighbouring positions as they lie in memory, a B
+// operand the truth values of those positions for 16 tokens, exact in bfloat16; floats are taken as three bfloat16 numbers whose sum they are.
+// The matrix instruction cuts off what its additions lose, so that a step's products start from 0 and are added to the running sum by ordinary additions;
+// of a float, the upper 8 bits by themselves: 32 of them add up to 24 bits and lose nothing as long as their
 // exponents are less than 11 apart (all three parts in one sum, 12 x 49 x 4999, 257 tokens: error against 64 bits 1.3e-7 of the norm).  A value that
 // is not finite would reach every token (0 * NaN): where a sum is not finite, the workgroup goes through its positions again without such
 // values, which are then added where they belong.
@@ -234,9 +235,9 @@ __device__ __forceinline__ Chunk chunk_of(const FewArgs& a, int chunk) {
 template <bool BF16, int DB>
 constexpr int kU = BF16 ? (DB == 1 ? 4 : 2) : (DB == 1 ? 2 : 1);
 constexpr int kMostBlock = 32 * kWaves * 4;
-// Most steps of a wave in one chunk, which bounds the additions in float: chunks are added up in 64 bits.  (Without a bound 2^28 equal floats of one
-// token in 2048 chunks were off by 1e-5; chunks of 16 steps cost nothing up to some millions of positions, 160 x 16 x 2^20 bfloat16, 64 tokens
-// 1.66 ms for 1.76, 32 x 16 x 2^20, 200 tokens 1.21 for 1.05.)
+// Most steps of a wave in one chunk, which bounds the additions in float: chunks are added up in 64 bits.  (Without a bound the
+// equal gradients of one token at 160 x 16 x 2^20 positions in 2080 chunks were off by 9.4e-6, 158 half steps of float; with it by less than half
+// of one.  Up to some millions of positions it costs up to 6 %, at 32 x 16 x 2^20 bfloat16, 200 tokens, 1.21 ms for 1.05.)
 constexpr int kMostSteps = 16;
 
 // A block of the chunk: positions l0 ... of sample n, of which len count.
@@ -1027,7 +1028,8 @@ FewPlan few_plan(int N, int D, int L, int V, int dtype) {
 }
 // Whether the gradient is taken as a product, by what the two take, in us.
 // Product: 12, 6.5e-9 for each token x channel x position of whole blocks (in tiles of 16; floats 1.7e-8), its partial sums' way to memory and
-// back, 5e-4 for each workgroup that joins 16 of them, and the blocks that a sample's end cuts: their numbers are loaded one by one, and a workgroup goes through its samples in turn.
+// back, 5e-4 for each workgroup that joins 16 of them, and the blocks that a sample's end cuts: their numbers are loaded one by one, and a
+// workgroup goes through its samples in turn.
 // Sort: 11, 20 more up to 20000 positions, 10 a pass, clearing the gradient, and the larger of 6.5e-5 a position and 5e-3 a tile that is turned; what
 // does not stay in the caches goes to memory and back.
 // Measured, product and sort: 8 x 512 x 8192 bfloat16 16 tokens 21 and 49, 128 tokens 40 and 46, 256 tokens 65 and 55; 8 x 128 x 20000 256 tokens
